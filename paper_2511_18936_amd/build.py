@@ -19,15 +19,19 @@ BENCH_LIB = os.path.join(HERE, "libswanbench.so")
 BENCH_SOURCES = ["stream_ceiling.hip"]
 SOURCES = ["swan_api.hip", "decode.hip", "decode_gqa.hip", "decode_asym.hip",
            "decode_gqa_asym.hip", "decode_fused.hip", "compress.hip", "prefill.hip",
-           "change_k.hip", "rope.hip", "calibrate.hip"]
+           "change_k.hip", "rope.hip", "calibrate.hip", "qkv_rows.hip", "attend_pages.hip",
+           "attend_dense.hip", "attend_rows.hip"]
 ARCH = "gfx950"
-# per-source flags: the GQA kernels and the prefill rotation keep their MFMA
-# accumulators in VGPRs (the default puts them in AGPRs and copies them across
+# per-source flags: the GQA and several-row attention kernels and the prefill rotation
+# keep their MFMA accumulators in VGPRs (the default puts them in AGPRs and copies them across
 # for the VALU work on them: the per-page rescale, the per-element conversion)
 SOURCE_FLAGS = {
     "decode_gqa.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "decode_gqa_asym.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "prefill.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+    "attend_pages.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+    "attend_dense.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+    "attend_rows.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
 }
 FLAGS = [
     "-O3", "-std=c++17", "-fPIC", "-shared", f"--offload-arch={ARCH}",

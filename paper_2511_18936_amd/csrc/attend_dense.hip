@@ -1,0 +1,294 @@
+// Attention of the rows of a prompt (causal), or of rows over another sequence's keys and
+// values: dense tiles of attend.h, continued from a state where one is given.
+#include "attend.h"
+
+namespace swan {
+
+// One tile's rows of k and v in flight: thread t holds 16-byte pieces t, t + 256, ... of K
+// and, of V, E dims (16 bytes) of each of 4 keys, which it writes transposed.
+template <typename T>
+struct Stage {
+  static constexpr int E = 16 / (int)sizeof(T);           // elements of a piece
+  static constexpr int kPieces = kTileKeys * kD / E / 256; // per thread: 4 (binary16) or 8
+  static constexpr int kSets = kPieces / 4;                // of 4 keys x E dims
+  u32x4 k[kPieces], v[kSets][4];
+
+  // rows `key0`.. of k and v (row 0 at kp, vp), zeros from row `keys` on
+  __device__ __forceinline__ void load(const T* kp, const T* vp, int key0, int keys, int tid) {
+    const u32x4 zero = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int x = 0; x < kPieces; ++x) {
+      const int piece = tid + 256 * x, r = key0 + piece / (kD / E);
+      k[x] = r < keys ? *(const u32x4*)(kp + (int64_t)r * kD + piece % (kD / E) * E) : zero;
+    }
+#pragma unroll
+    for (int x = 0; x < kSets; ++x) {
+      const int set = tid + 256 * x, dim = set / (kTileKeys / 4) * E;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int r = key0 + set % (kTileKeys / 4) * 4 + e;
+        v[x][e] = r < keys ? *(const u32x4*)(vp + (int64_t)r * kD + dim) : zero;
+      }
+    }
+  }
+
+  // Values that are no numbers leave the tile (0 times them would be NaN in the rows that
+  // must not see their key): 1 where a key of this thread has one.  Returns bits of keys.
+  __device__ __forceinline__ uint64_t take_nonfinite(int tid) {
+    uint64_t keys = 0;
+#pragma unroll
+    for (int x = 0; x < kSets; ++x)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int key = (tid + 256 * x) % (kTileKeys / 4) * 4 + e;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          if constexpr (sizeof(T) == 4) {
+            if ((v[x][e][w] & 0x7F800000u) == 0x7F800000u) {
+              v[x][e][w] = 0u;
+              keys |= 1ull << key;
+            }
+          } else {
+            if ((v[x][e][w] & 0x7C00u) == 0x7C00u) {
+              v[x][e][w] &= 0xFFFF0000u;
+              keys |= 1ull << key;
+            }
+            if ((v[x][e][w] & 0x7C000000u) == 0x7C000000u) {
+              v[x][e][w] &= 0xFFFFu;
+              keys |= 1ull << key;
+            }
+          }
+        }
+      }
+    return keys;
+  }
+
+  __device__ __forceinline__ void store(typename Tile<T>::Buf& b, int tid) const {
+    using Tl = Tile<T>;
+#pragma unroll
+    for (int x = 0; x < kPieces; ++x) {
+      const int piece = tid + 256 * x;
+      *(u32x4*)(b.k + piece / (kD / E) * Tl::KS + piece % (kD / E) * E) = k[x];
+    }
+#pragma unroll
+    for (int x = 0; x < kSets; ++x) {
+      const int set = tid + 256 * x, dim = set / (kTileKeys / 4) * E;
+      T* to = b.v + dim * Tl::VS + Tl::col(set % (kTileKeys / 4) * 4);
+      if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          *(u32x4*)(to + e * Tl::VS) = u32x4{v[x][0][e], v[x][1][e], v[x][2][e], v[x][3][e]};
+      } else {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          // dims 2 w and 2 w + 1 of the four keys
+          const u32x2 even = {__builtin_amdgcn_perm(v[x][1][w], v[x][0][w], 0x05040100u),
+                              __builtin_amdgcn_perm(v[x][3][w], v[x][2][w], 0x05040100u)};
+          const u32x2 odd = {__builtin_amdgcn_perm(v[x][1][w], v[x][0][w], 0x07060302u),
+                             __builtin_amdgcn_perm(v[x][3][w], v[x][2][w], 0x07060302u)};
+          *(u32x2*)(to + 2 * w * Tl::VS) = even;
+          *(u32x2*)(to + (2 * w + 1) * Tl::VS) = odd;
+        }
+      }
+    }
+  }
+};
+
+// O += p v for the values that take_nonfinite() took out of the tile, key by key, in the
+// rows that see the key.  Rare: the loops are for size, not for speed.
+template <typename T>
+__device__ __forceinline__ void add_nonfinite(uint64_t keys, const T* vp, int key0, int limit,
+                                              const f16v (&P)[2], int lane, f16v (&O)[4]) {
+#pragma unroll 1
+  while (keys) {
+    const int key = __builtin_ctzll(keys);
+    keys &= keys - 1;
+    float mine = 0.f;  // p of key 8 (key / 8) + 4 (lane / 32) + key % 4
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (key_of(t, i, 0) == (key & ~4)) mine = P[t][i];
+    const f4v both = both_halves(mine);
+    const float p = key & 4 ? both.y : both.x;
+    const T* row = vp + (int64_t)(key0 + key) * kD + 4 * (lane >> 5);
+    if (key0 + key < limit) {
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float v = (float)row[32 * d + 8 * (i >> 2) + (i & 3)];
+          if (!(v - v == 0.f)) O[d][i] += p * v;
+        }
+    }
+  }
+}
+
+// Grid: a.units workgroups of 4 waves.  Unit u of a group: kv head u % Hkv (so that a
+// head's tiles fall to few of the 8 XCDs and its keys stay in their L2), then the split,
+// then the row tile, the last (of a causal prompt the longest) first.
+template <typename T>
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kernel(AttendLaunch a) {
+  using Tl = Tile<T>;
+  __shared__ typename Tl::Buf buf[2];
+  __shared__ uint64_t odd_keys;  // keys of a tile with values that are no numbers
+  __shared__ int any_odd;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int G = a.Hq / a.Hkv;
+  const int j = group_of(a, blockIdx.x);
+  int u = blockIdx.x - a.unit0[j];
+  const int h = u % a.Hkv;
+  u /= a.Hkv;
+  const int nsplit = a.nsplit[j], split = u % nsplit;
+  const int toks = a.toks[j], keys = a.keys[j];
+  const int tiles = (int)(((int64_t)toks * G + kTileRows - 1) / kTileRows);
+  const int64_t row0 = (int64_t)(tiles - 1 - u / nsplit) * kTileRows;
+  const int b = a.cseq[j];
+
+  // this lane's row
+  const int64_t r = row0 + 32 * wave + (lane & 31);
+  const int tok = (int)(r / G), g = (int)(r % G);
+  const bool live = tok < toks;
+  const int64_t row = ((int64_t)b * a.Hq + h * G + g) * a.n + tok;
+  const int shift = keys - toks;  // causal: row i sees keys up to i + shift
+  const int limit = !live ? 0 : a.causal ? min(keys, max(0, tok + shift + 1)) : keys;
+  // keys that every row of the wave sees, and that some row of the workgroup sees
+  const int tok_first = (int)((row0 + 32 * wave) / G);
+  const int64_t tok_last = min((int64_t)toks - 1, (row0 + kTileRows - 1) / G);
+  const int all_see = a.causal ? min(keys, max(0, tok_first + shift + 1)) : keys;
+  const int block_all = a.causal ? min(keys, max(0, (int)(row0 / G) + shift + 1)) : keys;
+  const int seen = a.causal ? (int)min((int64_t)keys, max((int64_t)0, tok_last + shift + 1)) : keys;
+  const int wave_last = (int)min((int64_t)toks - 1, (row0 + 32 * wave + 31) / G);
+  const int wave_sees = tok_first >= toks ? 0
+                        : a.causal ? min(keys, max(0, wave_last + shift + 1)) : keys;
+  const int nt = (seen + kTileKeys - 1) / kTileKeys;
+  const int t0 = (int)((int64_t)nt * split / nsplit), t1 = (int)((int64_t)nt * (split + 1) / nsplit);
+
+  const int64_t kv0 = ((int64_t)b * a.Hkv + h) * a.m * kD;
+  const T* kp = (const T*)a.k + kv0;
+  const T* vp = (const T*)a.v + kv0;
+  Stage<T> st;
+  if (tid == 0) any_odd = 0;
+  if (t0 < t1) st.load(kp, vp, t0 * kTileKeys, keys, tid);
+
+  typename Tl::template Q<false> q;
+  {
+    const T* qr = (const T*)a.q + row * kD;
+    constexpr int N = sizeof(q.hi) / 16, E = Stage<T>::E;
+    u32x4* to = (u32x4*)&q;
+#pragma unroll
+    for (int s = 0; s < N; ++s)
+      to[s] = live ? *(const u32x4*)(qr + 2 * E * s + E * (lane >> 5)) : u32x4{0u, 0u, 0u, 0u};
+  }
+  RowState rs;
+  rs.clear();
+  if (a.o0 && live && !a.part) {
+    const float lse = a.lse0[row] * kLog2e;
+    if (lse != -INFINITY) {
+      rs.ref = lse - kHead;
+      rs.l = lane < 32 ? 128.f : 0.f;  // 2^kHead
+      const float* o = a.o0 + row * kD + 4 * (lane >> 5);
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const f4v x = *(const f4v*)(o + 32 * d + 8 * i);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) rs.O[d][4 * i + e] = x[e] * 128.f;
+        }
+    }
+  }
+  __syncthreads();  // any_odd
+  auto put = [&](int t) {
+    // only tiles that some row sees in part are looked through
+    if ((t + 1) * kTileKeys > block_all && st.take_nonfinite(tid)) any_odd = 1;
+    st.store(buf[(t - t0) & 1], tid);
+  };
+  if (t0 < t1) {
+    put(t0);
+    if (t0 + 1 < t1) st.load(kp, vp, (t0 + 1) * kTileKeys, keys, tid);
+  }
+  __syncthreads();
+  for (int t = t0; t < t1; ++t) {
+    const typename Tl::Buf& tb = buf[(t - t0) & 1];
+    const int key0 = t * kTileKeys;
+    if (key0 < wave_sees) {  // uniform in the wave
+      f16v S[2];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) S[0][i] = S[1][i] = 0.f;
+      Tl::template scores<false>(tb, q, lane, S);
+      if (key0 + kTileKeys > all_see) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (key0 + key_of(x, i, lane) >= limit) S[x][i] = -INFINITY;
+      }
+      rs.raise(tile_max(S) * a.qmult);
+      rs.l += Tl::values(tb, S, a.qmult, rs.safe_ref(), lane, rs.O);
+    }
+    if (t + 1 < t1) {
+      put(t + 1);
+      if (t + 2 < t1) st.load(kp, vp, (t + 2) * kTileKeys, keys, tid);
+    }
+    __syncthreads();
+  }
+  if (any_odd) {  // uniform: their keys' values, with the scores taken again
+#pragma unroll 1
+    for (int t = max(t0, block_all / kTileKeys); t < t1; ++t) {
+      const int key0 = t * kTileKeys;
+      if (tid == 0) odd_keys = 0;
+      st.load(kp, vp, key0, keys, tid);
+      __syncthreads();
+      const uint64_t mine = st.take_nonfinite(tid);
+      if (mine) atomicOr((unsigned long long*)&odd_keys, (unsigned long long)mine);
+      st.store(buf[0], tid);
+      __syncthreads();
+      const uint64_t odd = odd_keys;
+      if (odd && key0 < wave_sees) {
+        f16v P[2];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) P[0][i] = P[1][i] = 0.f;
+        Tl::template scores<false>(buf[0], q, lane, P);
+        const float ref = rs.safe_ref();
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            P[x][i] = __builtin_amdgcn_exp2f(fmaf(P[x][i], a.qmult, -ref));
+        add_nonfinite(odd, vp, key0, limit, P, lane, rs.O);
+      }
+      __syncthreads();
+    }
+  }
+  if (a.part) {
+    write_partial(a, rs, row, split, live, lane);
+    return;
+  }
+  const float l = sum_halves(rs.l);
+  if (!live) return;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  T* out = (T*)a.out + row * kD + 4 * (lane >> 5);
+#pragma unroll
+  for (int d = 0; d < 4; ++d)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      struct alignas(4 * sizeof(T)) {
+        T v[4];
+      } y;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y.v[e] = (T)(rs.O[d][4 * i + e] * inv);
+      *(decltype(y)*)(out + 32 * d + 8 * i) = y;
+    }
+}
+
+hipError_t launch_attend_dense(const AttendLaunch& a) {
+  if (a.dtype == SWAN_F32)
+    hipLaunchKernelGGL(attend_dense_kernel<float>, dim3(a.units), dim3(256), 0, a.stream, a);
+  else
+    hipLaunchKernelGGL(attend_dense_kernel<_Float16>, dim3(a.units), dim3(256), 0, a.stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace swan

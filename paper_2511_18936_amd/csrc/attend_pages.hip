@@ -1,0 +1,251 @@
+// Attention of many query rows over the pruned pages and the ring of a cache: a page's
+// kept components are scattered into a dense tile of attend.h in LDS (its pruned zeros
+// beside them), once for all query rows of the workgroup, then multiplied on MFMA.
+//
+// The rotated queries are float32.  On the binary16 formats each row is brought by a power
+// of two to 2^13 .. 2^14 at its largest component and split into two binary16 parts, whose
+// products with the keys are both taken: 22 bits, as the decode kernels' float32 queries
+// against binary16 keys but for the last two.
+#include <type_traits>
+
+#include "attend.h"
+
+namespace swan {
+
+// Groups of 8 entries of both roles' pages, numbered keys first, go to the 4 waves round
+// robin; a lane holds its token's 8 values and indices of each.
+template <typename T, int NU>
+struct PageStage {
+  static constexpr int CB = Fmt<T>::kChunkBytes;
+  static constexpr int VCH = 8 * Fmt<T>::kValBytes / CB;
+  using Chunk = typename std::conditional<CB == 16, u32x4, u32x2>::type;
+  Chunk val[NU][VCH];
+  u32x2 idx[NU];
+
+  __device__ __forceinline__ void load(const char* kpage, const char* vpage, int nk, int nv,
+                                       int wave, int lane) {
+#pragma unroll
+    for (int x = 0; x < NU; ++x) {
+      const int u = wave + 4 * x;  // uniform
+      if (u < nk + nv) {
+        const bool key = u < nk;
+        const char* page = key ? kpage : vpage;
+        const int g = key ? u : u - nk, n8 = key ? nk : nv;
+#pragma unroll
+        for (int c = 0; c < VCH; ++c)
+          val[x][c] = *(const Chunk*)(page + (g * VCH + c) * 64 * CB + lane * CB);
+        idx[x] = *(const u32x2*)(page + n8 * VCH * 64 * CB + g * 512 + lane * 8);
+      }
+    }
+  }
+
+  __device__ __forceinline__ void scatter(typename Tile<typename Fmt<T>::Elem>::Buf& b, int nk,
+                                          int nv, int wave, int lane, bool valid) const {
+    using E = typename Fmt<T>::Elem;
+    using Tl = Tile<E>;
+    if (!valid) return;
+    E* kt = b.k + lane * Tl::KS;
+    E* vt = b.v + Tl::col(lane);
+#pragma unroll
+    for (int x = 0; x < NU; ++x) {
+      const int u = wave + 4 * x;
+      if (u < nk + nv) {
+        E* to = u < nk ? kt : vt;
+        const int step = u < nk ? 1 : Tl::VS;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int d = ((e < 4 ? idx[x].x : idx[x].y) >> (8 * (e & 3))) & 0x7F;
+          to[d * step] = value(x, e);
+        }
+      }
+    }
+  }
+
+  __device__ __forceinline__ typename Fmt<T>::Elem value(int x, int e) const {
+    if constexpr (sizeof(T) == 4) {
+      return __uint_as_float(val[x][e >> 2][e & 3]);
+    } else if constexpr (Fmt<T>::kValBytes == 1) {
+      const uint32_t w = e < 4 ? val[x][0].x : val[x][0].y;
+      const h2v two = (e & 2) ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, true)
+                              : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, false);
+      return (e & 1) ? two.y : two.x;
+    } else {
+      const uint32_t w = val[x][0][e >> 1];
+      return __builtin_bit_cast(_Float16, (uint16_t)((e & 1) ? w >> 16 : w & 0xFFFFu));
+    }
+  }
+};
+
+// 64 rows of the ring (zeros past its end) into a tile
+template <typename E>
+__device__ __forceinline__ void ring_tile(typename Tile<E>::Buf& b, const E* kr, const E* vr,
+                                          int row0, int rows, int tid) {
+  using Tl = Tile<E>;
+  constexpr int N = 16 / (int)sizeof(E);
+  const u32x4 zero = {0u, 0u, 0u, 0u};
+#pragma unroll 4
+  for (int piece = tid; piece < kTileKeys * kD / N; piece += 256) {
+    const int r = piece / (kD / N), d = piece % (kD / N) * N;
+    const bool in = row0 + r < rows;
+    const int64_t at = (int64_t)(row0 + r) * kD + d;
+    *(u32x4*)(b.k + r * Tl::KS + d) = in ? *(const u32x4*)(kr + at) : zero;
+    const u32x4 v = in ? *(const u32x4*)(vr + at) : zero;
+    struct alignas(16) {
+      E e[N];
+    } x = __builtin_bit_cast(decltype(x), v);
+#pragma unroll
+    for (int e = 0; e < N; ++e) b.v[(d + e) * Tl::VS + Tl::col(r)] = x.e[e];
+  }
+}
+
+// Grid as in attend_dense_kernel.  A group's keys are its pages, then tiles of its ring
+// (in slot order: the sum has none).
+template <typename T, int NU>
+__global__ __launch_bounds__(256, sizeof(typename Fmt<T>::Elem) == 2 ? 2 : 1) void
+attend_pages_kernel(AttendLaunch a) {
+  using E = typename Fmt<T>::Elem;
+  using Tl = Tile<E>;
+  __shared__ typename Tl::Buf buf[2];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int G = a.Hq / a.Hkv;
+  const int j = group_of(a, blockIdx.x);
+  int u = blockIdx.x - a.unit0[j];
+  const int h = u % a.Hkv;
+  u /= a.Hkv;
+  const int nsplit = a.nsplit[j], split = u % nsplit;
+  const int toks = a.toks[j], L = a.keys[j], cs = a.cseq[j];
+  const int64_t r = (int64_t)(u / nsplit) * kTileRows + 32 * wave + (lane & 31);
+  const int tok = (int)(r / G), g = (int)(r % G);
+  const bool live = tok < toks;
+  const bool busy = ((int64_t)(u / nsplit) * kTileRows + 32 * wave) / G < toks;  // some row is
+  int b = 0, i = 0;
+  if (live) token_at(a, j, tok, b, i);
+  const int64_t row = ((int64_t)b * a.Hq + h * G + g) * a.n + i;
+
+  const int S = L > a.bb ? L - a.bb : 0, np = pages_for(S), nb = L < a.bb ? L : a.bb;
+  const int nt = np + (nb + kTileKeys - 1) / kTileKeys;
+  const int t0 = (int)((int64_t)nt * split / nsplit), t1 = (int)((int64_t)nt * (split + 1) / nsplit);
+  const int nk = kpad_of(a.kact[0][j]) / 8, nv = kpad_of(a.kact[1][j]) / 8;
+  const int64_t kbytes = page_bytes_of(Fmt<T>::kValBytes, 8 * nk);
+  const int64_t vbytes = page_bytes_of(Fmt<T>::kValBytes, 8 * nv);
+  const char* kpages = (const char*)a.k + a.off[0][j] + (int64_t)h * a.npc * kbytes;
+  const char* vpages = (const char*)a.v + a.off[1][j] + (int64_t)h * a.npc * vbytes;
+  const int64_t ring = ((int64_t)cs * a.Hkv + h) * a.bb * kD;
+
+  PageStage<T, NU> st;
+  auto load = [&](int t) {
+    if (t < np) st.load(kpages + t * kbytes, vpages + t * vbytes, nk, nv, wave, lane);
+  };
+  if (t0 < t1) load(t0);
+
+  // the row's queries
+  typename Tl::template Q<true> q;
+  float c = 1.f;
+  {
+    const float* qr = (const float*)a.q + row * kD;
+    if constexpr (sizeof(E) == 4) {
+#pragma unroll
+      for (int s = 0; s < 16; ++s)
+        q.hi[s] = live ? *(const f4v*)(qr + 8 * s + 4 * (lane >> 5)) : f4v{0.f, 0.f, 0.f, 0.f};
+    } else {
+      float x[64], top = 0.f;
+#pragma unroll
+      for (int s = 0; s < 16; ++s) {
+        const f4v v = live ? *(const f4v*)(qr + 16 * (s >> 1) + 8 * (lane >> 5) + 4 * (s & 1))
+                           : f4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          x[4 * s + e] = v[e];
+          top = fmaxf(top, fabsf(v[e]));
+        }
+      }
+      top = max_halves(top);
+      // 2^(13 - exponent); a row of zeros, infinities or NaNs as it is
+      const int ex = (int)((__float_as_uint(top) >> 23) & 0xFF) - 127;
+      const int up = top > 0.f && ex < 128 ? 13 - (ex < -100 ? -100 : ex) : 0;
+      const float f = __builtin_ldexpf(1.f, up);
+      c = __builtin_ldexpf(1.f, -up);
+#pragma unroll
+      for (int s = 0; s < 8; ++s)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float y = x[8 * s + e] * f;
+          const _Float16 hi = (_Float16)y;
+          q.hi[s][e] = hi;
+          q.lo[s][e] = (_Float16)(y - (float)hi);
+        }
+    }
+  }
+  RowState rs;
+  rs.clear();
+  auto clear = [&](int t) {  // a page's tile starts from zeros; its stores follow a barrier
+    if (t >= np) return;
+    u32x4* z = (u32x4*)&buf[(t - t0) & 1];
+    for (int x = tid; x < (int)(sizeof(buf[0]) / 16); x += 256) z[x] = u32x4{0u, 0u, 0u, 0u};
+  };
+  auto put = [&](int t) {
+    typename Tl::Buf& tb = buf[(t - t0) & 1];
+    if (t < np) st.scatter(tb, nk, nv, wave, lane, t * kPage + lane < S);
+    else
+      ring_tile<E>(tb, (const E*)a.k_ring + ring, (const E*)a.v_ring + ring,
+                   (t - np) * kTileKeys, nb, tid);
+  };
+  if (t0 < t1) {
+    clear(t0);
+    __syncthreads();
+    put(t0);
+    if (t0 + 1 < t1) load(t0 + 1);
+    __syncthreads();
+  }
+  for (int t = t0; t < t1; ++t) {
+    if (t + 1 < t1) {
+      clear(t + 1);
+      __syncthreads();
+      put(t + 1);
+      if (t + 2 < t1) load(t + 2);
+    }
+    if (busy) {
+      const typename Tl::Buf& tb = buf[(t - t0) & 1];
+      f16v Sc[2];
+#pragma unroll
+      for (int x = 0; x < 16; ++x) Sc[0][x] = Sc[1][x] = 0.f;
+      Tl::template scores<true>(tb, q, lane, Sc);
+      const int count = t < np ? S - t * kPage : nb - (t - np) * kTileKeys;
+      if (count < kTileKeys) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (key_of(x, e, lane) >= count) Sc[x][e] = -INFINITY;
+      }
+      rs.raise(tile_max(Sc) * c);
+      rs.l += Tl::values(tb, Sc, c, rs.safe_ref(), lane, rs.O);
+    }
+    __syncthreads();
+  }
+  write_partial(a, rs, row, split, live, lane);
+}
+
+template <typename T>
+static hipError_t launch_pages_t(const AttendLaunch& a) {
+  // registers for 4 or 8 groups a wave in flight: up to 128 components of both roles, or 256
+  int most = 0;
+  for (int j = 0; j < a.groups; ++j) {
+    const int n = kpad_of(a.kact[0][j]) / 8 + kpad_of(a.kact[1][j]) / 8;
+    most = n > most ? n : most;
+  }
+  if (most <= 16)
+    hipLaunchKernelGGL((attend_pages_kernel<T, 4>), dim3(a.units), dim3(256), 0, a.stream, a);
+  else
+    hipLaunchKernelGGL((attend_pages_kernel<T, 8>), dim3(a.units), dim3(256), 0, a.stream, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_attend_pages(const AttendLaunch& a) {
+  if (a.dtype == SWAN_F32) return launch_pages_t<float>(a);
+  if (a.dtype == SWAN_F16_E4M3) return launch_pages_t<E4M3V>(a);
+  return launch_pages_t<_Float16>(a);
+}
+
+}  // namespace swan

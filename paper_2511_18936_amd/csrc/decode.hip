@@ -238,6 +238,7 @@ static hipError_t launch_decode_t(const DecodeLaunch& a) {
     }
     if ((e = launch_attn_fused(a, f)) != hipSuccess) return e;
     if (a.prof_stop && (e = hipEventRecord(a.prof_stop, a.stream)) != hipSuccess) return e;
+    if (a.leave_partials) return hipSuccess;
     hipLaunchKernelGGL(merge_kernel<E>, dim3(BH), dim3(128), 0, a.stream, a);
     return hipGetLastError();
   }
@@ -300,6 +301,7 @@ static hipError_t launch_decode_t(const DecodeLaunch& a) {
     }
   }
   if (a.prof_stop && (e = hipEventRecord(a.prof_stop, a.stream)) != hipSuccess) return e;
+  if (a.leave_partials) return hipSuccess;
   hipLaunchKernelGGL(merge_kernel<E>, dim3(BH), dim3(128), 0, a.stream, a);
   return hipGetLastError();
 }

@@ -13,6 +13,7 @@
 #include "swan.h"
 #include "swan_cache_ops.h"
 #include "swan_layer.h"
+#include "swan_layer_ops.h"
 
 // ---------------------------------------------------------------------------
 // Scratch of swan_decode_attention_noalloc: the decode workspace (q_hat, then
@@ -332,7 +333,7 @@ swan_status decode_prep(const swan_cache* c, const int32_t* seq_len_host,
                         const int32_t* k_active_host, const int32_t* k_value_host, const void* q,
                         const float* P_qk, const float* P_vo, float scale, void* out,
                         void* workspace, size_t workspace_bytes, void* stream, bool no_alloc,
-                        swan::DecodeLaunch& a) {
+                        swan::DecodeLaunch& a, int least = 1) {
   swan_status st = check_cache_shape(c);
   if (st != SWAN_OK) return st;
   if ((st = check_k(c, k_active_host, k_value_host)) != SWAN_OK) return st;
@@ -343,7 +344,8 @@ swan_status decode_prep(const swan_cache* c, const int32_t* seq_len_host,
     return fail(SWAN_ERR_INVALID_ARG, "P_qk / P_vo must be 16-byte aligned");
   for (int b = 0; b < c->batch; ++b) {
     const int64_t L = seq_len_host[b];
-    if (L < 1) return fail(SWAN_ERR_INVALID_ARG, "seq_len[%d] = %lld: need L >= 1", b, (long long)L);
+    if (L < least)
+      return fail(SWAN_ERR_INVALID_ARG, "seq_len[%d] = %lld: need L >= %d", b, (long long)L, least);
     if (L - c->buffer_tokens > c->sparse_capacity)
       return fail(SWAN_ERR_CAPACITY, "sequence %d has %lld sparse tokens, capacity %d", b,
                   (long long)(L - c->buffer_tokens), c->sparse_capacity);
@@ -407,6 +409,362 @@ swan_status decode_impl(const swan_cache* c, const int32_t* seq_len_host,
                                      no_alloc, a);
   if (st != SWAN_OK) return st;
   return hip_status(swan::launch_decode(a), "decode launch");
+}
+
+// A decode step's validation, the compress part's and the attention's, into `ca` and `da`
+swan_status step_prep(const swan_cache* c, const int32_t* seq_len_host,
+                      const int32_t* k_active_host, const int32_t* k_value_host,
+                      const void* k_new, const void* v_new, const void* q, const float* P_qk,
+                      const float* P_vo, float scale, void* out, void* workspace,
+                      size_t workspace_bytes, void* stream, swan::CompressLaunch& ca,
+                      swan::DecodeLaunch& da) {
+  bool any_new = false;
+  swan_status st = compress_prep(c, seq_len_host, k_active_host, k_value_host, k_new, v_new, 1,
+                                 nullptr, P_qk, P_vo, stream, ca, any_new);
+  if (st != SWAN_OK) return st;
+  int32_t len1[SWAN_MAX_BATCH];
+  for (int b = 0; b < c->batch; ++b) len1[b] = seq_len_host[b] + 1;
+  st = decode_prep(c, len1, k_active_host, k_value_host, q, P_qk, P_vo, scale, out, workspace,
+                   workspace_bytes, stream, false, da);
+  if (st != SWAN_OK) return st;
+  if (c->n_q_heads / c->n_kv_heads <= swan::kStepQG) {  // the key waves rotate the queries
+    ca.q = q;
+    ca.qhat = da.qhat;
+    ca.Hq = da.Hq;
+    ca.qmult = da.qmult;
+    da.qhat_ready = 1;
+  }
+  return SWAN_OK;
+}
+
+// ---------------------------------------------------------------------------
+// attention of several rows per sequence, and of decode steps behind a prefix
+// ---------------------------------------------------------------------------
+// units of attend kernels that fill the GPU (two workgroups on each of 256 CUs)
+constexpr int64_t kUnits = 512;
+
+swan_status check_scale(float scale) {
+  if (!(scale == scale) || isinf(scale)) return fail(SWAN_ERR_INVALID_ARG, "scale is not finite");
+  if (scale > 0.f && scale < 0x1p-64f)
+    return fail(SWAN_ERR_INVALID_ARG, "scale %g below 2^-64", (double)scale);
+  return SWAN_OK;
+}
+float scale_or_default(float scale) {
+  return scale > 0.f ? scale : 1.0f / sqrtf((float)SWAN_HEAD_DIM);
+}
+
+// every entry of per_host (or NULL) within 0..n
+swan_status check_rows(const char* name, const int32_t* per_host, int32_t batch, int32_t n) {
+  if (n < 0) return fail(SWAN_ERR_INVALID_ARG, "%s %d < 0", name, n);
+  if (n > INT32_MAX / 4) return fail(SWAN_ERR_INVALID_ARG, "%s %d too large", name, n);
+  for (int b = 0; per_host && b < batch; ++b)
+    if (per_host[b] < 0 || per_host[b] > n)
+      return fail(SWAN_ERR_INVALID_ARG, "%s of sequence %d = %d outside 0..%d", name, b,
+                  per_host[b], n);
+  return SWAN_OK;
+}
+
+// A source's checks; queries of `batch` sequences.  need_ptrs: for a launch.
+swan_status check_source(const swan_prefix* s, int32_t batch, bool need_ptrs) {
+  if (!s) return fail(SWAN_ERR_INVALID_ARG, "prefix is NULL");
+  swan_status st = check_cache_shape(s->cache);
+  if (st != SWAN_OK) return st;
+  const swan_cache* c = s->cache;
+  if ((st = check_k(c, s->k_active_host, s->k_value_host)) != SWAN_OK) return st;
+  if (need_ptrs && (st = check_cache_ptrs(c)) != SWAN_OK) return st;
+  if (!s->seq_len_host || !s->of_host)
+    return fail(SWAN_ERR_INVALID_ARG, "prefix: seq_len_host / of_host is NULL");
+  for (int p = 0; p < c->batch; ++p) {
+    const int64_t L = s->seq_len_host[p];
+    if (L < 0 || L > INT32_MAX / 2)
+      return fail(SWAN_ERR_INVALID_ARG, "prefix: seq_len[%d] = %lld", p, (long long)L);
+    if (L - c->buffer_tokens > c->sparse_capacity)
+      return fail(SWAN_ERR_CAPACITY, "prefix: sequence %d has %lld sparse tokens, capacity %d", p,
+                  (long long)(L - c->buffer_tokens), c->sparse_capacity);
+  }
+  for (int b = 0; b < batch; ++b)
+    if (s->of_host[b] < -1 || s->of_host[b] >= c->batch)
+      return fail(SWAN_ERR_INVALID_ARG, "prefix: of[%d] = %d outside -1..%d", b, s->of_host[b],
+                  c->batch - 1);
+  return SWAN_OK;
+}
+
+// key tiles of a cache sequence: pages, then its buffer's
+int key_tiles(const swan_cache* c, int L) {
+  const int S = L > c->buffer_tokens ? L - c->buffer_tokens : 0;
+  return swan::pages_for(S) + swan::pages_for(L < c->buffer_tokens ? L : c->buffer_tokens);
+}
+
+// Groups and splits of a source: one group per cache sequence with tokens and query rows.
+// About kUnits workgroups in all, every split with a tile; used[b] = splits of query
+// sequence b's group (0: none).  Returns the largest.
+int plan_pages(const swan_prefix* s, int32_t batch, int32_t n, const int32_t* n_host,
+               swan::AttendLaunch& a, int16_t* used) {
+  const swan_cache* c = s->cache;
+  const int G = c->n_q_heads / c->n_kv_heads;
+  swan::SeqTab tab;
+  int64_t bytes[2];
+  fill_layout(c, s->k_active_host, s->k_value_host, tab, bytes);
+  a.groups = 0;
+  int entries = 0;
+  int64_t work = 0;
+  int64_t row_tiles[SWAN_MAX_BATCH];
+  for (int b = 0; b < batch; ++b) used[b] = 0;
+  for (int p = 0; p < c->batch; ++p) {
+    if (s->seq_len_host[p] == 0) continue;
+    const int j = a.groups, e0 = entries;
+    int64_t toks = 0;
+    for (int b = 0; b < batch; ++b) {
+      const int nb = n_host ? n_host[b] : n;
+      if (s->of_host[b] != p || nb == 0) continue;
+      a.seq[entries] = (uint8_t)b;
+      a.tok0[entries] = (int32_t)toks;
+      ++entries;
+      toks += nb;
+    }
+    if (!toks) continue;
+    a.first[j] = (uint8_t)e0;
+    a.toks[j] = (int32_t)toks;
+    a.keys[j] = s->seq_len_host[p];
+    a.cseq[j] = (uint8_t)p;
+    for (int r = 0; r < 2; ++r) {
+      a.off[r][j] = tab.page_off[r][p];
+      a.kact[r][j] = (uint8_t)tab.kact[r][p];
+    }
+    row_tiles[j] = (toks * G + swan::kTileRows - 1) / swan::kTileRows;
+    work += row_tiles[j] * key_tiles(c, a.keys[j]);
+    ++a.groups;
+  }
+  a.first[a.groups] = (uint8_t)entries;
+  const int64_t per = (work * c->n_kv_heads + kUnits - 1) / kUnits;  // key tiles of a unit
+  int most = 0;
+  int64_t units = 0;
+  for (int j = 0; j < a.groups; ++j) {
+    const int nt = key_tiles(c, a.keys[j]);
+    int64_t ns = (nt + per - 1) / per;
+    ns = ns > swan::kMaxSlots ? swan::kMaxSlots : ns < 1 ? 1 : ns;
+    a.nsplit[j] = (int16_t)ns;
+    a.unit0[j] = (int32_t)units;
+    units += row_tiles[j] * ns * c->n_kv_heads;
+    for (int e = a.first[j]; e < a.first[j + 1]; ++e) used[a.seq[e]] = (int16_t)ns;
+    most = ns > most ? (int)ns : most;
+  }
+  a.unit0[a.groups] = (int32_t)units;
+  a.units = units > INT32_MAX ? -1 : (int)units;
+  a.B = batch;
+  a.Hq = c->n_q_heads;
+  a.Hkv = c->n_kv_heads;
+  a.n = n;
+  a.bb = c->buffer_tokens;
+  a.npc = swan::pages_for(c->sparse_capacity);
+  a.k = c->k_pages;
+  a.v = c->v_pages;
+  a.k_ring = c->k_ring;
+  a.v_ring = c->v_ring;
+  a.dtype = c->dtype;
+  a.o0 = nullptr;
+  a.lse0 = nullptr;
+  a.out = nullptr;
+  a.qmult = 0.f;
+  a.m = a.causal = 0;
+  return most;
+}
+
+struct AttendPlan {
+  swan::AttendLaunch a[2];
+  int16_t used[2][SWAN_MAX_BATCH];
+  int base[2], slots;
+  size_t qhat, bytes;  // bytes of q_hat; of the workspace
+};
+
+swan_status attend_prep(const swan_prefix* sources, int32_t n_sources, int32_t batch, int32_t n,
+                        const int32_t* n_host, bool need_ptrs, AttendPlan& pl) {
+  if (!sources || n_sources < 1 || n_sources > 2)
+    return fail(SWAN_ERR_INVALID_ARG, "sources is NULL, or n_sources %d outside 1..2", n_sources);
+  if (batch < 1 || batch > SWAN_MAX_BATCH)
+    return fail(SWAN_ERR_INVALID_ARG, "batch %d outside 1..%d", batch, SWAN_MAX_BATCH);
+  swan_status st = check_rows("n", n_host, batch, n);
+  if (st != SWAN_OK) return st;
+  for (int s = 0; s < n_sources; ++s)
+    if ((st = check_source(&sources[s], batch, need_ptrs)) != SWAN_OK) return st;
+  const swan_cache* c = sources[0].cache;
+  if (n_sources == 2) {
+    const swan_cache* d = sources[1].cache;
+    if (c->n_q_heads != d->n_q_heads || c->n_kv_heads != d->n_kv_heads ||
+        elem_bytes(c->dtype) != elem_bytes(d->dtype))
+      return fail(SWAN_ERR_INVALID_ARG, "the sources differ in heads or element type");
+  }
+  if ((int64_t)batch * c->n_q_heads * n > INT32_MAX)
+    return fail(SWAN_ERR_UNSUPPORTED, "%d sequences x %d heads x %d rows: above 2^31 - 1", batch,
+                c->n_q_heads, n);
+  pl.slots = 0;
+  for (int s = 0; s < 2; ++s) {
+    pl.base[s] = pl.slots;
+    if (s < n_sources) {
+      pl.slots += plan_pages(&sources[s], batch, n, n_host, pl.a[s], pl.used[s]);
+      if (pl.a[s].units < 0) return fail(SWAN_ERR_UNSUPPORTED, "too many rows for one call");
+    } else {
+      pl.a[s].groups = 0;
+      for (int b = 0; b < SWAN_MAX_BATCH; ++b) pl.used[s][b] = 0;
+    }
+  }
+  const size_t rows = (size_t)batch * c->n_q_heads * n;
+  pl.qhat = round256(rows * swan::kD * sizeof(float));
+  pl.bytes = pl.qhat + rows * pl.slots * swan::kPartFloats * sizeof(float);
+  return SWAN_OK;
+}
+
+// plan of swan_prompt_attention
+struct PromptPlan {
+  swan::AttendLaunch a;
+  int16_t used[SWAN_MAX_BATCH];
+  size_t bytes;
+};
+
+swan_status prompt_prep(int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t n, int32_t m,
+                        int32_t head_dim, const int32_t* n_host, const int32_t* m_host,
+                        int32_t causal, PromptPlan& pl) {
+  if (batch < 1 || batch > SWAN_MAX_BATCH)
+    return fail(SWAN_ERR_INVALID_ARG, "batch %d outside 1..%d", batch, SWAN_MAX_BATCH);
+  if (n_kv_heads < 1 || n_q_heads < 1 || n_q_heads % n_kv_heads != 0)
+    return fail(SWAN_ERR_INVALID_ARG, "n_q_heads %d is not a multiple of n_kv_heads %d", n_q_heads,
+                n_kv_heads);
+  if (head_dim != SWAN_HEAD_DIM)
+    return fail(SWAN_ERR_UNSUPPORTED, "head_dim %d: the GPU path supports %d only", head_dim,
+                SWAN_HEAD_DIM);
+  swan_status st = check_rows("n", n_host, batch, n);
+  if (st != SWAN_OK) return st;
+  if ((st = check_rows("m", m_host, batch, m)) != SWAN_OK) return st;
+  if (causal != 0 && causal != 1) return fail(SWAN_ERR_INVALID_ARG, "causal %d", causal);
+  if ((int64_t)batch * n_q_heads * n > INT32_MAX)
+    return fail(SWAN_ERR_UNSUPPORTED, "%d sequences x %d heads x %d rows: above 2^31 - 1", batch,
+                n_q_heads, n);
+  swan::AttendLaunch& a = pl.a;
+  const int G = n_q_heads / n_kv_heads;
+  // sequences with the most keys first: the longest workgroups start first
+  int order[SWAN_MAX_BATCH], count = 0;
+  for (int b = 0; b < batch; ++b) {
+    pl.used[b] = 0;
+    if ((n_host ? n_host[b] : n) == 0) continue;
+    int at = count++;
+    const int keys = m_host ? m_host[b] : m;
+    while (at > 0 && (m_host ? m_host[order[at - 1]] : m) < keys) {
+      order[at] = order[at - 1];
+      --at;
+    }
+    order[at] = b;
+  }
+  int64_t base = 0;
+  for (int j = 0; j < count; ++j) {
+    const int b = order[j];
+    a.first[j] = (uint8_t)j;
+    a.seq[j] = a.cseq[j] = (uint8_t)b;
+    a.tok0[j] = 0;
+    a.toks[j] = n_host ? n_host[b] : n;
+    a.keys[j] = m_host ? m_host[b] : m;
+    base += ((int64_t)a.toks[j] * G + swan::kTileRows - 1) / swan::kTileRows * n_kv_heads;
+  }
+  a.first[count] = (uint8_t)count;
+  a.groups = count;
+  int64_t units = 0;
+  int most = 1;
+  for (int j = 0; j < count; ++j) {
+    const int64_t tiles = ((int64_t)a.toks[j] * G + swan::kTileRows - 1) / swan::kTileRows;
+    // few row tiles: the keys are split over more workgroups, four tiles of them at least
+    const int nt = (a.keys[j] + swan::kTileKeys - 1) / swan::kTileKeys;
+    int64_t ns = kUnits / base < nt / 4 ? kUnits / base : nt / 4;
+    ns = ns > swan::kMaxSlots ? swan::kMaxSlots : ns < 1 ? 1 : ns;
+    a.nsplit[j] = (int16_t)ns;
+    a.unit0[j] = (int32_t)units;
+    units += tiles * ns * n_kv_heads;
+    most = ns > most ? (int)ns : most;
+    pl.used[order[j]] = (int16_t)ns;
+    if (units > INT32_MAX) return fail(SWAN_ERR_UNSUPPORTED, "too many rows for one call");
+  }
+  a.unit0[count] = (int32_t)units;
+  a.units = (int)units;
+  a.B = batch;
+  a.Hq = n_q_heads;
+  a.Hkv = n_kv_heads;
+  a.n = n;
+  a.m = m;
+  a.causal = causal;
+  a.slots = most;
+  a.slot0 = 0;
+  a.k_ring = a.v_ring = nullptr;
+  a.bb = a.npc = 0;
+  pl.bytes = most == 1 ? 0
+                       : (size_t)batch * n_q_heads * n * most * swan::kPartFloats * sizeof(float);
+  return SWAN_OK;
+}
+
+// decode entry points with a prefix: the prefix's plan beside the own cache's
+swan_status prefix_prep(const swan_prefix* prefix, const swan_cache* c, bool need_ptrs,
+                        AttendPlan& pl) {
+  swan_status st = check_cache_shape(c);
+  if (st != SWAN_OK) return st;
+  if ((st = attend_prep(prefix, 1, c->batch, 1, nullptr, need_ptrs, pl)) != SWAN_OK) return st;
+  const swan_cache* p = prefix->cache;
+  if (p->n_q_heads != c->n_q_heads || p->n_kv_heads != c->n_kv_heads ||
+      elem_bytes(p->dtype) != elem_bytes(c->dtype))
+    return fail(SWAN_ERR_INVALID_ARG, "the prefix's cache differs in heads or element type");
+  return SWAN_OK;
+}
+
+size_t prefix_part_bytes(const swan_cache* c, const AttendPlan& pl) {
+  return (size_t)c->batch * c->n_q_heads * pl.slots * swan::kPartFloats * sizeof(float);
+}
+
+// the shortest own length that a decode call behind `prefix` takes: 0 where every
+// sequence has a prefix token
+swan_status check_some_token(const swan_prefix* prefix, const swan_cache* c,
+                             const int32_t* seq_len_host) {
+  if (!seq_len_host) return fail(SWAN_ERR_INVALID_ARG, "seq_len_host is NULL");
+  for (int b = 0; b < c->batch; ++b) {
+    const int p = prefix->of_host[b];
+    if (seq_len_host[b] < 1 && (p < 0 || prefix->seq_len_host[p] < 1))
+      return fail(SWAN_ERR_INVALID_ARG, "sequence %d has no token, of its own or of a prefix", b);
+  }
+  return SWAN_OK;
+}
+
+// after decode_prep of the own cache: attention over both, joined
+hipError_t launch_decode_prefix(swan::DecodeLaunch& da, AttendPlan& pl, void* workspace,
+                                size_t decode_bytes) {
+  da.leave_partials = 1;
+  hipError_t e = swan::launch_decode(da);
+  if (e != hipSuccess) return e;
+  swan::AttendLaunch& a = pl.a[0];
+  a.q = da.qhat;
+  a.part = (float*)((char*)workspace + round256(decode_bytes));
+  a.slots = pl.slots;
+  a.slot0 = 0;
+  a.stream = da.stream;
+  if (a.units > 0 && (e = swan::launch_attend_pages(a)) != hipSuccess) return e;
+  swan::JoinLaunch j;
+  j.part = a.part;
+  j.o0 = j.lse0 = nullptr;
+  j.P_vo = da.P_vo;
+  j.out = da.out;
+  j.o = j.lse = nullptr;
+  j.B = da.B;
+  j.H = da.Hq;
+  j.Hkv = da.Hkv;
+  j.n = 1;
+  j.slots = pl.slots;
+  j.dtype = da.dtype;
+  j.own_slots = da.n_splits;
+  j.own = da.part;
+  j.own_bb = da.bb;
+  j.own_tab = da.tab;
+  for (int b = 0; b < SWAN_MAX_BATCH; ++b) {
+    j.used[0][b] = b < da.B ? pl.used[0][b] : 0;
+    j.used[1][b] = 0;
+    j.rows[b] = 1;
+  }
+  j.base[0] = j.base[1] = 0;
+  j.stream = da.stream;
+  return swan::launch_join(j);
 }
 
 }  // namespace
@@ -564,23 +922,11 @@ swan_status swan_decode_step(const swan_cache* c, const int32_t* seq_len_host,
                              void* workspace, size_t workspace_bytes, void* stream) {
   // every check of both halves before anything is enqueued
   swan::CompressLaunch ca;
-  bool any_new = false;
-  swan_status st = compress_prep(c, seq_len_host, k_active_host, k_value_host, k_new, v_new, 1,
-                                 nullptr, P_qk, P_vo, stream, ca, any_new);
-  if (st != SWAN_OK) return st;
-  int32_t len1[SWAN_MAX_BATCH];
-  for (int b = 0; b < c->batch; ++b) len1[b] = seq_len_host[b] + 1;
   swan::DecodeLaunch da;
-  st = decode_prep(c, len1, k_active_host, k_value_host, q, P_qk, P_vo, scale, out, workspace,
-                   workspace_bytes, stream, false, da);
+  const swan_status st = step_prep(c, seq_len_host, k_active_host, k_value_host, k_new, v_new, q,
+                                   P_qk, P_vo, scale, out, workspace, workspace_bytes, stream, ca,
+                                   da);
   if (st != SWAN_OK) return st;
-  if (c->n_q_heads / c->n_kv_heads <= swan::kStepQG) {  // the key waves rotate the queries
-    ca.q = q;
-    ca.qhat = da.qhat;
-    ca.Hq = da.Hq;
-    ca.qmult = da.qmult;
-    da.qhat_ready = 1;
-  }
   const hipError_t e = swan::launch_compress(ca);
   if (e != hipSuccess) return hip_status(e, "compress launch");
   return hip_status(swan::launch_decode(da), "decode launch");
@@ -683,6 +1029,317 @@ swan_status swan_rope(const void* x, void* y, int32_t dtype, int32_t batch, int3
   a.base = base;
   a.stream = (hipStream_t)stream;
   return hip_status(swan::launch_rope(a), "rope launch");
+}
+
+swan_status swan_qkv_rows(const void* qkv, int64_t seq_stride, int64_t row_stride, int32_t dtype,
+                          int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t n,
+                          int32_t head_dim, const int32_t* pos0_host, double base,
+                          const void* q_weight, const void* k_weight, int32_t weights_per_head,
+                          int32_t weights_f32, double eps, void* q, void* k, void* v,
+                          void* stream) {
+  if (!dtype_ok(dtype)) return fail(SWAN_ERR_UNSUPPORTED, "dtype %d not supported", dtype);
+  if (head_dim != SWAN_HEAD_DIM)
+    return fail(SWAN_ERR_UNSUPPORTED, "head_dim %d: the GPU path supports %d only", head_dim,
+                SWAN_HEAD_DIM);
+  if (batch < 1 || batch > SWAN_MAX_BATCH || n < 0)
+    return fail(SWAN_ERR_INVALID_ARG, "batch %d, n %d", batch, n);
+  if (n_q_heads < 0 || n_kv_heads < 0 || n_q_heads + (int64_t)n_kv_heads < 1 ||
+      n_q_heads + 2 * (int64_t)n_kv_heads > 65535)
+    return fail(SWAN_ERR_INVALID_ARG, "n_q_heads %d, n_kv_heads %d", n_q_heads, n_kv_heads);
+  if ((int64_t)batch * n > INT32_MAX)
+    return fail(SWAN_ERR_INVALID_ARG, "batch %d x n %d: above 2^31 - 1 rows", batch, n);
+  if (!(base > 1.0) || isinf(base)) return fail(SWAN_ERR_INVALID_ARG, "base must be > 1");
+  if (!(eps >= 0.0) || isinf(eps)) return fail(SWAN_ERR_INVALID_ARG, "eps must be finite, >= 0");
+  if ((weights_per_head != 0 && weights_per_head != 1) || (weights_f32 != 0 && weights_f32 != 1))
+    return fail(SWAN_ERR_INVALID_ARG, "weights_per_head %d, weights_f32 %d: 0 or 1",
+                weights_per_head, weights_f32);
+  if (!pos0_host) return fail(SWAN_ERR_INVALID_ARG, "pos0_host is NULL");
+  if (n == 0) return ok();
+  const int64_t width = (n_q_heads + 2 * (int64_t)n_kv_heads) * SWAN_HEAD_DIM;
+  if (row_stride < width || row_stride % 8 != 0 || seq_stride < 0 || seq_stride % 8 != 0)
+    return fail(SWAN_ERR_INVALID_ARG,
+                "strides %lld (sequence) and %lld (row of %lld): multiples of 8, a row at least",
+                (long long)seq_stride, (long long)row_stride, (long long)width);
+  if (!qkv || (n_q_heads && !q) || (n_kv_heads && (!k || !v)))
+    return fail(SWAN_ERR_INVALID_ARG, "qkv / q / k / v is NULL");
+  const void* ptrs[6] = {qkv, q, k, v, q_weight, k_weight};
+  for (const void* p : ptrs)
+    if (((uintptr_t)p & 15) != 0)
+      return fail(SWAN_ERR_INVALID_ARG, "pointers must be 16-byte aligned");
+  swan::QkvRowsLaunch a;
+  a.x = qkv;
+  a.seq = seq_stride;
+  a.row = row_stride;
+  a.out[0] = q;
+  a.out[1] = k;
+  a.out[2] = v;
+  a.w[0] = q_weight;
+  a.w[1] = k_weight;
+  a.wstep = weights_per_head ? SWAN_HEAD_DIM : 0;
+  a.w32 = weights_f32;
+  a.B = batch;
+  a.Hq = n_q_heads;
+  a.Hkv = n_kv_heads;
+  a.n = n;
+  a.dtype = dtype;
+  a.eps = eps;
+  a.base = base;
+  for (int b = 0; b < SWAN_MAX_BATCH; ++b) {
+    if (b < batch && (pos0_host[b] < 0 || (int64_t)pos0_host[b] + n > INT32_MAX))
+      return fail(SWAN_ERR_INVALID_ARG, "pos0[%d] = %d out of range", b, pos0_host[b]);
+    a.pos0[b] = b < batch ? pos0_host[b] : 0;
+  }
+  // the outputs and the rows read share no byte
+  const int64_t es = elem_bytes(dtype), each = (int64_t)batch * n * SWAN_HEAD_DIM * es;
+  const char* lo[4] = {(const char*)qkv, (const char*)q, (const char*)k, (const char*)v};
+  const int64_t size[4] = {((batch - 1) * seq_stride + (n - 1) * row_stride + width) * es,
+                           each * n_q_heads, each * n_kv_heads, each * n_kv_heads};
+  for (int x = 0; x < 4; ++x)
+    for (int y = x + 1; y < 4; ++y)
+      if (size[x] && size[y] && lo[x] < lo[y] + size[y] && lo[y] < lo[x] + size[x])
+        return fail(SWAN_ERR_INVALID_ARG, "qkv, q, k and v overlap");
+  a.stream = (hipStream_t)stream;
+  return hip_status(swan::launch_qkv_rows(a), "qkv_rows launch");
+}
+
+swan_status swan_attend_workspace_bytes(const swan_prefix* sources, int32_t n_sources,
+                                        int32_t batch, int32_t n, const int32_t* n_host,
+                                        size_t* bytes) {
+  if (!bytes) return fail(SWAN_ERR_INVALID_ARG, "bytes is NULL");
+  AttendPlan pl;
+  const swan_status st = attend_prep(sources, n_sources, batch, n, n_host, false, pl);
+  if (st != SWAN_OK) return st;
+  *bytes = pl.bytes;
+  return ok();
+}
+
+swan_status swan_attend(const swan_prefix* sources, int32_t n_sources, int32_t batch, int32_t n,
+                        const int32_t* n_host, const void* q, const float* P_qk,
+                        const float* P_vo, float scale, float* o, float* lse, void* workspace,
+                        size_t workspace_bytes, void* stream) {
+  AttendPlan pl;
+  swan_status st = attend_prep(sources, n_sources, batch, n, n_host, true, pl);
+  if (st != SWAN_OK) return st;
+  if ((st = check_scale(scale)) != SWAN_OK) return st;
+  int32_t rows[SWAN_MAX_BATCH] = {};
+  bool any = false;
+  for (int b = 0; b < batch; ++b) {
+    rows[b] = n_host ? n_host[b] : n;
+    any |= rows[b] > 0;
+  }
+  if (!any) return ok();
+  if (!q || !P_qk || !o || !lse) return fail(SWAN_ERR_INVALID_ARG, "q / P_qk / o / lse is NULL");
+  if ((((uintptr_t)q | (uintptr_t)P_qk | (uintptr_t)P_vo | (uintptr_t)o) & 15) != 0)
+    return fail(SWAN_ERR_INVALID_ARG, "q / P_qk / P_vo / o must be 16-byte aligned");
+  if (!workspace || workspace_bytes < pl.bytes)
+    return fail(SWAN_ERR_WORKSPACE, "workspace of %zu bytes, need %zu", workspace_bytes, pl.bytes);
+  if (((uintptr_t)workspace & 255) != 0)
+    return fail(SWAN_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+  const swan_cache* c = sources[0].cache;
+  float* qhat = (float*)workspace;
+  float* part = (float*)((char*)workspace + pl.qhat);
+  swan::RotateLaunch r;
+  r.x = q;
+  r.P = P_qk;
+  r.y = qhat;
+  r.mult = scale_or_default(scale) * 1.4426950408889634f;
+  r.x_dtype = c->dtype == SWAN_F32 ? SWAN_F32 : SWAN_F16;
+  r.transposed = 0;
+  r.B = batch;
+  r.H = c->n_q_heads;
+  r.Hkv = c->n_kv_heads;
+  r.n = n;
+  for (int b = 0; b < SWAN_MAX_BATCH; ++b) r.rows[b] = b < batch ? rows[b] : 0;
+  r.stream = (hipStream_t)stream;
+  hipError_t e = swan::launch_rotate_rows(r);
+  if (e != hipSuccess) return hip_status(e, "rotate launch");
+  for (int s = 0; s < n_sources; ++s) {
+    swan::AttendLaunch& a = pl.a[s];
+    if (a.units == 0) continue;
+    a.q = qhat;
+    a.part = part;
+    a.slots = pl.slots;
+    a.slot0 = pl.base[s];
+    a.stream = (hipStream_t)stream;
+    if ((e = swan::launch_attend_pages(a)) != hipSuccess) return hip_status(e, "attend launch");
+  }
+  swan::JoinLaunch j;
+  j.part = part;
+  j.o0 = j.lse0 = nullptr;
+  j.P_vo = nullptr;
+  j.out = nullptr;
+  j.o = P_vo ? qhat : o;  // q_hat's place is free by now
+  j.lse = lse;
+  j.B = batch;
+  j.H = c->n_q_heads;
+  j.Hkv = c->n_kv_heads;
+  j.n = n;
+  j.slots = pl.slots;
+  j.dtype = c->dtype;
+  j.own_slots = 0;
+  j.own = nullptr;
+  j.own_bb = 0;
+  for (int b = 0; b < SWAN_MAX_BATCH; ++b) {
+    for (int s = 0; s < 2; ++s) j.used[s][b] = b < batch ? pl.used[s][b] : 0;
+    j.rows[b] = b < batch ? rows[b] : 0;
+  }
+  j.base[0] = pl.base[0];
+  j.base[1] = pl.base[1];
+  j.stream = (hipStream_t)stream;
+  if ((e = swan::launch_join(j)) != hipSuccess) return hip_status(e, "join launch");
+  if (!P_vo) return ok();
+  r.x = qhat;
+  r.P = P_vo;
+  r.y = o;
+  r.mult = 1.f;
+  r.x_dtype = SWAN_F32;
+  r.transposed = 1;
+  return hip_status(swan::launch_rotate_rows(r), "rotate launch");
+}
+
+swan_status swan_prompt_workspace_bytes(int32_t batch, int32_t n_q_heads, int32_t n_kv_heads,
+                                        int32_t n, int32_t m, int32_t head_dim,
+                                        const int32_t* n_host, const int32_t* m_host,
+                                        int32_t causal, size_t* bytes) {
+  if (!bytes) return fail(SWAN_ERR_INVALID_ARG, "bytes is NULL");
+  PromptPlan pl;
+  const swan_status st = prompt_prep(batch, n_q_heads, n_kv_heads, n, m, head_dim, n_host, m_host,
+                                     causal, pl);
+  if (st != SWAN_OK) return st;
+  *bytes = pl.bytes;
+  return ok();
+}
+
+swan_status swan_prompt_attention(const void* q, const void* k, const void* v, int32_t dtype,
+                                  int32_t batch, int32_t n_q_heads, int32_t n_kv_heads,
+                                  int32_t n, int32_t m, int32_t head_dim, const int32_t* n_host,
+                                  const int32_t* m_host, int32_t causal, float scale,
+                                  const float* o0, const float* lse0, void* out,
+                                  void* workspace, size_t workspace_bytes, void* stream) {
+  if (!dtype_ok(dtype)) return fail(SWAN_ERR_UNSUPPORTED, "dtype %d not supported", dtype);
+  PromptPlan pl;
+  swan_status st = prompt_prep(batch, n_q_heads, n_kv_heads, n, m, head_dim, n_host, m_host,
+                               causal, pl);
+  if (st != SWAN_OK) return st;
+  if ((st = check_scale(scale)) != SWAN_OK) return st;
+  if ((o0 == nullptr) != (lse0 == nullptr))
+    return fail(SWAN_ERR_INVALID_ARG, "pass both parts of the state or neither");
+  if (pl.a.groups == 0) return ok();
+  bool any_key = false;
+  for (int j = 0; j < pl.a.groups; ++j) any_key |= pl.a.keys[j] > 0;
+  if (!q || !out || (any_key && (!k || !v)))
+    return fail(SWAN_ERR_INVALID_ARG, "q / k / v / out is NULL");
+  const void* ptrs[5] = {q, k, v, o0, out};
+  for (const void* p : ptrs)
+    if (((uintptr_t)p & 15) != 0)
+      return fail(SWAN_ERR_INVALID_ARG, "q / k / v / o0 / out must be 16-byte aligned");
+  if (pl.bytes > 0) {
+    if (!workspace || workspace_bytes < pl.bytes)
+      return fail(SWAN_ERR_WORKSPACE, "workspace of %zu bytes, need %zu", workspace_bytes,
+                  pl.bytes);
+    if (((uintptr_t)workspace & 255) != 0)
+      return fail(SWAN_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+  }
+  swan::AttendLaunch& a = pl.a;
+  a.q = q;
+  a.o0 = o0;
+  a.lse0 = lse0;
+  a.out = out;
+  a.part = pl.bytes > 0 ? (float*)workspace : nullptr;
+  a.k = k;
+  a.v = v;
+  a.qmult = scale_or_default(scale) * 1.4426950408889634f;
+  a.dtype = dtype == SWAN_F32 ? SWAN_F32 : SWAN_F16;
+  a.stream = (hipStream_t)stream;
+  hipError_t e = swan::launch_attend_dense(a);
+  if (e != hipSuccess || !a.part) return hip_status(e, "prompt attention launch");
+  swan::JoinLaunch j;
+  j.part = a.part;
+  j.o0 = o0;
+  j.lse0 = lse0;
+  j.P_vo = nullptr;
+  j.out = out;
+  j.o = j.lse = nullptr;
+  j.B = batch;
+  j.H = n_q_heads;
+  j.Hkv = n_kv_heads;
+  j.n = n;
+  j.slots = a.slots;
+  j.dtype = a.dtype;
+  j.own_slots = 0;
+  j.own = nullptr;
+  j.own_bb = 0;
+  for (int b = 0; b < SWAN_MAX_BATCH; ++b) {
+    j.used[0][b] = b < batch ? pl.used[b] : 0;
+    j.used[1][b] = 0;
+    j.rows[b] = b < batch ? (n_host ? n_host[b] : n) : 0;
+  }
+  j.base[0] = j.base[1] = 0;
+  j.stream = a.stream;
+  return hip_status(swan::launch_join(j), "join launch");
+}
+
+swan_status swan_prefix_workspace_bytes(const swan_prefix* prefix, const swan_cache* c,
+                                        const int32_t* seq_len_host,
+                                        const int32_t* k_active_host,
+                                        const int32_t* k_value_host, size_t* bytes) {
+  size_t own = 0;
+  swan_status st = swan_decode_workspace_bytes(c, seq_len_host, k_active_host, k_value_host, &own);
+  if (st != SWAN_OK) return st;
+  if (!bytes) return fail(SWAN_ERR_INVALID_ARG, "bytes is NULL");
+  AttendPlan pl;
+  if ((st = prefix_prep(prefix, c, false, pl)) != SWAN_OK) return st;
+  *bytes = round256(own) + prefix_part_bytes(c, pl);
+  return ok();
+}
+
+swan_status swan_decode_attention_prefix(const swan_prefix* prefix, const swan_cache* c,
+                                         const int32_t* seq_len_host,
+                                         const int32_t* k_active_host,
+                                         const int32_t* k_value_host, const void* q,
+                                         const float* P_qk, const float* P_vo, float scale,
+                                         void* out, void* workspace, size_t workspace_bytes,
+                                         void* stream) {
+  AttendPlan pl;
+  swan_status st = prefix_prep(prefix, c, true, pl);
+  if (st != SWAN_OK) return st;
+  if ((st = check_some_token(prefix, c, seq_len_host)) != SWAN_OK) return st;
+  swan::DecodeLaunch da;
+  st = decode_prep(c, seq_len_host, k_active_host, k_value_host, q, P_qk, P_vo, scale, out,
+                   workspace, workspace_bytes, stream, false, da, 0);
+  if (st != SWAN_OK) return st;
+  const size_t own = decode_ws_bytes(c, da.n_splits);
+  const size_t need = round256(own) + prefix_part_bytes(c, pl);
+  if (workspace_bytes < need)
+    return fail(SWAN_ERR_WORKSPACE, "workspace of %zu bytes, need %zu", workspace_bytes, need);
+  return hip_status(launch_decode_prefix(da, pl, workspace, own), "decode launch");
+}
+
+swan_status swan_decode_step_prefix(const swan_prefix* prefix, const swan_cache* c,
+                                    const int32_t* seq_len_host, const int32_t* k_active_host,
+                                    const int32_t* k_value_host, const void* k_new,
+                                    const void* v_new, const void* q, const float* P_qk,
+                                    const float* P_vo, float scale, void* out, void* workspace,
+                                    size_t workspace_bytes, void* stream) {
+  // every check of all parts before anything is enqueued
+  AttendPlan pl;
+  swan_status st = prefix_prep(prefix, c, true, pl);
+  if (st != SWAN_OK) return st;
+  if ((c->k_pages && c->k_pages == prefix->cache->k_pages) ||
+      (c->k_ring && c->k_ring == prefix->cache->k_ring))
+    return fail(SWAN_ERR_INVALID_ARG, "the prefix's cache is the one appended to");
+  swan::CompressLaunch ca;
+  swan::DecodeLaunch da;
+  if ((st = step_prep(c, seq_len_host, k_active_host, k_value_host, k_new, v_new, q, P_qk, P_vo,
+                      scale, out, workspace, workspace_bytes, stream, ca, da)) != SWAN_OK)
+    return st;
+  const size_t own = decode_ws_bytes(c, da.n_splits);
+  const size_t need = round256(own) + prefix_part_bytes(c, pl);
+  if (workspace_bytes < need)
+    return fail(SWAN_ERR_WORKSPACE, "workspace of %zu bytes, need %zu", workspace_bytes, need);
+  const hipError_t e = swan::launch_compress(ca);
+  if (e != hipSuccess) return hip_status(e, "compress launch");
+  return hip_status(launch_decode_prefix(da, pl, workspace, own), "decode launch");
 }
 
 swan_status swan_set_decode_tuning(const swan_decode_tuning* t) {

@@ -72,6 +72,7 @@ struct DecodeLaunch {
   int merge_pct;          // launch grouping of a mixed-k batch (<= 0: none)
   int side_streams;       // library streams for those launches, 0..kSideStreams
   int qhat_ready = 0;     // 1: qhat already holds the rotated queries (decode steps)
+  int leave_partials = 0; // 1: no merge, the caller joins the partials with others
 };
 hipError_t launch_decode(const DecodeLaunch& a);
 constexpr int kSideStreams = 3;  // extra streams for the launches of a mixed-k batch

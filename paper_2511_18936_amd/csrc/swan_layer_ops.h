@@ -1,0 +1,107 @@
+// Launchers of what a layer runs around its cache: the rows of its projections, and the
+// attention of several rows per sequence (over cached tokens, over a prompt).
+#pragma once
+
+#include "swan_device.h"
+#include "swan_internal.h"
+#include "swan_layer.h"
+
+namespace swan {
+
+// [q | k | v] projections to heads (qkv_rows.hip)
+struct QkvRowsLaunch {
+  const void* x;        // rows of Hq q, Hkv k and Hkv v heads, 128 elements each
+  int64_t seq, row;     // elements from a sequence (a row) to the next
+  void* out[3];         // q, k, v: [B][heads][n][128]
+  const void* w[2];     // norm weights of q and k (NULL: no norm)
+  int wstep;            // elements from a head's weights to the next's (0: shared)
+  int w32;              // the weights are float32 (else the rows' type)
+  int B, Hq, Hkv, n, dtype;
+  double eps, base;
+  int32_t pos0[SWAN_MAX_BATCH];
+  hipStream_t stream;
+};
+hipError_t launch_qkv_rows(const QkvRowsLaunch& a);
+
+// ---------------------------------------------------------------------------
+// attention of several rows per sequence (attend.h): rows of q over one of
+//   pages  the pruned pages and the ring of a sequence of a cache (attend_pages.hip)
+//   dense  keys and values [B][Hkv][m][128], causal or not (attend_dense.hip)
+// Query rows go by group: a group's sequences attend to the same keys of a kv head, so
+// all their tokens and all G query heads of it are rows of the same tiles; row
+// tok * G + g of a (group, kv head) is head g of token tok, the tokens of the group's
+// sequences one sequence after another.
+// ---------------------------------------------------------------------------
+constexpr int kTileRows = 128;   // query rows of a workgroup, 32 per wave
+constexpr int kTileKeys = 64;    // keys of a tile (a page)
+constexpr int kMaxSlots = 256;   // splits of the keys of a group, per source
+
+struct AttendLaunch {
+  const void* q;       // dense: rows of the storage type; pages: float32, rotated, x qmult
+  const float* o0;     // dense: the state to continue from (or NULL), as o / lse below
+  const float* lse0;
+  void* out;           // dense, one split: [B][Hq][n][128] of the storage type
+  float* part;         // partials [B Hq n][slots][kPartFloats]; NULL: write `out`
+  const void* k;       // dense: keys; pages: the keys' pages
+  const void* v;
+  const void* k_ring;  // pages
+  const void* v_ring;
+  float qmult;         // dense: scale log2(e)
+  int B, Hq, Hkv, n;   // n: rows of q per sequence (its token stride)
+  int m, causal;       // dense: rows of k and v per sequence
+  int bb, npc;         // pages: buffer tokens; page capacity of a (sequence, head)
+  int slots, slot0;    // partials of a row, and the first of this source
+  int dtype, groups;
+  int units;           // kv heads x row tiles x splits of all groups
+  int32_t unit0[SWAN_MAX_BATCH + 1];  // first unit of a group
+  int32_t tok0[SWAN_MAX_BATCH + 1];   // first token of a list entry, from its group's first
+  int32_t keys[SWAN_MAX_BATCH];       // keys of a group
+  int32_t toks[SWAN_MAX_BATCH];       // tokens of a group
+  int64_t off[2][SWAN_MAX_BATCH];     // pages: byte offset of the group's key / value pages
+  int16_t nsplit[SWAN_MAX_BATCH];     // splits of a group's keys
+  uint8_t first[SWAN_MAX_BATCH + 1];  // first list entry of a group
+  uint8_t seq[SWAN_MAX_BATCH];        // sequence of a list entry
+  uint8_t cseq[SWAN_MAX_BATCH];       // pages: cache sequence of a group; dense: its sequence
+  uint8_t kact[2][SWAN_MAX_BATCH];    // pages: k of the group's keys / values
+  hipStream_t stream;
+};
+hipError_t launch_attend_pages(const AttendLaunch& a);
+hipError_t launch_attend_dense(const AttendLaunch& a);
+
+// y = x . M of float32 or storage-type rows [B][H][n][128], M = P of the head's kv head
+// (H / Hkv heads share it) or its transpose, times mult; float32 rows out
+struct RotateLaunch {
+  const void* x;
+  const float* P;
+  float* y;
+  float mult;
+  int x_dtype;     // SWAN_F32 or SWAN_F16
+  int transposed;
+  int B, H, Hkv, n;
+  int32_t rows[SWAN_MAX_BATCH];
+  hipStream_t stream;
+};
+hipError_t launch_rotate_rows(const RotateLaunch& a);
+
+// the partials of up to two sources (and a state) of a row to one result
+struct JoinLaunch {
+  const float* part;   // [B H n][slots][kPartFloats]
+  const float* o0;     // a state to continue from, or NULL
+  const float* lse0;
+  const float* P_vo;   // decode: rotates the result back, or NULL
+  void* out;           // storage type, or NULL
+  float* o;            // float32 state, or NULL (unless `out`)
+  float* lse;
+  int B, H, Hkv, n, slots, dtype;
+  int own_slots;       // decode: the partials of swan_decode_attention, own_slots + 1 per row
+  const float* own;
+  int own_bb;
+  SeqTab own_tab;
+  int16_t used[2][SWAN_MAX_BATCH];  // partials of a sequence from slot base[s] on
+  int base[2];
+  int32_t rows[SWAN_MAX_BATCH];
+  hipStream_t stream;
+};
+hipError_t launch_join(const JoinLaunch& a);
+
+}  // namespace swan

@@ -71,6 +71,17 @@ class CacheDesc(ctypes.Structure):
     ]
 
 
+class PrefixDesc(ctypes.Structure):
+    """swan_prefix: a cache, its lengths and k, and the sequence of it per query sequence."""
+    _fields_ = [
+        ("cache", ctypes.POINTER(CacheDesc)),
+        ("seq_len_host", ctypes.POINTER(ctypes.c_int32)),
+        ("k_active_host", ctypes.POINTER(ctypes.c_int32)),
+        ("k_value_host", ctypes.POINTER(ctypes.c_int32)),
+        ("of_host", ctypes.POINTER(ctypes.c_int32)),
+    ]
+
+
 def _load() -> ctypes.CDLL:
     # torch first: its HIP runtime (soname libamdhip64.so.7) then also serves
     # libswan, so the process holds a single runtime and a single device context
@@ -83,6 +94,7 @@ def _load() -> ctypes.CDLL:
     lib = ctypes.CDLL(LIB_PATH)
     i32, i64, sz, vp = ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.c_void_p
     pi32, psz, pdesc = ctypes.POINTER(i32), ctypes.POINTER(sz), ctypes.POINTER(CacheDesc)
+    pprefix = ctypes.POINTER(PrefixDesc)
     lib.swan_last_error.restype = ctypes.c_char_p
     lib.swan_last_error.argtypes = []
     lib.swan_version.restype = i32
@@ -103,6 +115,19 @@ def _load() -> ctypes.CDLL:
                              sz, vp],
         "swan_change_k": [pdesc, pi32, pi32, pdesc, pi32, pi32, pi32, vp],
         "swan_rope": [vp, vp, i32, i32, i32, i32, i32, pi32, ctypes.c_double, vp],
+        "swan_qkv_rows": [vp, i64, i64, i32, i32, i32, i32, i32, i32, pi32, ctypes.c_double, vp,
+                          vp, i32, i32, ctypes.c_double, vp, vp, vp, vp],
+        "swan_attend_workspace_bytes": [pprefix, i32, i32, i32, pi32, psz],
+        "swan_attend": [pprefix, i32, i32, i32, pi32, vp, vp, vp, ctypes.c_float, vp, vp, vp, sz,
+                        vp],
+        "swan_prompt_workspace_bytes": [i32, i32, i32, i32, i32, i32, pi32, pi32, i32, psz],
+        "swan_prompt_attention": [vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, pi32, pi32, i32,
+                                  ctypes.c_float, vp, vp, vp, vp, sz, vp],
+        "swan_prefix_workspace_bytes": [pprefix, pdesc, pi32, pi32, pi32, psz],
+        "swan_decode_attention_prefix": [pprefix, pdesc, pi32, pi32, pi32, vp, vp, vp,
+                                         ctypes.c_float, vp, vp, sz, vp],
+        "swan_decode_step_prefix": [pprefix, pdesc, pi32, pi32, pi32, vp, vp, vp, vp, vp,
+                                    ctypes.c_float, vp, vp, sz, vp],
         "swan_set_decode_tuning": [ctypes.POINTER(DecodeTuning)],
         "swan_set_profile_events": [vp, vp],
     }
@@ -375,6 +400,280 @@ def rope(x, pos0: Sequence[int], base: float, out=None, stream=None):
     return out
 
 
+def _same_gpu(**tensors):
+    """The one GPU that all the tensors (None left out) are on."""
+    _on_gpu(**tensors)
+    device = None
+    for name, t in tensors.items():
+        if t is None:
+            continue
+        device = t.device if device is None else device
+        if t.device != device:
+            raise SwanError(SWAN_ERR_INVALID_ARG, f"{name} is on {t.device}, not on {device}")
+    return device
+
+
+def _calls_on(device):
+    """Makes `device` current where it is not: a call is enqueued on a stream of the
+    current device."""
+    import contextlib
+
+    import torch
+
+    if device.index is None or device.index == torch.cuda.current_device():
+        return contextlib.nullcontext()
+    return torch.cuda.device(device)
+
+
+def _per_sequence(values: Optional[Sequence[int]], batch: int, name: str):
+    if values is not None and len(values) != batch:
+        raise SwanError(SWAN_ERR_INVALID_ARG,
+                        f"{name} has {len(values)} entries for {batch} sequences")
+    return _opt_i32_array(values)
+
+
+def _storage_code(dtype) -> int:
+    import torch
+
+    if dtype not in (torch.float16, torch.float32):
+        raise SwanError(SWAN_ERR_UNSUPPORTED, f"dtype {dtype} not supported")
+    return SWAN_F16 if dtype == torch.float16 else SWAN_F32
+
+
+def _workspace(workspace, need: int, device, stream):
+    """`workspace`, or `need` bytes of the caching allocator for work on `stream`."""
+    if workspace is not None:
+        if not workspace.is_cuda or not workspace.is_contiguous():
+            raise SwanError(SWAN_ERR_WORKSPACE, "workspace must be a contiguous GPU tensor")
+        if workspace.device != device:
+            raise SwanError(SWAN_ERR_WORKSPACE,
+                            f"workspace is on {workspace.device}, not on {device}")
+        return workspace
+    return _made("empty", (max(need, 16),), "uint8", device, stream)
+
+
+def _made(how: str, shape, dtype, device, stream):
+    """torch.empty or torch.zeros, on the stream that the call is enqueued on (memory of
+    another stream's could still be in use there)."""
+    import torch
+
+    dtype = getattr(torch, dtype) if isinstance(dtype, str) else dtype
+    with torch.cuda.stream(stream):  # (None: the current one)
+        return getattr(torch, how)(shape, dtype=dtype, device=device)
+
+
+def qkv_rows(qkv, n_q_heads: int, n_kv_heads: int, pos0: Sequence[int], base: float,
+             q_weight=None, k_weight=None, eps: float = 1e-6, out=None, stream=None):
+    """A layer's projections qkv [B][n][(n_q + 2 n_kv) * 128] (float16 or float32, cuda; rows
+    may be strided) as q [B][n_q][n][128], k and v [B][n_kv][n][128]: q and k divided by
+    their root mean square and weighted (q_weight / k_weight: [128], or [heads][128], of
+    qkv's type or float32; None: no norm), then rotated to positions pos0[b] + i as by
+    rope(); v as it is.  out = (q, k, v) writes existing tensors; n_q_heads = 0 gives
+    (None, k, v)."""
+    import torch
+
+    if qkv.dim() != 3:
+        raise SwanError(SWAN_ERR_INVALID_ARG, "qkv must be [B][n][(n_q + 2 n_kv) * 128]")
+    code = _storage_code(qkv.dtype)
+    B, n, width = qkv.shape
+    if width != (n_q_heads + 2 * n_kv_heads) * HEAD_DIM or n_q_heads < 0 or n_kv_heads < 0:
+        raise SwanError(SWAN_ERR_INVALID_ARG,
+                        f"rows of {width} elements for {n_q_heads} + 2 x {n_kv_heads} heads")
+    if qkv.stride(2) != 1 and width > 1:
+        raise SwanError(SWAN_ERR_INVALID_ARG, "qkv's last dimension must be contiguous")
+    w32 = per_head = None
+    for name, w, heads in (("q_weight", q_weight, n_q_heads), ("k_weight", k_weight, n_kv_heads)):
+        if w is None:
+            continue
+        if w.dtype not in (qkv.dtype, torch.float32):
+            raise SwanError(SWAN_ERR_INVALID_ARG,
+                            f"{name} has dtype {w.dtype}, expected {qkv.dtype} or float32")
+        _tensor(w, name, w.dtype, (HEAD_DIM,) if w.dim() == 1 else (heads, HEAD_DIM))
+        form = (w.dtype == torch.float32, w.dim() == 2)
+        if w32 is not None and form != (w32, per_head):
+            raise SwanError(SWAN_ERR_INVALID_ARG, "q_weight and k_weight differ in form")
+        w32, per_head = form
+    shapes = [(B, h, n, HEAD_DIM) for h in (n_q_heads, n_kv_heads, n_kv_heads)]
+    if out is None:
+        _same_gpu(qkv=qkv)
+        out = [_made("empty", s, qkv.dtype, qkv.device, stream) if s[1] else None
+               for s in shapes]
+    else:
+        for name, t, s in zip("qkv", out, shapes):
+            if s[1]:
+                _tensor(t, name, qkv.dtype, s)
+    q, k, v = out
+    device = _same_gpu(qkv=qkv, q=q, k=k, v=v, q_weight=q_weight, k_weight=k_weight)
+    # a dimension of one element has no stride of its own
+    row = qkv.stride(1) if n > 1 else width
+    seq = qkv.stride(0) if B > 1 else 0
+    with _calls_on(device):
+        _check(_lib.swan_qkv_rows(_ptr(qkv), seq, row, code, B, n_q_heads, n_kv_heads, n, HEAD_DIM,
+                                  _per_sequence(pos0, B, "pos0"), float(base), _ptr(q_weight),
+                                  _ptr(k_weight), int(bool(per_head)), int(bool(w32)), float(eps),
+                                  _ptr(q), _ptr(k), _ptr(v), _stream(stream, device.index)))
+    return q, k, v
+
+
+def prompt_attention(q, k, v, causal: bool = True, n: Optional[Sequence[int]] = None,
+                     m: Optional[Sequence[int]] = None, scale: float = 0.0, state=None, out=None,
+                     workspace=None, stream=None):
+    """Dense attention of rows q [B][H_q][n][128] over k, v [B][H_kv][m][128] (float16 or
+    float32, cuda): a prompt's (causal: row i sees keys j <= i + m_b - n_b) or rows over
+    another sequence's keys and values (causal=False).  n / m: the rows used of each
+    sequence (None: all); the others are not read, and out's rows past n_b not written
+    (zeros where out is None).  state: what SwanCache.attend or attend returned for these
+    rows, to continue from."""
+    if q.dim() != 4 or k.dim() != 4:
+        raise SwanError(SWAN_ERR_INVALID_ARG, "q, k and v must be [B][heads][rows][128]")
+    code = _storage_code(q.dtype)
+    B, hq, nq, d = q.shape
+    hkv, nk = int(k.shape[1]), int(k.shape[2])
+    _tensor(q, "q", q.dtype, (B, hq, nq, HEAD_DIM))
+    _tensor(k, "k", q.dtype, (B, hkv, nk, HEAD_DIM))
+    _tensor(v, "v", q.dtype, (B, hkv, nk, HEAD_DIM))
+    o0, lse0 = _state(state, B, hq, nq)
+    if out is None:
+        _same_gpu(q=q)
+        out = _made("empty" if n is None else "zeros", q.shape, q.dtype, q.device, stream)
+    _tensor(out, "out", q.dtype, (B, hq, nq, HEAD_DIM))
+    device = _same_gpu(q=q, k=k, v=v, out=out, o=o0, lse=lse0)
+    ns, ms = _per_sequence(n, B, "n"), _per_sequence(m, B, "m")
+    need = ctypes.c_size_t()
+    _check(_lib.swan_prompt_workspace_bytes(B, hq, hkv, nq, nk, d, ns, ms, int(causal),
+                                            ctypes.byref(need)))
+    ws = None
+    if need.value:
+        ws = _workspace(workspace, need.value, device, stream)
+    with _calls_on(device):
+        _check(_lib.swan_prompt_attention(
+            _ptr(q), _ptr(k), _ptr(v), code, B, hq, hkv, nq, nk, d, ns, ms, int(causal),
+            float(scale), _ptr(o0), _ptr(lse0), _ptr(out), _ptr(ws),
+            0 if ws is None else ws.numel() * ws.element_size(), _stream(stream, device.index)))
+    return out
+
+
+def _state(state, B: int, heads: int, n: int):
+    import torch
+
+    if state is None:
+        return None, None
+    o, lse = state
+    _tensor(o, "state o", torch.float32, (B, heads, n, HEAD_DIM))
+    _tensor(lse, "state lse", torch.float32, (B, heads, n))
+    return o, lse
+
+
+class Prefix:
+    """Cached tokens that the sequences of a batch share: query sequence b attends to the
+    tokens of sequence of[b] of `cache` (-1: none; of=None: sequence 0, for all) before its
+    own.  It only refers to the cache: tokens appended to that later belong to the prefix."""
+
+    def __init__(self, cache: "SwanCache", of: Optional[Sequence[int]] = None):
+        self.cache = cache
+        self.of = None if of is None else [int(x) for x in of]
+
+    def _desc(self, batch: int):
+        c = self.cache
+        of = [0] * batch if self.of is None else self.of
+        if len(of) != batch:
+            raise SwanError(SWAN_ERR_INVALID_ARG,
+                            f"the prefix is for {len(of)} sequences, not {batch}")
+        return PrefixDesc(ctypes.pointer(c.desc), _i32_array(c.seq_len), _i32_array(c.k_active),
+                          _opt_i32_array(c.k_value), _i32_array(of))
+
+
+def attend(sources, q, P_qk, P_vo, n: Optional[Sequence[int]] = None, scale: float = 0.0,
+           out=None, workspace=None, stream=None):
+    """Rows q [B][H_q][n][128] over all cached tokens of one or two sources (Prefix objects:
+    a shared prefix, the sequences' own caches), none masked: the state (o [B][H_q][n][128],
+    lse [B][H_q][n]) in float32 that prompt_attention continues from.  n: the rows used of
+    each sequence (None: all); the others are not read, and not written (zeros where out
+    is None).  P_vo None leaves o rotated."""
+    sources = list(sources)
+    if not sources:
+        raise SwanError(SWAN_ERR_INVALID_ARG, "no sources")
+    c = sources[0].cache
+    if q.dim() != 4:
+        raise SwanError(SWAN_ERR_INVALID_ARG, "q must be [B][H_q][n][128]")
+    B, nq = int(q.shape[0]), int(q.shape[2])
+    hq = c.desc.n_q_heads
+    _tensor(q, "q", _elem_torch_dtype(c.desc.dtype), (B, hq, nq, HEAD_DIM))
+    _rotations(c.desc, P_qk, P_vo)
+    if out is None:
+        _same_gpu(q=q)
+        how = "empty" if n is None else "zeros"
+        out = (_made(how, (B, hq, nq, HEAD_DIM), "float32", q.device, stream),
+               _made(how, (B, hq, nq), "float32", q.device, stream))
+    o, lse = _state(out, B, hq, nq)
+    pages = {f"source {i}": s.cache.k_pages for i, s in enumerate(sources)}
+    device = _same_gpu(q=q, P_qk=P_qk, P_vo=P_vo, o=o, lse=lse, **pages)
+    descs = (PrefixDesc * len(sources))(*[s._desc(B) for s in sources])
+    ns = _per_sequence(n, B, "n")
+    need = ctypes.c_size_t()
+    _check(_lib.swan_attend_workspace_bytes(descs, len(sources), B, nq, ns, ctypes.byref(need)))
+    ws = _workspace(workspace, need.value, device, stream)
+    with _calls_on(device):
+        _check(_lib.swan_attend(descs, len(sources), B, nq, ns, _ptr(q), _ptr(P_qk), _ptr(P_vo),
+                                float(scale), _ptr(o), _ptr(lse), _ptr(ws),
+                                ws.numel() * ws.element_size(), _stream(stream, device.index)))
+    return o, lse
+
+
+def decode_attention_prefix(prefix: Prefix, desc: CacheDesc, seq_len: Sequence[int],
+                            k_active: Sequence[int], q, P_qk, P_vo, out, workspace,
+                            scale: float = 0.0, stream=None,
+                            k_value: Optional[Sequence[int]] = None) -> None:
+    """swan_decode_attention_prefix: decode_attention with a prefix before each sequence's
+    own tokens."""
+    _decode_tensors(desc, q, P_qk, P_vo, out)
+    device = _same_gpu(q=q, out=out, P_qk=P_qk, P_vo=P_vo, workspace=workspace,
+                       prefix=prefix.cache.k_pages)
+    if workspace is None or not workspace.is_contiguous():
+        raise SwanError(SWAN_ERR_WORKSPACE, "workspace must be a contiguous GPU tensor")
+    p = prefix._desc(desc.batch)
+    with _calls_on(device):
+        _check(_lib.swan_decode_attention_prefix(
+            ctypes.byref(p), ctypes.byref(desc), _i32_array(seq_len), _i32_array(k_active),
+            _opt_i32_array(k_value), _ptr(q), _ptr(P_qk), _ptr(P_vo), float(scale), _ptr(out),
+            _ptr(workspace), workspace.numel() * workspace.element_size(),
+            _stream(stream, device.index)))
+
+
+def decode_step_prefix(prefix: Prefix, desc: CacheDesc, seq_len: Sequence[int],
+                       k_active: Sequence[int], k_new, v_new, q, P_qk, P_vo, out, workspace,
+                       scale: float = 0.0, stream=None,
+                       k_value: Optional[Sequence[int]] = None) -> None:
+    """swan_decode_step_prefix: decode_step with a prefix before each sequence's own tokens."""
+    et = _elem_torch_dtype(desc.dtype)
+    shape = (desc.batch, desc.n_kv_heads, 1, desc.head_dim)
+    _tensor(k_new, "k_new", et, shape)
+    _tensor(v_new, "v_new", et, shape)
+    _decode_tensors(desc, q, P_qk, P_vo, out)
+    device = _same_gpu(q=q, k_new=k_new, v_new=v_new, out=out, P_qk=P_qk, P_vo=P_vo,
+                       workspace=workspace, prefix=prefix.cache.k_pages)
+    if workspace is None or not workspace.is_contiguous():
+        raise SwanError(SWAN_ERR_WORKSPACE, "workspace must be a contiguous GPU tensor")
+    p = prefix._desc(desc.batch)
+    with _calls_on(device):
+        _check(_lib.swan_decode_step_prefix(
+            ctypes.byref(p), ctypes.byref(desc), _i32_array(seq_len), _i32_array(k_active),
+            _opt_i32_array(k_value), _ptr(k_new), _ptr(v_new), _ptr(q), _ptr(P_qk), _ptr(P_vo),
+            float(scale), _ptr(out), _ptr(workspace),
+            workspace.numel() * workspace.element_size(), _stream(stream, device.index)))
+
+
+def prefix_workspace_bytes(prefix: Prefix, desc: CacheDesc, seq_len: Sequence[int],
+                           k_active: Sequence[int],
+                           k_value: Optional[Sequence[int]] = None) -> int:
+    out = ctypes.c_size_t()
+    p = prefix._desc(desc.batch)
+    _check(_lib.swan_prefix_workspace_bytes(ctypes.byref(p), ctypes.byref(desc),
+                                            _i32_array(seq_len), _i32_array(k_active),
+                                            _opt_i32_array(k_value), ctypes.byref(out)))
+    return out.value
+
+
 def set_decode_tuning(target_waves: int = 0, short_split_pages: int = 0, merge_pct: int = 0,
                       side_streams: int = 0) -> None:
     """Split plan and launch grouping of the decode calls on this thread
@@ -472,35 +771,60 @@ class SwanCache:
         self.k_active, self.k_value = k_active, k_value
         self._ws = None
 
-    def workspace(self):
+    def workspace(self, seq_len: Optional[Sequence[int]] = None, prefix: Optional[Prefix] = None):
+        """The decode workspace for these lengths (default: the present ones) and prefix."""
         import torch
 
-        need = decode_workspace_bytes(self.desc, self.seq_len, self.k_active, self.k_value)
+        lens = self.seq_len if seq_len is None else seq_len
+        if prefix is None:
+            need = decode_workspace_bytes(self.desc, lens, self.k_active, self.k_value)
+        else:
+            need = prefix_workspace_bytes(prefix, self.desc, lens, self.k_active, self.k_value)
         if self._ws is None or self._ws.numel() < need:
             self._ws = torch.empty(need, dtype=torch.uint8, device=self.device)
         return self._ws
 
-    def decode(self, q, P_qk, P_vo, out=None, scale: float = 0.0, stream=None):
+    def attend(self, q, P_qk, P_vo, of: Optional[Sequence[int]] = None,
+               n: Optional[Sequence[int]] = None, scale: float = 0.0,
+               prefix: Optional[Prefix] = None, out=None, workspace=None, stream=None):
+        """Rows q [B][H_q][n][128] over all tokens of this cache, of sequence of[b] for query
+        sequence b (-1: none; None: its own, b), and of a prefix: see attend()."""
+        own = Prefix(self, range(self.batch) if of is None else of)
+        return attend([own] if prefix is None else [prefix, own], q, P_qk, P_vo, n, scale, out,
+                      workspace, stream)
+
+    def decode(self, q, P_qk, P_vo, out=None, scale: float = 0.0, stream=None,
+               prefix: Optional[Prefix] = None):
+        """Attention of q ([B][H_q][d]) over the cache, behind a prefix where one is given."""
         import torch
 
         if out is None:
             out = torch.empty_like(q)
-        decode_attention(self.desc, self.seq_len, self.k_active, q, P_qk, P_vo, out,
-                         self.workspace(), scale, stream, self.k_value)
+        if prefix is None:
+            decode_attention(self.desc, self.seq_len, self.k_active, q, P_qk, P_vo, out,
+                             self.workspace(), scale, stream, self.k_value)
+        else:
+            decode_attention_prefix(prefix, self.desc, self.seq_len, self.k_active, q, P_qk, P_vo,
+                                    out, self.workspace(prefix=prefix), scale, stream,
+                                    self.k_value)
         return out
 
-    def step(self, k_new, v_new, q, P_qk, P_vo, out=None, scale: float = 0.0, stream=None):
+    def step(self, k_new, v_new, q, P_qk, P_vo, out=None, scale: float = 0.0, stream=None,
+             prefix: Optional[Prefix] = None):
         """One decode step (swan_decode_step): append k_new / v_new ([B][H_kv][1][d]),
-        advance the lengths, and return the attention of q ([B][H_q][d]) over the cache."""
+        advance the lengths, and return the attention of q ([B][H_q][d]) over the cache,
+        behind a prefix where one is given."""
         import torch
 
         if out is None:
             out = torch.empty_like(q)
         after = [L + 1 for L in self.seq_len]
-        need = decode_workspace_bytes(self.desc, after, self.k_active, self.k_value)
-        if self._ws is None or self._ws.numel() < need:
-            self._ws = torch.empty(need, dtype=torch.uint8, device=self.device)
-        decode_step(self.desc, self.seq_len, self.k_active, k_new, v_new, q, P_qk, P_vo, out,
-                    self._ws, scale, stream, self.k_value)
+        ws = self.workspace(after, prefix)
+        if prefix is None:
+            decode_step(self.desc, self.seq_len, self.k_active, k_new, v_new, q, P_qk, P_vo, out,
+                        ws, scale, stream, self.k_value)
+        else:
+            decode_step_prefix(prefix, self.desc, self.seq_len, self.k_active, k_new, v_new, q,
+                               P_qk, P_vo, out, ws, scale, stream, self.k_value)
         self.seq_len = after
         return out
