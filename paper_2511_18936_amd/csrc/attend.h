@@ -48,50 +48,139 @@ __device__ __forceinline__ float sum_halves(float v) {
   return b.x + b.y;
 }
 
-// The tile in LDS and its products, by element type.  K [key][dim] and V^T [dim][key], with
-// row strides that put 16-byte reads of consecutive rows on distinct banks; key t of a
-// binary16 V^T is at column col(t), which swaps the middle two quads of every 16 so that a
-// lane's 8 keys (8 (i / 4) + 4 (lane / 32) + i % 4, i = 0..7) are contiguous.
+#define SWAN_LDS __attribute__((address_space(3)))
+
+// A tile in LDS: 64 keys' rows of K or V, row-major as in memory, so that they can be
+// loaded without passing through registers.  The 16-byte pieces of row `key` are permuted,
+// piece c at place c ^ turn(key), which puts on distinct banks what the products read
+// together: the same piece of 16 keys (K), and of V the 4 x 2 pieces that a transposing
+// read takes from 4 keys (binary16) or one dim group of two keys (float32).
+template <typename T>
+struct Rows {
+  static constexpr int kBytes = kD * (int)sizeof(T);        // of a row
+  static constexpr int kTile = kTileKeys * kBytes;          // of a tile
+  static constexpr int kPieces = kBytes / 16;               // of a row
+  __device__ static __forceinline__ int turn(int key) {
+    if constexpr (sizeof(T) == 2) return (key & 3) << 2 | (key >> 2 & 3);
+    else return (key >> 2 & 1) << 3 | (key & 3) << 1 | (key >> 3 & 1);
+  }
+  // byte of element d of row `key`
+  __device__ static __forceinline__ int at(int key, int d) {
+    constexpr int N = 16 / (int)sizeof(T);
+    return key * kBytes + ((d / N) ^ turn(key)) * 16 + d % N * (int)sizeof(T);
+  }
+};
+
+// Loads a tile's first `rows` rows (at most 64) from p, zeros in the place of the others;
+// dma_wait() and a barrier before it is read.  Wave w has rows 16 w .. + 15, 1 KiB at a
+// time in the order of the places; `from` are the lane's places in memory (dma_from).
+// Binary16: asynchronous, straight to LDS, in assembly because the compiler would have
+// every later read of LDS wait for it.  Float32, whose tiles lie beyond the 64 KiB that such
+// loads reach: through registers.
+template <typename T>
+struct DmaFrom {
+  static constexpr int N = Rows<T>::kTile / 4096;
+  uint32_t at[N];
+};
+template <typename T>
+__device__ __forceinline__ DmaFrom<T> dma_from(int wave, int lane) {
+  using R = Rows<T>;
+  DmaFrom<T> f;
+#pragma unroll
+  for (int x = 0; x < DmaFrom<T>::N; ++x) {
+    const int key = 16 * wave + x * (1024 / R::kBytes) + lane / R::kPieces;
+    f.at[x] = (uint32_t)(key * R::kBytes + ((lane % R::kPieces) ^ R::turn(key)) * 16);
+  }
+  return f;
+}
+template <typename T>
+__device__ __forceinline__ void dma_tile(char* lds, const T* p, int rows, const DmaFrom<T>& from,
+                                         int wave) {
+  typedef int i4v __attribute__((ext_vector_type(4)));
+  const uint64_t base = (uint64_t)p;
+  rows = rows > kTileKeys ? kTileKeys : rows < 0 ? 0 : rows;
+  if constexpr (sizeof(T) == 4) {
+    u32x4 r[DmaFrom<T>::N];
+#pragma unroll
+    for (int x = 0; x < DmaFrom<T>::N; ++x)
+      r[x] = from.at[x] < (uint32_t)(rows * Rows<T>::kBytes)
+                 ? *(const u32x4*)((const char*)p + from.at[x]) : u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int x = 0; x < DmaFrom<T>::N; ++x)
+      *(u32x4*)(lds + wave * (Rows<T>::kTile / 4) + 1024 * x + 16 * __lane_id()) = r[x];
+    return;
+  }
+  const i4v rsrc = {__builtin_amdgcn_readfirstlane((int)(uint32_t)base),
+                    __builtin_amdgcn_readfirstlane((int)(uint32_t)(base >> 32)),
+                    __builtin_amdgcn_readfirstlane(rows * Rows<T>::kBytes), 0x00020000};
+  const uint32_t to = __builtin_amdgcn_readfirstlane(
+      (uint32_t)(uintptr_t)(SWAN_LDS char*)lds + wave * (Rows<T>::kTile / 4));
+  // (wait states: 5 from v_readfirstlane's SGPRs to a load that reads them, 1 from M0's write)
+#pragma unroll
+  for (int x = 0; x < DmaFrom<T>::N; ++x)
+    asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(from.at[x]), "s"(rsrc),
+                 "{m0}"(to + 1024 * x)
+                 : "memory");
+}
+__device__ __forceinline__ void dma_wait() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// The products, by element type.
 template <typename T>
 struct Tile;
 
 template <>
 struct Tile<_Float16> {
-  static constexpr int KS = 136, VS = 72;
-  struct alignas(16) Buf {
-    _Float16 k[kTileKeys * KS];
-    _Float16 v[kD * VS];
-  };
-  __device__ static __forceinline__ int col(int t) {
-    return (t & ~12) | ((t & 4) << 1) | ((t & 8) >> 1);
-  }
+  using R = Rows<_Float16>;
   // Q of the wave's rows: dims 16 s + 8 (lane / 32) .. + 7 of row lane % 32; kLow: a second
   // part for what the first rounds off
   template <bool kLow>
   struct Q {
     h8v hi[8], lo[kLow ? 8 : 1];
   };
+  static constexpr int kSteps = 16;  // of scores()
+  // S += K . Q^T, the steps (16 dims of one half of the keys) from s0 to s1; the first two
+  // start from zero
   template <bool kLow>
-  __device__ static __forceinline__ void scores(const Buf& b, const Q<kLow>& q, int lane,
-                                                f16v (&S)[2]) {
-    const _Float16* k0 = b.k + (lane & 31) * KS + 8 * (lane >> 5);
+  __device__ static __forceinline__ void scores(const char* kb, const Q<kLow>& q, int lane,
+                                                f16v (&S)[2], int s0 = 0, int s1 = kSteps) {
+    const int key = lane & 31;
 #pragma unroll
-    for (int s = 0; s < 8; ++s)
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const h8v k = *(const h8v*)(k0 + 32 * t * KS + 16 * s);
-        S[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q.hi[s], S[t], 0, 0, 0);
-        if constexpr (kLow) S[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q.lo[s], S[t], 0, 0, 0);
-      }
+    for (int x = s0; x < s1; ++x) {
+      const int t = x & 1, s = x >> 1;
+      const h8v k = *(const SWAN_LDS h8v*)((SWAN_LDS const char*)kb + 32 * t * R::kBytes +
+                                           R::at(key, 16 * s + 8 * (lane >> 5)));
+      if (s == 0) S[t] = f16v{};
+      S[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q.hi[s], S[t], 0, 0, 0);
+      if constexpr (kLow) S[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q.lo[s], S[t], 0, 0, 0);
+    }
   }
-  // p = exp2(S c - ref) into S's place (rounded), O += V^T . p; returns the lane's sum of p
-  __device__ static __forceinline__ float values(const Buf& b, f16v (&S)[2], float c, float ref,
-                                                 int lane, f16v (&O)[4]) {
-    const _Float16* v0 = b.v + (lane & 31) * VS + 8 * (lane >> 5);
+  // V^T of dims 32 d .. + 31 (lane % 32) and the lane's 8 keys of 16 s .. + 15, as the
+  // scores' layout has them: 4 (lane / 32) + {0..3, 8..11}
+  __device__ static __forceinline__ h8v value(const char* vb, int lane, int d, int s) {
+    typedef short s4v __attribute__((ext_vector_type(4)));
+    const int j = lane & 15, dim = 32 * d + 16 * (lane >> 4 & 1) + 4 * (j & 3);
+    const int key = 4 * (lane >> 5) + (j >> 2);
+    s4v x[2];
+#pragma unroll
+    for (int w = 0; w < 2; ++w)
+      x[w] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (SWAN_LDS s4v*)((SWAN_LDS char*)vb + 16 * s * R::kBytes + R::at(8 * w + key, dim)));
+    const u32x2 a = __builtin_bit_cast(u32x2, x[0]), b = __builtin_bit_cast(u32x2, x[1]);
+    return __builtin_bit_cast(h8v, u32x4{a.x, a.y, b.x, b.y});
+  }
+  // p = exp2(S c - ref) (rounded), O += V^T . p; returns the lane's sum of p.  kNext: the
+  // scores of the next tile are taken in between, so that its products run while the
+  // exponentials are computed.
+  template <bool kNext, bool kLow>
+  __device__ static __forceinline__ float values(const char* vb, const f16v (&S)[2], float c,
+                                                 float ref, int lane, f16v (&O)[4],
+                                                 const char* next_k, const Q<kLow>& q,
+                                                 f16v (&next)[2]) {
     const h2v one = {(_Float16)1.f, (_Float16)1.f};
     float l = 0.f;
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
+      if constexpr (kNext) scores<kLow>(next_k, q, lane, next, 4 * s, 4 * s + 4);
       h8v p;
 #pragma unroll
       for (int e = 0; e < 8; e += 2) {
@@ -104,10 +193,8 @@ struct Tile<_Float16> {
         p[e + 1] = two.y;
       }
 #pragma unroll
-      for (int d = 0; d < 4; ++d) {
-        const h8v v = *(const h8v*)(v0 + 32 * d * VS + 16 * s);
-        O[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p, O[d], 0, 0, 0);
-      }
+      for (int d = 0; d < 4; ++d)
+        O[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(value(vb, lane, d, s), p, O[d], 0, 0, 0);
     }
     return l;
   }
@@ -115,48 +202,46 @@ struct Tile<_Float16> {
 
 template <>
 struct Tile<float> {
-  static constexpr int KS = 132, VS = 68;
-  struct alignas(16) Buf {
-    float k[kTileKeys * KS];
-    float v[kD * VS];
-  };
-  __device__ static __forceinline__ int col(int t) { return t; }
+  using R = Rows<float>;
   template <bool kLow>
   struct Q {
     f4v hi[16];  // dims 8 s + 4 (lane / 32) .. + 3
   };
+  static constexpr int kSteps = 32;
   template <bool kLow>
-  __device__ static __forceinline__ void scores(const Buf& b, const Q<kLow>& q, int lane,
-                                                f16v (&S)[2]) {
-    const float* k0 = b.k + (lane & 31) * KS + 4 * (lane >> 5);
+  __device__ static __forceinline__ void scores(const char* kb, const Q<kLow>& q, int lane,
+                                                f16v (&S)[2], int s0 = 0, int s1 = kSteps) {
+    const int key = lane & 31;
 #pragma unroll
-    for (int s = 0; s < 16; ++s)
+    for (int x = s0; x < s1; ++x) {
+      const int t = x & 1, s = x >> 1;
+      const f4v k = *(const SWAN_LDS f4v*)((SWAN_LDS const char*)kb + 32 * t * R::kBytes +
+                                           R::at(key, 8 * s + 4 * (lane >> 5)));
+      if (s == 0) S[t] = f16v{};
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const f4v k = *(const f4v*)(k0 + 32 * t * KS + 8 * s);
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          S[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(k[e], q.hi[s][e], S[t], 0, 0, 0);
-      }
+      for (int e = 0; e < 4; ++e)
+        S[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(k[e], q.hi[s][e], S[t], 0, 0, 0);
+    }
   }
-  __device__ static __forceinline__ float values(const Buf& b, f16v (&S)[2], float c, float ref,
-                                                 int lane, f16v (&O)[4]) {
-    const float* v0 = b.v + (lane & 31) * VS + 4 * (lane >> 5);
+  template <bool kNext, bool kLow>
+  __device__ static __forceinline__ float values(const char* vb, const f16v (&S)[2], float c,
+                                                 float ref, int lane, f16v (&O)[4],
+                                                 const char* next_k, const Q<kLow>& q,
+                                                 f16v (&next)[2]) {
     float l = 0.f;
 #pragma unroll
     for (int s = 0; s < 8; ++s) {
-      f4v p;
+      if constexpr (kNext) scores<kLow>(next_k, q, lane, next, 4 * s, 4 * s + 4);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        p[e] = __builtin_amdgcn_exp2f(fmaf(S[s >> 2][4 * (s & 3) + e], c, -ref));
-        l += p[e];
-      }
+        const float p = __builtin_amdgcn_exp2f(fmaf(S[s >> 2][4 * (s & 3) + e], c, -ref));
+        l += p;
+        const int key = 8 * s + 4 * (lane >> 5) + e;
 #pragma unroll
-      for (int d = 0; d < 4; ++d) {
-        const f4v v = *(const f4v*)(v0 + 32 * d * VS + 8 * s);
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          O[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v[e], p[e], O[d], 0, 0, 0);
+        for (int d = 0; d < 4; ++d)
+          O[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(
+              *(const SWAN_LDS float*)((SWAN_LDS const char*)vb + R::at(key, 32 * d + (lane & 31))),
+              p, O[d], 0, 0, 0);
       }
     }
     return l;

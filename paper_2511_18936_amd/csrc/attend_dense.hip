@@ -4,95 +4,35 @@
 
 namespace swan {
 
-// One tile's rows of k and v in flight: thread t holds 16-byte pieces t, t + 256, ... of K
-// and, of V, E dims (16 bytes) of each of 4 keys, which it writes transposed.
+// Values of a tile that are no numbers leave it (0 times them would be NaN in the rows that
+// must not see their key): zeros in their place, and the keys of this thread's that had one.
 template <typename T>
-struct Stage {
-  static constexpr int E = 16 / (int)sizeof(T);           // elements of a piece
-  static constexpr int kPieces = kTileKeys * kD / E / 256; // per thread: 4 (binary16) or 8
-  static constexpr int kSets = kPieces / 4;                // of 4 keys x E dims
-  u32x4 k[kPieces], v[kSets][4];
-
-  // rows `key0`.. of k and v (row 0 at kp, vp), zeros from row `keys` on
-  __device__ __forceinline__ void load(const T* kp, const T* vp, int key0, int keys, int tid) {
-    const u32x4 zero = {0u, 0u, 0u, 0u};
+__device__ __forceinline__ uint64_t take_nonfinite(char* vb, int tid) {
+  using R = Rows<T>;
+  uint64_t keys = 0;
+#pragma unroll 1
+  for (int piece = tid; piece < R::kTile / 16; piece += 256) {
+    u32x4 x = *(u32x4*)(vb + 16 * piece);
+    bool odd = false;
 #pragma unroll
-    for (int x = 0; x < kPieces; ++x) {
-      const int piece = tid + 256 * x, r = key0 + piece / (kD / E);
-      k[x] = r < keys ? *(const u32x4*)(kp + (int64_t)r * kD + piece % (kD / E) * E) : zero;
-    }
-#pragma unroll
-    for (int x = 0; x < kSets; ++x) {
-      const int set = tid + 256 * x, dim = set / (kTileKeys / 4) * E;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int r = key0 + set % (kTileKeys / 4) * 4 + e;
-        v[x][e] = r < keys ? *(const u32x4*)(vp + (int64_t)r * kD + dim) : zero;
-      }
-    }
-  }
-
-  // Values that are no numbers leave the tile (0 times them would be NaN in the rows that
-  // must not see their key): 1 where a key of this thread has one.  Returns bits of keys.
-  __device__ __forceinline__ uint64_t take_nonfinite(int tid) {
-    uint64_t keys = 0;
-#pragma unroll
-    for (int x = 0; x < kSets; ++x)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int key = (tid + 256 * x) % (kTileKeys / 4) * 4 + e;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          if constexpr (sizeof(T) == 4) {
-            if ((v[x][e][w] & 0x7F800000u) == 0x7F800000u) {
-              v[x][e][w] = 0u;
-              keys |= 1ull << key;
-            }
-          } else {
-            if ((v[x][e][w] & 0x7C00u) == 0x7C00u) {
-              v[x][e][w] &= 0xFFFF0000u;
-              keys |= 1ull << key;
-            }
-            if ((v[x][e][w] & 0x7C000000u) == 0x7C000000u) {
-              v[x][e][w] &= 0xFFFFu;
-              keys |= 1ull << key;
-            }
-          }
-        }
-      }
-    return keys;
-  }
-
-  __device__ __forceinline__ void store(typename Tile<T>::Buf& b, int tid) const {
-    using Tl = Tile<T>;
-#pragma unroll
-    for (int x = 0; x < kPieces; ++x) {
-      const int piece = tid + 256 * x;
-      *(u32x4*)(b.k + piece / (kD / E) * Tl::KS + piece % (kD / E) * E) = k[x];
-    }
-#pragma unroll
-    for (int x = 0; x < kSets; ++x) {
-      const int set = tid + 256 * x, dim = set / (kTileKeys / 4) * E;
-      T* to = b.v + dim * Tl::VS + Tl::col(set % (kTileKeys / 4) * 4);
+    for (int w = 0; w < 4; ++w) {
       if constexpr (sizeof(T) == 4) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          *(u32x4*)(to + e * Tl::VS) = u32x4{v[x][0][e], v[x][1][e], v[x][2][e], v[x][3][e]};
+        const bool a = (x[w] & 0x7F800000u) == 0x7F800000u;
+        x[w] = a ? 0u : x[w];
+        odd |= a;
       } else {
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          // dims 2 w and 2 w + 1 of the four keys
-          const u32x2 even = {__builtin_amdgcn_perm(v[x][1][w], v[x][0][w], 0x05040100u),
-                              __builtin_amdgcn_perm(v[x][3][w], v[x][2][w], 0x05040100u)};
-          const u32x2 odd = {__builtin_amdgcn_perm(v[x][1][w], v[x][0][w], 0x07060302u),
-                             __builtin_amdgcn_perm(v[x][3][w], v[x][2][w], 0x07060302u)};
-          *(u32x2*)(to + 2 * w * Tl::VS) = even;
-          *(u32x2*)(to + (2 * w + 1) * Tl::VS) = odd;
-        }
+        const bool a = (x[w] & 0x7C00u) == 0x7C00u, b = (x[w] & 0x7C000000u) == 0x7C000000u;
+        x[w] &= (a ? 0xFFFF0000u : ~0u) & (b ? 0xFFFFu : ~0u);
+        odd |= a || b;
       }
     }
+    if (odd) {
+      *(u32x4*)(vb + 16 * piece) = x;
+      keys |= 1ull << (piece / R::kPieces);
+    }
   }
-};
+  return keys;
+}
 
 // O += p v for the values that take_nonfinite() took out of the tile, key by key, in the
 // rows that see the key.  Rare: the loops are for size, not for speed.
@@ -130,7 +70,9 @@ __device__ __forceinline__ void add_nonfinite(uint64_t keys, const T* vp, int ke
 template <typename T>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kernel(AttendLaunch a) {
   using Tl = Tile<T>;
-  __shared__ typename Tl::Buf buf[2];
+  using R = Rows<T>;
+  __shared__ __align__(1024) char kbuf[2][R::kTile];
+  __shared__ __align__(1024) char vbuf[2][R::kTile];
   __shared__ uint64_t odd_keys;  // keys of a tile with values that are no numbers
   __shared__ int any_odd;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -159,23 +101,32 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kern
   const int all_see = a.causal ? min(keys, max(0, tok_first + shift + 1)) : keys;
   const int block_all = a.causal ? min(keys, max(0, (int)(row0 / G) + shift + 1)) : keys;
   const int seen = a.causal ? (int)min((int64_t)keys, max((int64_t)0, tok_last + shift + 1)) : keys;
-  const int wave_last = (int)min((int64_t)toks - 1, (row0 + 32 * wave + 31) / G);
-  const int wave_sees = tok_first >= toks ? 0
-                        : a.causal ? min(keys, max(0, wave_last + shift + 1)) : keys;
   const int nt = (seen + kTileKeys - 1) / kTileKeys;
   const int t0 = (int)((int64_t)nt * split / nsplit), t1 = (int)((int64_t)nt * (split + 1) / nsplit);
 
   const int64_t kv0 = ((int64_t)b * a.Hkv + h) * a.m * kD;
   const T* kp = (const T*)a.k + kv0;
   const T* vp = (const T*)a.v + kv0;
-  Stage<T> st;
+  const DmaFrom<T> from = dma_from<T>(wave, lane);
+  // tile t is tile t - t0 of its buffers' turns; past the last, nothing
+  auto load_k = [&](int t) {
+    if (t < t1)
+      dma_tile(kbuf[(t - t0) & 1], kp + (int64_t)t * kTileKeys * kD, keys - t * kTileKeys, from,
+               wave);
+  };
+  auto load_v = [&](int t) {
+    if (t < t1)
+      dma_tile(vbuf[(t - t0) & 1], vp + (int64_t)t * kTileKeys * kD, keys - t * kTileKeys, from,
+               wave);
+  };
   if (tid == 0) any_odd = 0;
-  if (t0 < t1) st.load(kp, vp, t0 * kTileKeys, keys, tid);
+  load_k(t0);
+  load_v(t0);
 
   typename Tl::template Q<false> q;
   {
     const T* qr = (const T*)a.q + row * kD;
-    constexpr int N = sizeof(q.hi) / 16, E = Stage<T>::E;
+    constexpr int N = sizeof(q.hi) / 16, E = 16 / (int)sizeof(T);
     u32x4* to = (u32x4*)&q;
 #pragma unroll
     for (int s = 0; s < N; ++s)
@@ -199,58 +150,60 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kern
         }
     }
   }
-  __syncthreads();  // any_odd
-  auto put = [&](int t) {
-    // only tiles that some row sees in part are looked through
-    if ((t + 1) * kTileKeys > block_all && st.take_nonfinite(tid)) any_odd = 1;
-    st.store(buf[(t - t0) & 1], tid);
-  };
-  if (t0 < t1) {
-    put(t0);
-    if (t0 + 1 < t1) st.load(kp, vp, (t0 + 1) * kTileKeys, keys, tid);
-  }
+  // A tile's scores are taken during the exponentials of the one before, so its keys are in
+  // LDS one tile ahead of its values; a buffer is loaded again after the barrier behind its
+  // last reads.
+  f16v S[2], next[2];
+  dma_wait();
+  __syncthreads();  // tile t0, any_odd
+  load_k(t0 + 1);
+  if (t0 < t1) Tl::template scores<false>(kbuf[0], q, lane, S);
+  dma_wait();
   __syncthreads();
   for (int t = t0; t < t1; ++t) {
-    const typename Tl::Buf& tb = buf[(t - t0) & 1];
-    const int key0 = t * kTileKeys;
-    if (key0 < wave_sees) {  // uniform in the wave
-      f16v S[2];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) S[0][i] = S[1][i] = 0.f;
-      Tl::template scores<false>(tb, q, lane, S);
-      if (key0 + kTileKeys > all_see) {
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (key0 + key_of(x, i, lane) >= limit) S[x][i] = -INFINITY;
-      }
-      rs.raise(tile_max(S) * a.qmult);
-      rs.l += Tl::values(tb, S, a.qmult, rs.safe_ref(), lane, rs.O);
+    const int key0 = t * kTileKeys, par = (t - t0) & 1;
+    load_k(t + 2);
+    load_v(t + 1);
+    if (key0 + kTileKeys > block_all) {  // only tiles that some row sees in part
+      if (take_nonfinite<T>(vbuf[par], tid)) any_odd = 1;
+      __syncthreads();
     }
+    if (key0 + kTileKeys > all_see) {
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (key0 + key_of(x, i, lane) >= limit) S[x][i] = -INFINITY;
+    }
+    rs.raise(tile_max(S) * a.qmult);
+    const float ref = rs.safe_ref();
     if (t + 1 < t1) {
-      put(t + 1);
-      if (t + 2 < t1) st.load(kp, vp, (t + 2) * kTileKeys, keys, tid);
+      rs.l += Tl::template values<true>(vbuf[par], S, a.qmult, ref, lane, rs.O, kbuf[par ^ 1], q,
+                                        next);
+      S[0] = next[0];
+      S[1] = next[1];
+    } else {
+      rs.l += Tl::template values<false>(vbuf[par], S, a.qmult, ref, lane, rs.O, kbuf[0], q, next);
     }
+    dma_wait();
     __syncthreads();
   }
-  if (any_odd) {  // uniform: their keys' values, with the scores taken again
+  if (any_odd) {  // uniform: what take_nonfinite() took, with its keys' scores taken again
 #pragma unroll 1
     for (int t = max(t0, block_all / kTileKeys); t < t1; ++t) {
       const int key0 = t * kTileKeys;
       if (tid == 0) odd_keys = 0;
-      st.load(kp, vp, key0, keys, tid);
+      dma_tile(kbuf[0], kp + (int64_t)key0 * kD, keys - key0, from, wave);
+      dma_tile(vbuf[0], vp + (int64_t)key0 * kD, keys - key0, from, wave);
+      dma_wait();
       __syncthreads();
-      const uint64_t mine = st.take_nonfinite(tid);
+      const uint64_t mine = take_nonfinite<T>(vbuf[0], tid);
       if (mine) atomicOr((unsigned long long*)&odd_keys, (unsigned long long)mine);
-      st.store(buf[0], tid);
       __syncthreads();
       const uint64_t odd = odd_keys;
-      if (odd && key0 < wave_sees) {
+      if (odd) {
         f16v P[2];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) P[0][i] = P[1][i] = 0.f;
-        Tl::template scores<false>(buf[0], q, lane, P);
+        Tl::template scores<false>(kbuf[0], q, lane, P);
         const float ref = rs.safe_ref();
 #pragma unroll
         for (int x = 0; x < 2; ++x)

@@ -12,24 +12,26 @@
 
 namespace swan {
 
-// Groups of 8 entries of both roles' pages, numbered keys first, go to the 4 waves round
-// robin; a lane holds its token's 8 values and indices of each.
+// Groups of 8 entries of a page of keys and one of values, numbered keys first, go to the 4
+// waves round robin; a lane holds its token's 8 values and indices of each.
 template <typename T, int NU>
 struct PageStage {
+  using E = typename Fmt<T>::Elem;
   static constexpr int CB = Fmt<T>::kChunkBytes;
   static constexpr int VCH = 8 * Fmt<T>::kValBytes / CB;
   using Chunk = typename std::conditional<CB == 16, u32x4, u32x2>::type;
   Chunk val[NU][VCH];
   u32x2 idx[NU];
 
+  // kpage / vpage: NULL for a tile that is no page
   __device__ __forceinline__ void load(const char* kpage, const char* vpage, int nk, int nv,
                                        int wave, int lane) {
 #pragma unroll
     for (int x = 0; x < NU; ++x) {
       const int u = wave + 4 * x;  // uniform
-      if (u < nk + nv) {
-        const bool key = u < nk;
-        const char* page = key ? kpage : vpage;
+      const bool key = u < nk;
+      const char* page = key ? kpage : vpage;
+      if (u < nk + nv && page) {
         const int g = key ? u : u - nk, n8 = key ? nk : nv;
 #pragma unroll
         for (int c = 0; c < VCH; ++c)
@@ -39,23 +41,26 @@ struct PageStage {
     }
   }
 
-  __device__ __forceinline__ void scatter(typename Tile<typename Fmt<T>::Elem>::Buf& b, int nk,
-                                          int nv, int wave, int lane, bool valid) const {
-    using E = typename Fmt<T>::Elem;
-    using Tl = Tile<E>;
-    if (!valid) return;
-    E* kt = b.k + lane * Tl::KS;
-    E* vt = b.v + Tl::col(lane);
+  // into the (zeroed) tiles; ktoken / vtoken: this lane has a token there
+  __device__ __forceinline__ void scatter(char* kb, char* vb, int nk, int nv, int wave, int lane,
+                                          bool ktoken, bool vtoken) const {
+    using R = Rows<E>;
+    constexpr int N = 16 / (int)sizeof(E);
+    SWAN_LDS E* krow = (SWAN_LDS E*)((SWAN_LDS char*)kb + lane * R::kBytes);
+    SWAN_LDS E* vrow = (SWAN_LDS E*)((SWAN_LDS char*)vb + lane * R::kBytes);
+    const int turn = R::turn(lane) * N;
 #pragma unroll
     for (int x = 0; x < NU; ++x) {
       const int u = wave + 4 * x;
       if (u < nk + nv) {
-        E* to = u < nk ? kt : vt;
-        const int step = u < nk ? 1 : Tl::VS;
+        SWAN_LDS E* to = u < nk ? krow : vrow;
+        if (u < nk ? ktoken : vtoken) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int d = ((e < 4 ? idx[x].x : idx[x].y) >> (8 * (e & 3))) & 0x7F;
-          to[d * step] = value(x, e);
+          for (int e = 0; e < 8; ++e) {
+            // (the mask keeps a damaged page's indices inside the row)
+            const int d = ((e < 4 ? idx[x].x : idx[x].y) >> (8 * (e & 3))) & 0x7F;
+            to[d ^ turn] = value(x, e);
+          }
         }
       }
     }
@@ -76,28 +81,6 @@ struct PageStage {
   }
 };
 
-// 64 rows of the ring (zeros past its end) into a tile
-template <typename E>
-__device__ __forceinline__ void ring_tile(typename Tile<E>::Buf& b, const E* kr, const E* vr,
-                                          int row0, int rows, int tid) {
-  using Tl = Tile<E>;
-  constexpr int N = 16 / (int)sizeof(E);
-  const u32x4 zero = {0u, 0u, 0u, 0u};
-#pragma unroll 4
-  for (int piece = tid; piece < kTileKeys * kD / N; piece += 256) {
-    const int r = piece / (kD / N), d = piece % (kD / N) * N;
-    const bool in = row0 + r < rows;
-    const int64_t at = (int64_t)(row0 + r) * kD + d;
-    *(u32x4*)(b.k + r * Tl::KS + d) = in ? *(const u32x4*)(kr + at) : zero;
-    const u32x4 v = in ? *(const u32x4*)(vr + at) : zero;
-    struct alignas(16) {
-      E e[N];
-    } x = __builtin_bit_cast(decltype(x), v);
-#pragma unroll
-    for (int e = 0; e < N; ++e) b.v[(d + e) * Tl::VS + Tl::col(r)] = x.e[e];
-  }
-}
-
 // Grid as in attend_dense_kernel.  A group's keys are its pages, then tiles of its ring
 // (in slot order: the sum has none).
 template <typename T, int NU>
@@ -105,7 +88,9 @@ __global__ __launch_bounds__(256, sizeof(typename Fmt<T>::Elem) == 2 ? 2 : 1) vo
 attend_pages_kernel(AttendLaunch a) {
   using E = typename Fmt<T>::Elem;
   using Tl = Tile<E>;
-  __shared__ typename Tl::Buf buf[2];
+  using R = Rows<E>;
+  __shared__ __align__(1024) char kbuf[2][R::kTile];
+  __shared__ __align__(1024) char vbuf[2][R::kTile];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int G = a.Hq / a.Hkv;
@@ -133,11 +118,43 @@ attend_pages_kernel(AttendLaunch a) {
   const char* vpages = (const char*)a.v + a.off[1][j] + (int64_t)h * a.npc * vbytes;
   const int64_t ring = ((int64_t)cs * a.Hkv + h) * a.bb * kD;
 
+  const DmaFrom<E> from = dma_from<E>(wave, lane);
   PageStage<T, NU> st;
-  auto load = [&](int t) {
-    if (t < np) st.load(kpages + t * kbytes, vpages + t * vbytes, nk, nv, wave, lane);
+  // stage(k, v): the loads of tile k's keys and of tile v's values, where they are pages
+  auto stage = [&](int k, int v) {
+    st.load(k < t1 && k < np ? kpages + k * kbytes : nullptr,
+            v < t1 && v < np ? vpages + v * vbytes : nullptr, nk, nv, wave, lane);
   };
-  if (t0 < t1) load(t0);
+  // clear(k, v): zeros where those tiles are pages, the ring's rows where they are not
+  auto clear = [&](int k, int v) {
+    const u32x4 zero = {0u, 0u, 0u, 0u};
+    bool ring_tile = false;
+    if (k < t1 && k < np) {
+#pragma unroll
+      for (int x = 0; x < R::kTile / 4096; ++x)
+        ((u32x4*)kbuf[(k - t0) & 1])[tid + 256 * x] = zero;
+    } else if (k < t1) {
+      dma_tile(kbuf[(k - t0) & 1], (const E*)a.k_ring + ring + (int64_t)(k - np) * kTileKeys * kD,
+               nb - (k - np) * kTileKeys, from, wave);
+      ring_tile = true;
+    }
+    if (v < t1 && v < np) {
+#pragma unroll
+      for (int x = 0; x < R::kTile / 4096; ++x)
+        ((u32x4*)vbuf[(v - t0) & 1])[tid + 256 * x] = zero;
+    } else if (v < t1) {
+      dma_tile(vbuf[(v - t0) & 1], (const E*)a.v_ring + ring + (int64_t)(v - np) * kTileKeys * kD,
+               nb - (v - np) * kTileKeys, from, wave);
+      ring_tile = true;
+    }
+    return ring_tile;
+  };
+  // scatter(k, v): what stage(k, v) loaded
+  auto scatter = [&](int k, int v) {
+    st.scatter(kbuf[(k - t0) & 1], vbuf[(v - t0) & 1], nk, nv, wave, lane,
+               k < t1 && k * kPage + lane < S, v < t1 && v * kPage + lane < S);
+  };
+  stage(t0, t0);
 
   // the row's queries
   typename Tl::template Q<true> q;
@@ -179,38 +196,21 @@ attend_pages_kernel(AttendLaunch a) {
   }
   RowState rs;
   rs.clear();
-  auto clear = [&](int t) {  // a page's tile starts from zeros; its stores follow a barrier
-    if (t >= np) return;
-    u32x4* z = (u32x4*)&buf[(t - t0) & 1];
-    for (int x = tid; x < (int)(sizeof(buf[0]) / 16); x += 256) z[x] = u32x4{0u, 0u, 0u, 0u};
-  };
-  auto put = [&](int t) {
-    typename Tl::Buf& tb = buf[(t - t0) & 1];
-    if (t < np) st.scatter(tb, nk, nv, wave, lane, t * kPage + lane < S);
-    else
-      ring_tile<E>(tb, (const E*)a.k_ring + ring, (const E*)a.v_ring + ring,
-                   (t - np) * kTileKeys, nb, tid);
-  };
-  if (t0 < t1) {
-    clear(t0);
-    __syncthreads();
-    put(t0);
-    if (t0 + 1 < t1) load(t0 + 1);
-    __syncthreads();
-  }
+  f16v Sc[2];
+  bool ring_tile = clear(t0, t0);
+  __syncthreads();
+  scatter(t0, t0);
+  stage(t0 + 1, t0 + 1);
+  if (ring_tile) dma_wait();
+  __syncthreads();
   for (int t = t0; t < t1; ++t) {
-    if (t + 1 < t1) {
-      clear(t + 1);
-      __syncthreads();
-      put(t + 1);
-      if (t + 2 < t1) load(t + 2);
-    }
+    const int par = (t - t0) & 1;
+    ring_tile = clear(t + 1, t + 1);
+    __syncthreads();
+    scatter(t + 1, t + 1);
+    stage(t + 2, t + 2);
     if (busy) {
-      const typename Tl::Buf& tb = buf[(t - t0) & 1];
-      f16v Sc[2];
-#pragma unroll
-      for (int x = 0; x < 16; ++x) Sc[0][x] = Sc[1][x] = 0.f;
-      Tl::template scores<true>(tb, q, lane, Sc);
+      Tl::template scores<true>(kbuf[par], q, lane, Sc);
       const int count = t < np ? S - t * kPage : nb - (t - np) * kTileKeys;
       if (count < kTileKeys) {
 #pragma unroll
@@ -220,8 +220,10 @@ attend_pages_kernel(AttendLaunch a) {
             if (key_of(x, e, lane) >= count) Sc[x][e] = -INFINITY;
       }
       rs.raise(tile_max(Sc) * c);
-      rs.l += Tl::values(tb, Sc, c, rs.safe_ref(), lane, rs.O);
+      rs.l += Tl::template values<false>(vbuf[par], Sc, c, rs.safe_ref(), lane, rs.O, kbuf[0], q,
+                                         Sc);
     }
+    if (ring_tile) dma_wait();
     __syncthreads();
   }
   write_partial(a, rs, row, split, live, lane);
