@@ -112,10 +112,10 @@ swan_status swan_attend(const swan_prefix* sources, int32_t n_sources, int32_t b
  *                256-byte aligned.
  * Values that a row does not see do not reach it, infinities and NaNs included.
  */
-swan_status swan_prompt_workspace_bytes(int32_t batch, int32_t n_q_heads, int32_t n_kv_heads,
-                                        int32_t n, int32_t m, int32_t head_dim,
-                                        const int32_t* n_host, const int32_t* m_host,
-                                        int32_t causal, size_t* bytes);
+swan_status swan_prompt_workspace_bytes(int32_t dtype, int32_t batch, int32_t n_q_heads,
+                                        int32_t n_kv_heads, int32_t n, int32_t m,
+                                        int32_t head_dim, const int32_t* n_host,
+                                        const int32_t* m_host, int32_t causal, size_t* bytes);
 swan_status swan_prompt_attention(const void* q, const void* k, const void* v, int32_t dtype,
                                   int32_t batch, int32_t n_q_heads, int32_t n_kv_heads,
                                   int32_t n, int32_t m, int32_t head_dim, const int32_t* n_host,

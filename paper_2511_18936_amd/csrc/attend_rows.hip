@@ -79,67 +79,87 @@ hipError_t launch_rotate_rows(const RotateLaunch& a) {
   return hipGetLastError();
 }
 
-// One workgroup per row, thread t the dim t: out of partials (m, l, acc) the sums
-// l = sum_i 2^(m_i - m) l_i, o = sum_i 2^(m_i - m) acc_i / l in fixed order.  The partials:
-// those of swan_decode_attention's kernels (a decode step's own cache), then of each
-// source, then the state (lse, 1, o).
+// The parts of a row: (m, l, acc) of swan_decode_attention's kernels over a decode step's
+// own cache, then those of each source, then the state (lse, 1, o).  Their sum is
+//   l = sum_i 2^(m_i - m) l_i,  o = sum_i 2^(m_i - m) acc_i / l
+// (an empty part has m = -inf, l = 0 and a zero accumulator).
+struct Parts {
+  const float* own;
+  const float* part;
+  const float* lse0;
+  int own_ns, own_slots, n0, n1, n2, total, base0, base1;
+  __device__ __forceinline__ Parts(const JoinLaunch& a, int b, int64_t row) {
+    own_slots = a.own_slots;
+    own_ns = n0 = 0;
+    if (a.own) {
+      const int L = a.own_tab.len[b];
+      const int np = pages_for(L > a.own_bb ? L - a.own_bb : 0);
+      own_ns = np < a.own_tab.nsplit[b] ? np : a.own_tab.nsplit[b];
+      n0 = own_ns + (min(L, a.own_bb) > 0 ? 1 : 0);  // the last: the buffer's, in slot own_slots
+    }
+    n1 = n0 + a.used[0][b];
+    n2 = n1 + a.used[1][b];
+    total = n2 + (a.o0 ? 1 : 0);
+    base0 = a.base[0] - n0;
+    base1 = a.base[1] - n1;
+    own = a.own + row * (a.own_slots + 1) * kPartFloats;
+    part = a.part + row * a.slots * kPartFloats;
+    lse0 = a.lse0 + row;
+  }
+  __device__ __forceinline__ const float* at(int x) const {  // x < n2
+    if (x < n0) return own + (x < own_ns ? x : own_slots) * kPartFloats;
+    return part + (x < n1 ? base0 + x : base1 + x) * kPartFloats;
+  }
+  __device__ __forceinline__ float m_of(int x) const {  // x < total
+    return x < n2 ? at(x)[0] : *lse0 * kLog2e;
+  }
+};
+
+// Decode: a workgroup per row.  The weights of its parts once, in LDS; then a quarter of the
+// threads (32 lanes of 4 dims) adds up every fourth part, and the result is turned back.
 constexpr int kMaxJoin = kMaxSplits + 1 + 2 * kMaxSlots + 1;
 template <typename T>
-__global__ __launch_bounds__(128) void join_kernel(JoinLaunch a) {
+__global__ __launch_bounds__(128) void join_decode_kernel(JoinLaunch a) {
   __shared__ float wts[kMaxJoin];
+  __shared__ f4v sums[4][kD / 4];
   __shared__ float oh[kD];
   __shared__ float red[4];
-  const int t = threadIdx.x, i = blockIdx.x % a.n, bh = blockIdx.x / a.n;
-  const int b = bh / a.H;
-  if (i >= a.rows[b]) return;
-  const int64_t row = blockIdx.x;
-  int own_ns = 0, own_n = 0;  // splits; with the buffer's partial (slot own_slots)
-  if (a.own) {
-    const int L = a.own_tab.len[b];
-    const int np = pages_for(L > a.own_bb ? L - a.own_bb : 0);
-    own_ns = np < a.own_tab.nsplit[b] ? np : a.own_tab.nsplit[b];
-    own_n = own_ns + (min(L, a.own_bb) > 0 ? 1 : 0);
-  }
-  const int n0 = own_n, n1 = n0 + a.used[0][b], n2 = n1 + a.used[1][b];
-  const int total = n2 + (a.o0 ? 1 : 0);
-  const float* own = a.own + row * (a.own_slots + 1) * kPartFloats;
-  const float* part = a.part + row * a.slots * kPartFloats;
-  auto at = [&](int x) {  // x < n2
-    if (x < n0) return own + (x < own_ns ? x : a.own_slots) * kPartFloats;
-    return part + (x < n1 ? a.base[0] + x - n0 : a.base[1] + x - n1) * kPartFloats;
-  };
+  const int t = threadIdx.x, bh = blockIdx.x, b = bh / a.H;
+  const Parts ps(a, b, bh);
   float mloc = -INFINITY;
-  for (int x = t; x < total; x += 128)
-    mloc = fmaxf(mloc, x < n2 ? at(x)[0] : a.lse0[row] * kLog2e);
+  for (int x = t; x < ps.n2; x += 128) mloc = fmaxf(mloc, ps.at(x)[0]);
   mloc = wave_max(mloc);
   if ((t & 63) == 0) red[t >> 6] = mloc;
   __syncthreads();
   const float m = fmaxf(red[0], red[1]);
   float lloc = 0.f;
-  for (int x = t; x < total; x += 128) {
-    const float mx = x < n2 ? at(x)[0] : a.lse0[row] * kLog2e;
-    const float w = mx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mx - m);
+  for (int x = t; x < ps.n2; x += 128) {
+    const float* part = ps.at(x);
+    const float w = part[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(part[0] - m);
     wts[x] = w;
-    lloc += w * (x < n2 ? at(x)[1] : 1.f);
+    lloc += w * part[1];
   }
   lloc = wave_sum(lloc);
   if ((t & 63) == 0) red[2 + (t >> 6)] = lloc;
   __syncthreads();
   const float l = red[2] + red[3];
-  float o = 0.f;
-  for (int x = 0; x < n2; ++x) o = fmaf(wts[x], at(x)[4 + t], o);  // (an empty part's are 0)
-  if (n2 < total && wts[n2] != 0.f) o = fmaf(wts[n2], a.o0[row * kD + t], o);
-  o = l == 0.f ? 0.f : o / l;
-  if (!a.out) {
-    a.o[row * kD + t] = o;
-    if (t == 0) a.lse[row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) / kLog2e;
-    return;
+  f4v o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int x = t >> 5; x < ps.n2; x += 4) {
+    const f4v acc = *(const f4v*)(ps.at(x) + 4 + 4 * (t & 31));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = fmaf(wts[x], acc[e], o[e]);
   }
+  sums[t >> 5][t & 31] = o;
+  __syncthreads();
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const float* s = (const float*)sums;
+  const float mine = ((s[t] + s[kD + t]) + (s[2 * kD + t] + s[3 * kD + t])) * inv;
   if (!a.P_vo) {
-    ((T*)a.out)[row * kD + t] = (T)o;
+    ((T*)a.out)[(int64_t)bh * kD + t] = (T)mine;
     return;
   }
-  oh[t] = o;
+  oh[t] = mine;
   __syncthreads();
   const float4* P = (const float4*)(a.P_vo + ((int64_t)(bh % a.H / (a.H / a.Hkv)) * kD + t) * kD);
   float r = 0.f;
@@ -151,16 +171,79 @@ __global__ __launch_bounds__(128) void join_kernel(JoinLaunch a) {
     r = fmaf(p.z, oh[4 * j4 + 2], r);
     r = fmaf(p.w, oh[4 * j4 + 3], r);
   }
-  ((T*)a.out)[row * kD + t] = (T)r;
+  ((T*)a.out)[(int64_t)bh * kD + t] = (T)r;
+}
+
+// Many rows: half a wave per row, a lane 4 dims; 32 parts' weights at a time are the lanes'.
+template <typename T>
+__global__ __launch_bounds__(256) void join_rows_kernel(JoinLaunch a) {
+  const int lane = threadIdx.x & 31;
+  const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  if (row >= (int64_t)a.B * a.H * a.n) return;
+  const int i = (int)(row % a.n), b = (int)(row / a.n / a.H);
+  if (i >= a.rows[b]) return;
+  const Parts ps(a, b, row);
+  float m = -INFINITY;
+  for (int x = lane; x < ps.total; x += 32) m = fmaxf(m, ps.m_of(x));
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 32));
+  float l = 0.f;
+  f4v o = {0.f, 0.f, 0.f, 0.f};
+  for (int x0 = 0; x0 < ps.total; x0 += 32) {
+    float w = 0.f;
+    if (x0 + lane < ps.total) {
+      const float mx = ps.m_of(x0 + lane);
+      w = mx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mx - m);
+      l += w * (x0 + lane < ps.n2 ? ps.at(x0 + lane)[1] : 1.f);
+    }
+    const int count = min(32, ps.n2 - x0);
+#pragma unroll 4
+    for (int x = 0; x < count; ++x) {
+      const f4v acc = *(const f4v*)(ps.at(x0 + x) + 4 + 4 * lane);
+      const float wx = __shfl(w, x, 32);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = fmaf(wx, acc[e], o[e]);
+    }
+    if (ps.n2 < ps.total && ps.n2 >= x0 && ps.n2 < x0 + 32) {  // the state
+      const float wx = __shfl(w, ps.n2 - x0, 32);
+      if (wx != 0.f) {  // (the o of a row that has none is not looked at)
+        const f4v acc = *(const f4v*)(a.o0 + row * kD + 4 * lane);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = fmaf(wx, acc[e], o[e]);
+      }
+    }
+  }
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) l += __shfl_xor(l, d, 32);
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o[e] *= inv;
+  if (!a.out) {
+    *(f4v*)(a.o + row * kD + 4 * lane) = o;
+    if (lane == 0) a.lse[row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) / kLog2e;
+    return;
+  }
+  struct alignas(4 * sizeof(T)) {
+    T v[4];
+  } y;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) y.v[e] = (T)o[e];
+  *(decltype(y)*)((T*)a.out + row * kD + 4 * lane) = y;
+}
+
+template <typename T>
+static hipError_t launch_join_t(const JoinLaunch& a) {
+  const int64_t rows = (int64_t)a.B * a.H * a.n;
+  if (a.own)
+    hipLaunchKernelGGL(join_decode_kernel<T>, dim3((unsigned)rows), dim3(128), 0, a.stream, a);
+  else
+    hipLaunchKernelGGL(join_rows_kernel<T>, dim3((unsigned)((rows + 7) / 8)), dim3(256), 0,
+                       a.stream, a);
+  return hipGetLastError();
 }
 
 hipError_t launch_join(const JoinLaunch& a) {
-  const dim3 grid((unsigned)((int64_t)a.B * a.H * a.n));
-  if (a.dtype == SWAN_F32)
-    hipLaunchKernelGGL(join_kernel<float>, grid, dim3(128), 0, a.stream, a);
-  else
-    hipLaunchKernelGGL(join_kernel<_Float16>, grid, dim3(128), 0, a.stream, a);
-  return hipGetLastError();
+  return a.dtype == SWAN_F32 ? launch_join_t<float>(a) : launch_join_t<_Float16>(a);
 }
 
 }  // namespace swan

@@ -11,10 +11,19 @@ namespace swan {
 
 typedef double f64x2 __attribute__((ext_vector_type(2)));
 
+// y rounded once.  Binary16: y cut to float32's 24 bits, the last one set if anything was
+// cut off (round to odd), is a float32 number that rounds to binary16 as y does.  (The same
+// as f64_to_f16_bits_fast, half the instructions, no branch.)
 template <typename T>
 __device__ __forceinline__ T stored(double y) {
-  if constexpr (sizeof(T) == 2) return __builtin_bit_cast(T, f64_to_f16_bits_fast(y));
-  else return (T)y;
+  if constexpr (sizeof(T) == 2) {
+    const uint64_t bits = (uint64_t)__double_as_longlong(y);
+    const uint32_t lo = (uint32_t)bits, cut = (lo & 0x1FFFFFFFu) + 0x1FFFFFFFu;
+    const uint64_t odd = (bits & 0xFFFFFFFF00000000ull) | ((lo | cut) & 0xE0000000u);
+    return (T)(float)__longlong_as_double((long long)odd);
+  } else {
+    return (T)y;
+  }
 }
 
 template <typename T>
@@ -55,27 +64,81 @@ __device__ __forceinline__ void weights_at(const QkvRowsLaunch& a, int role, int
   }
 }
 
-// sum over the `N` (16 or 64) lanes that hold a row
+// sum over the 16 lanes of a row of lanes, then (N = 64) over the wave
+template <int CTRL>
+__device__ __forceinline__ double rotated(double v) {
+  const uint64_t x = (uint64_t)__double_as_longlong(v);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)x, CTRL, 0xF, 0xF, true);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(x >> 32), CTRL, 0xF, 0xF, true);
+  return __longlong_as_double((long long)((uint64_t)hi << 32 | lo));
+}
 template <int N>
 __device__ __forceinline__ double row_sum(double v) {
-#pragma unroll
-  for (int d = N / 2; d > 0; d >>= 1) v += __shfl_xor(v, d, 64);
+  v += rotated<0x128>(v);
+  v += rotated<0x124>(v);
+  v += rotated<0x122>(v);
+  v += rotated<0x121>(v);
+  if constexpr (N == 64) {
+    v += __shfl_xor(v, 16, 64);
+    v += __shfl_xor(v, 32, 64);
+  }
   return v;
 }
 
 constexpr int kTilePos = 4;  // positions of a workgroup
 
-// A workgroup takes 4 positions at a time: its 256 threads compute their 4 x 64 sines and
-// cosines once for all heads, then a quarter wave (16 lanes of 4 pairs, 8-byte accesses for
-// binary16) has a head's row of one position, wave w heads w, w + 4, ...
 template <typename T>
-__global__ __launch_bounds__(256) void qkv_rows_kernel(QkvRowsLaunch a) {
+struct alignas(4 * sizeof(T)) Four {
+  T v[4];
+};
+
+// One row's 4 + 4 elements of a lane (of 16): norm with weights w (NULL: none), rotation
+template <typename T>
+__device__ __forceinline__ void turn_row(Four<T>& lo, Four<T>& hi, const double* w, double eps,
+                                         const double (&c)[4], const double (&s)[4]) {
+  double x0[4], x1[4];
+  bool nan = false;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    x0[e] = (double)(float)lo.v[e];
+    x1[e] = (double)(float)hi.v[e];
+    nan |= __builtin_isunordered((float)lo.v[e], (float)hi.v[e]);
+  }
+  if (w) {
+    double ss = 0.0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) ss += x0[e] * x0[e] + x1[e] * x1[e];
+    const double r = inv_root<T>(row_sum<16>(ss) * (1.0 / kD) + eps);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      x0[e] *= r * w[e];
+      x1[e] *= r * w[4 + e];
+    }
+    nan |= !(r - r == 0.0);
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    lo.v[e] = stored<T>(x0[e] * c[e] - x1[e] * s[e]);
+    hi.v[e] = stored<T>(x1[e] * c[e] + x0[e] * s[e]);
+  }
+  if (nan)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      one_nan_of(lo.v[e]);
+      one_nan_of(hi.v[e]);
+    }
+}
+
+// A workgroup takes 4 positions at a time and `heads` of their heads (grid: positions,
+// chunks of heads): its 256 threads compute the 4 x 64 sines and cosines once for all of
+// them, then a quarter wave (16 lanes of 4 pairs, 8-byte accesses for binary16) has a head's
+// row of one position, wave w every fourth head, two at a time.
+template <typename T>
+__global__ __launch_bounds__(256) void qkv_rows_kernel(QkvRowsLaunch a, int heads) {
   __shared__ f64x2 cs[kTilePos][kD / 2];
-  struct alignas(4 * sizeof(T)) Vec {
-    T v[4];
-  };
+  using Vec = Four<T>;
   const int t = threadIdx.x, wave = t >> 6, p = (t >> 4) & 3, l = t & 15;
-  const int H = a.Hq + 2 * a.Hkv;
+  const int h0 = blockIdx.y * heads, h1 = min(a.Hq + 2 * a.Hkv, h0 + heads);
   const uint32_t n = (uint32_t)a.n, positions = (uint32_t)a.B * n;  // below 2^31
   const uint32_t tiles = (positions + kTilePos - 1) / kTilePos;
   const double freq = pow(a.base, -(2.0 * (t & 63)) / kD);
@@ -91,62 +154,54 @@ __global__ __launch_bounds__(256) void qkv_rows_kernel(QkvRowsLaunch a) {
     }
     __syncthreads();
     const uint32_t at = tile * kTilePos + p;
-    const bool live = at < positions;
-    const int b = live ? (int)(at / n) : 0, i = live ? (int)(at - b * n) : 0;
-    double c[4], s[4];
+    if (at < positions) {
+      const int b = (int)(at / n), i = (int)(at - b * n);
+      const T* row = (const T*)a.x + b * a.seq + i * a.row + 4 * l;
+      double c[4], s[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const f64x2 v = cs[p][4 * l + e];
-      c[e] = v.x;
-      s[e] = v.y;
-    }
-    const T* row = (const T*)a.x + b * a.seq + i * a.row + 4 * l;
-    if (live) {
-      for (int h = wave; h < H; h += 4) {
-        const Vec lo = *(const Vec*)(row + h * kD), hi = *(const Vec*)(row + h * kD + kD / 2);
-        const int role = h < a.Hq ? 0 : h < a.Hq + a.Hkv ? 1 : 2;
-        const int hr = role == 0 ? h : role == 1 ? h - a.Hq : h - a.Hq - a.Hkv;
-        T* to = (T*)a.out[role] +
-                (((int64_t)b * (role == 0 ? a.Hq : a.Hkv) + hr) * a.n + i) * kD + 4 * l;
-        Vec y = lo, z = hi;
-        if (role < 2) {
-          double x0[4], x1[4];
-          bool nan = false;
+      for (int e = 0; e < 4; ++e) {
+        const f64x2 v = cs[p][4 * l + e];
+        c[e] = v.x;
+        s[e] = v.y;
+      }
+      int first = 0;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            x0[e] = (double)(float)lo.v[e];
-            x1[e] = (double)(float)hi.v[e];
-            nan |= __builtin_isunordered((float)lo.v[e], (float)hi.v[e]);
-          }
-          if (a.w[role]) {
-            double ss = 0.0;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) ss += x0[e] * x0[e] + x1[e] * x1[e];
-            const double r = inv_root<T>(row_sum<16>(ss) * (1.0 / kD) + a.eps);
-            double w0[4], w1[4];
-            weights_at<T>(a, role, (int64_t)hr * a.wstep + 4 * l, w0);
-            weights_at<T>(a, role, (int64_t)hr * a.wstep + 4 * l + kD / 2, w1);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              x0[e] *= r * w0[e];
-              x1[e] *= r * w1[e];
-            }
-            nan |= !(r - r == 0.0);
-          }
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            y.v[e] = stored<T>(x0[e] * c[e] - x1[e] * s[e]);
-            z.v[e] = stored<T>(x1[e] * c[e] + x0[e] * s[e]);
-          }
-          if (nan)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              one_nan_of(y.v[e]);
-              one_nan_of(z.v[e]);
-            }
+      for (int role = 0; role < 3; ++role) {
+        const int count = role == 0 ? a.Hq : a.Hkv, last = min(first + count, h1);
+        T* out = (T*)a.out[role] + (((int64_t)b * count - first) * a.n + i) * kD + 4 * l;
+        const bool norm = role < 2 && a.w[role] != nullptr;
+        double w[8];
+        if (norm && a.wstep == 0) {
+          weights_at<T>(a, role, 4 * l, *(double(*)[4])w);
+          weights_at<T>(a, role, 4 * l + kD / 2, *(double(*)[4])(w + 4));
         }
-        *(Vec*)to = y;
-        *(Vec*)(to + kD / 2) = z;
+        // the first of this wave's heads that is the chunk's and this role's
+        for (int h = max(first, h0) + wave; h < last; h += 8) {
+          const bool two = h + 4 < last;
+          Vec lo[2], hi[2];
+          lo[0] = *(const Vec*)(row + h * kD);
+          hi[0] = *(const Vec*)(row + h * kD + kD / 2);
+          if (two) {
+            lo[1] = *(const Vec*)(row + (h + 4) * kD);
+            hi[1] = *(const Vec*)(row + (h + 4) * kD + kD / 2);
+          }
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            if (x == 1 && !two) break;
+            if (role < 2) {
+              if (norm && a.wstep) {
+                const int64_t at = (int64_t)(h + 4 * x - first) * a.wstep + 4 * l;
+                weights_at<T>(a, role, at, *(double(*)[4])w);
+                weights_at<T>(a, role, at + kD / 2, *(double(*)[4])(w + 4));
+              }
+              turn_row<T>(lo[x], hi[x], norm ? w : nullptr, a.eps, c, s);
+            }
+            T* to = out + (int64_t)(h + 4 * x) * a.n * kD;
+            *(Vec*)to = lo[x];
+            *(Vec*)(to + kD / 2) = hi[x];
+          }
+        }
+        first += count;
       }
     }
     __syncthreads();
@@ -198,9 +253,15 @@ static hipError_t launch_qkv_rows_t(const QkvRowsLaunch& a) {
     hipLaunchKernelGGL(qkv_rows_few_kernel<T>, dim3(a.n, H, a.B), dim3(64), 0, a.stream, a);
     return hipGetLastError();
   }
+  // Few positions split their heads, 4 at least to each, over 512 workgroups: more of them
+  // only repeat the sines and cosines (32 + 2 x 8 heads x 1999 positions, binary16: 14.7 us
+  // with 512, 16.2 with 1100, 19.6 with 2048).
   const int64_t tiles = (positions + kTilePos - 1) / kTilePos;
-  const dim3 grid((unsigned)(tiles < 2048 ? tiles : 2048));
-  hipLaunchKernelGGL(qkv_rows_kernel<T>, grid, dim3(256), 0, a.stream, a);
+  int64_t chunks = 512 / tiles;
+  chunks = chunks < 1 ? 1 : chunks > (H + 3) / 4 ? (H + 3) / 4 : chunks;
+  const int heads = (int)(((H + chunks - 1) / chunks + 3) / 4 * 4);
+  const dim3 grid((unsigned)(tiles < 2048 ? tiles : 2048), (unsigned)((H + heads - 1) / heads));
+  hipLaunchKernelGGL(qkv_rows_kernel<T>, grid, dim3(256), 0, a.stream, a, heads);
   return hipGetLastError();
 }
 

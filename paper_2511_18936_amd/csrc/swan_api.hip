@@ -440,8 +440,70 @@ swan_status step_prep(const swan_cache* c, const int32_t* seq_len_host,
 // ---------------------------------------------------------------------------
 // attention of several rows per sequence, and of decode steps behind a prefix
 // ---------------------------------------------------------------------------
-// units of attend kernels that fill the GPU (two workgroups on each of 256 CUs)
-constexpr int64_t kUnits = 512;
+// What a plan of the attend kernels costs, in microseconds as measured: a workgroup's
+// start, and a tile of 64 keys of a workgroup on a full GPU (`slots` workgroups).
+struct AttendCost {
+  int slots;
+  double tile, start;
+};
+AttendCost attend_cost(int32_t dtype, bool pages) {
+  if (dtype == SWAN_F32) return {256, pages ? 16.0 : 12.0, 8.0};
+  return {512, pages ? 3.9 : 2.3, 6.0};
+}
+
+// Tiles of keys per workgroup, so that the launch and the join of its partials are
+// shortest: tiles[j] of keys for base[j] row tiles (times kv heads) of group j, `rows` rows
+// in all.  Plans that fill the GPU 1/2 (a workgroup alone on a CU takes its tiles in 0.65 of
+// the time), 1, 2, ... times are compared.  uneven: a row tile may have fewer tiles than the
+// others of its group (causal), so workgroups even out; join: also one part has to be joined.
+int plan_tiles(const AttendCost& c, int groups, const int64_t* base, const int* tiles,
+               int64_t rows, bool uneven, bool join) {
+  int longest = 1;
+  double total = 0;
+  for (int j = 0; j < groups; ++j) {
+    longest = tiles[j] > longest ? tiles[j] : longest;
+    total += (double)base[j] * tiles[j] * (uneven ? 0.5 : 1.0);
+  }
+  auto units = [&](int per) {
+    int64_t u = 0;
+    for (int j = 0; j < groups; ++j) u += base[j] * ((tiles[j] + per - 1) / per > 1 ? (tiles[j] + per - 1) / per : 1);
+    return u;
+  };
+  auto cost = [&](int per) {
+    const int64_t u = units(per);
+    const double waves = (double)((u + c.slots - 1) / c.slots);
+    const int parts = (longest + per - 1) / per;
+    double run = waves * per;
+    if (uneven || u > 4 * c.slots) {  // the GPU stays full until the last ones
+      const double even = total / c.slots + 0.5 * per;
+      run = even < run ? even : run;
+    }
+    if (run < per) run = per;
+    if (c.slots > 256 && u <= 256) run *= 0.65;
+    double t = waves * c.start + run * c.tile;
+    if (join || parts > 1) t += 4.0 + (double)rows * parts * (2.0 * 528 / 4e6);
+    return t;
+  };
+  int best = longest;
+  double least = cost(longest);
+  const int64_t fills[] = {256, c.slots, 2 * c.slots, 3 * c.slots, 4 * c.slots, 6 * c.slots};
+  for (const int64_t fill : fills) {
+    int lo = 1, hi = longest;  // the fewest tiles with at most `fill` workgroups
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if (units(mid) <= fill) hi = mid;
+      else lo = mid + 1;
+    }
+    const int least_per = (longest + swan::kMaxSlots - 1) / swan::kMaxSlots;
+    if (lo < least_per) lo = least_per;
+    const double t = cost(lo);
+    if (t < least * 0.98) {
+      least = t;
+      best = lo;
+    }
+  }
+  return best;
+}
 
 swan_status check_scale(float scale) {
   if (!(scale == scale) || isinf(scale)) return fail(SWAN_ERR_INVALID_ARG, "scale is not finite");
@@ -496,7 +558,7 @@ int key_tiles(const swan_cache* c, int L) {
 }
 
 // Groups and splits of a source: one group per cache sequence with tokens and query rows.
-// About kUnits workgroups in all, every split with a tile; used[b] = splits of query
+// Every split has a tile; used[b] = splits of query
 // sequence b's group (0: none).  Returns the largest.
 int plan_pages(const swan_prefix* s, int32_t batch, int32_t n, const int32_t* n_host,
                swan::AttendLaunch& a, int16_t* used) {
@@ -507,7 +569,6 @@ int plan_pages(const swan_prefix* s, int32_t batch, int32_t n, const int32_t* n_
   fill_layout(c, s->k_active_host, s->k_value_host, tab, bytes);
   a.groups = 0;
   int entries = 0;
-  int64_t work = 0;
   int64_t row_tiles[SWAN_MAX_BATCH];
   for (int b = 0; b < batch; ++b) used[b] = 0;
   for (int p = 0; p < c->batch; ++p) {
@@ -532,22 +593,26 @@ int plan_pages(const swan_prefix* s, int32_t batch, int32_t n, const int32_t* n_
       a.kact[r][j] = (uint8_t)tab.kact[r][p];
     }
     row_tiles[j] = (toks * G + swan::kTileRows - 1) / swan::kTileRows;
-    work += row_tiles[j] * key_tiles(c, a.keys[j]);
     ++a.groups;
   }
   a.first[a.groups] = (uint8_t)entries;
-  const int64_t per = (work * c->n_kv_heads + kUnits - 1) / kUnits;  // key tiles of a unit
+  int tiles[SWAN_MAX_BATCH];
+  int64_t base[SWAN_MAX_BATCH], rows = 0;
+  for (int j = 0; j < a.groups; ++j) {
+    tiles[j] = key_tiles(c, a.keys[j]);
+    base[j] = row_tiles[j] * c->n_kv_heads;
+    rows += (int64_t)a.toks[j] * c->n_q_heads;
+  }
+  const int per = plan_tiles(attend_cost(c->dtype, true), a.groups, base, tiles, rows, false, true);
   int most = 0;
   int64_t units = 0;
   for (int j = 0; j < a.groups; ++j) {
-    const int nt = key_tiles(c, a.keys[j]);
-    int64_t ns = (nt + per - 1) / per;
-    ns = ns > swan::kMaxSlots ? swan::kMaxSlots : ns < 1 ? 1 : ns;
+    const int ns = (tiles[j] + per - 1) / per;
     a.nsplit[j] = (int16_t)ns;
     a.unit0[j] = (int32_t)units;
     units += row_tiles[j] * ns * c->n_kv_heads;
     for (int e = a.first[j]; e < a.first[j + 1]; ++e) used[a.seq[e]] = (int16_t)ns;
-    most = ns > most ? (int)ns : most;
+    most = ns > most ? ns : most;
   }
   a.unit0[a.groups] = (int32_t)units;
   a.units = units > INT32_MAX ? -1 : (int)units;
@@ -621,9 +686,10 @@ struct PromptPlan {
   size_t bytes;
 };
 
-swan_status prompt_prep(int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t n, int32_t m,
+swan_status prompt_prep(int32_t dtype, int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t n, int32_t m,
                         int32_t head_dim, const int32_t* n_host, const int32_t* m_host,
                         int32_t causal, PromptPlan& pl) {
+  if (!dtype_ok(dtype)) return fail(SWAN_ERR_UNSUPPORTED, "dtype %d not supported", dtype);
   if (batch < 1 || batch > SWAN_MAX_BATCH)
     return fail(SWAN_ERR_INVALID_ARG, "batch %d outside 1..%d", batch, SWAN_MAX_BATCH);
   if (n_kv_heads < 1 || n_q_heads < 1 || n_q_heads % n_kv_heads != 0)
@@ -654,7 +720,8 @@ swan_status prompt_prep(int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, in
     }
     order[at] = b;
   }
-  int64_t base = 0;
+  int tiles[SWAN_MAX_BATCH];
+  int64_t base[SWAN_MAX_BATCH], rows = 0;
   for (int j = 0; j < count; ++j) {
     const int b = order[j];
     a.first[j] = (uint8_t)j;
@@ -662,22 +729,21 @@ swan_status prompt_prep(int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, in
     a.tok0[j] = 0;
     a.toks[j] = n_host ? n_host[b] : n;
     a.keys[j] = m_host ? m_host[b] : m;
-    base += ((int64_t)a.toks[j] * G + swan::kTileRows - 1) / swan::kTileRows * n_kv_heads;
+    tiles[j] = (a.keys[j] + swan::kTileKeys - 1) / swan::kTileKeys;
+    base[j] = ((int64_t)a.toks[j] * G + swan::kTileRows - 1) / swan::kTileRows * n_kv_heads;
+    rows += (int64_t)a.toks[j] * n_q_heads;
   }
   a.first[count] = (uint8_t)count;
   a.groups = count;
+  const int per = plan_tiles(attend_cost(dtype, false), count, base, tiles, rows, causal != 0, false);
   int64_t units = 0;
   int most = 1;
   for (int j = 0; j < count; ++j) {
-    const int64_t tiles = ((int64_t)a.toks[j] * G + swan::kTileRows - 1) / swan::kTileRows;
-    // few row tiles: the keys are split over more workgroups, four tiles of them at least
-    const int nt = (a.keys[j] + swan::kTileKeys - 1) / swan::kTileKeys;
-    int64_t ns = kUnits / base < nt / 4 ? kUnits / base : nt / 4;
-    ns = ns > swan::kMaxSlots ? swan::kMaxSlots : ns < 1 ? 1 : ns;
+    const int ns = tiles[j] > per ? (tiles[j] + per - 1) / per : 1;
     a.nsplit[j] = (int16_t)ns;
     a.unit0[j] = (int32_t)units;
-    units += tiles * ns * n_kv_heads;
-    most = ns > most ? (int)ns : most;
+    units += base[j] * ns;
+    most = ns > most ? ns : most;
     pl.used[order[j]] = (int16_t)ns;
     if (units > INT32_MAX) return fail(SWAN_ERR_UNSUPPORTED, "too many rows for one call");
   }
@@ -1197,13 +1263,13 @@ swan_status swan_attend(const swan_prefix* sources, int32_t n_sources, int32_t b
   return hip_status(swan::launch_rotate_rows(r), "rotate launch");
 }
 
-swan_status swan_prompt_workspace_bytes(int32_t batch, int32_t n_q_heads, int32_t n_kv_heads,
+swan_status swan_prompt_workspace_bytes(int32_t dtype, int32_t batch, int32_t n_q_heads, int32_t n_kv_heads,
                                         int32_t n, int32_t m, int32_t head_dim,
                                         const int32_t* n_host, const int32_t* m_host,
                                         int32_t causal, size_t* bytes) {
   if (!bytes) return fail(SWAN_ERR_INVALID_ARG, "bytes is NULL");
   PromptPlan pl;
-  const swan_status st = prompt_prep(batch, n_q_heads, n_kv_heads, n, m, head_dim, n_host, m_host,
+  const swan_status st = prompt_prep(dtype, batch, n_q_heads, n_kv_heads, n, m, head_dim, n_host, m_host,
                                      causal, pl);
   if (st != SWAN_OK) return st;
   *bytes = pl.bytes;
@@ -1216,9 +1282,8 @@ swan_status swan_prompt_attention(const void* q, const void* k, const void* v, i
                                   const int32_t* m_host, int32_t causal, float scale,
                                   const float* o0, const float* lse0, void* out,
                                   void* workspace, size_t workspace_bytes, void* stream) {
-  if (!dtype_ok(dtype)) return fail(SWAN_ERR_UNSUPPORTED, "dtype %d not supported", dtype);
   PromptPlan pl;
-  swan_status st = prompt_prep(batch, n_q_heads, n_kv_heads, n, m, head_dim, n_host, m_host,
+  swan_status st = prompt_prep(dtype, batch, n_q_heads, n_kv_heads, n, m, head_dim, n_host, m_host,
                                causal, pl);
   if (st != SWAN_OK) return st;
   if ((st = check_scale(scale)) != SWAN_OK) return st;

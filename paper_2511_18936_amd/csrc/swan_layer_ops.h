@@ -83,12 +83,13 @@ struct RotateLaunch {
 };
 hipError_t launch_rotate_rows(const RotateLaunch& a);
 
-// the partials of up to two sources (and a state) of a row to one result
+// The partials of a row to one result: of up to two sources and a state, or (decode, with
+// `own`) of one source and a decode step's own cache.
 struct JoinLaunch {
   const float* part;   // [B H n][slots][kPartFloats]
   const float* o0;     // a state to continue from, or NULL
   const float* lse0;
-  const float* P_vo;   // decode: rotates the result back, or NULL
+  const float* P_vo;   // with `own`: rotates the result back, or NULL
   void* out;           // storage type, or NULL
   float* o;            // float32 state, or NULL (unless `out`)
   float* lse;

@@ -120,7 +120,7 @@ def _load() -> ctypes.CDLL:
         "swan_attend_workspace_bytes": [pprefix, i32, i32, i32, pi32, psz],
         "swan_attend": [pprefix, i32, i32, i32, pi32, vp, vp, vp, ctypes.c_float, vp, vp, vp, sz,
                         vp],
-        "swan_prompt_workspace_bytes": [i32, i32, i32, i32, i32, i32, pi32, pi32, i32, psz],
+        "swan_prompt_workspace_bytes": [i32, i32, i32, i32, i32, i32, i32, pi32, pi32, i32, psz],
         "swan_prompt_attention": [vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, pi32, pi32, i32,
                                   ctypes.c_float, vp, vp, vp, vp, sz, vp],
         "swan_prefix_workspace_bytes": [pprefix, pdesc, pi32, pi32, pi32, psz],
@@ -413,16 +413,24 @@ def _same_gpu(**tensors):
     return device
 
 
-def _calls_on(device):
+class _CallsOn:
     """Makes `device` current where it is not: a call is enqueued on a stream of the
-    current device."""
-    import contextlib
+    current device.  Gives the stream's handle."""
 
-    import torch
+    def __init__(self, device, stream):
+        self.index, self.stream, self.guard = device.index, stream, None
 
-    if device.index is None or device.index == torch.cuda.current_device():
-        return contextlib.nullcontext()
-    return torch.cuda.device(device)
+    def __enter__(self):
+        import torch
+
+        if self.index != torch.cuda.current_device():
+            self.guard = torch.cuda.device(self.index)
+            self.guard.__enter__()
+        return _stream(self.stream, self.index)
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
 
 
 def _per_sequence(values: Optional[Sequence[int]], batch: int, name: str):
@@ -458,8 +466,11 @@ def _made(how: str, shape, dtype, device, stream):
     import torch
 
     dtype = getattr(torch, dtype) if isinstance(dtype, str) else dtype
-    with torch.cuda.stream(stream):  # (None: the current one)
-        return getattr(torch, how)(shape, dtype=dtype, device=device)
+    make = getattr(torch, how)
+    if stream is None:
+        return make(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return make(shape, dtype=dtype, device=device)
 
 
 def qkv_rows(qkv, n_q_heads: int, n_kv_heads: int, pos0: Sequence[int], base: float,
@@ -507,11 +518,11 @@ def qkv_rows(qkv, n_q_heads: int, n_kv_heads: int, pos0: Sequence[int], base: fl
     # a dimension of one element has no stride of its own
     row = qkv.stride(1) if n > 1 else width
     seq = qkv.stride(0) if B > 1 else 0
-    with _calls_on(device):
+    with _CallsOn(device, stream) as s:
         _check(_lib.swan_qkv_rows(_ptr(qkv), seq, row, code, B, n_q_heads, n_kv_heads, n, HEAD_DIM,
                                   _per_sequence(pos0, B, "pos0"), float(base), _ptr(q_weight),
                                   _ptr(k_weight), int(bool(per_head)), int(bool(w32)), float(eps),
-                                  _ptr(q), _ptr(k), _ptr(v), _stream(stream, device.index)))
+                                  _ptr(q), _ptr(k), _ptr(v), s))
     return q, k, v
 
 
@@ -540,16 +551,16 @@ def prompt_attention(q, k, v, causal: bool = True, n: Optional[Sequence[int]] = 
     device = _same_gpu(q=q, k=k, v=v, out=out, o=o0, lse=lse0)
     ns, ms = _per_sequence(n, B, "n"), _per_sequence(m, B, "m")
     need = ctypes.c_size_t()
-    _check(_lib.swan_prompt_workspace_bytes(B, hq, hkv, nq, nk, d, ns, ms, int(causal),
+    _check(_lib.swan_prompt_workspace_bytes(code, B, hq, hkv, nq, nk, d, ns, ms, int(causal),
                                             ctypes.byref(need)))
     ws = None
     if need.value:
         ws = _workspace(workspace, need.value, device, stream)
-    with _calls_on(device):
+    with _CallsOn(device, stream) as s:
         _check(_lib.swan_prompt_attention(
             _ptr(q), _ptr(k), _ptr(v), code, B, hq, hkv, nq, nk, d, ns, ms, int(causal),
             float(scale), _ptr(o0), _ptr(lse0), _ptr(out), _ptr(ws),
-            0 if ws is None else ws.numel() * ws.element_size(), _stream(stream, device.index)))
+            0 if ws is None else ws.numel() * ws.element_size(), s))
     return out
 
 
@@ -613,10 +624,10 @@ def attend(sources, q, P_qk, P_vo, n: Optional[Sequence[int]] = None, scale: flo
     need = ctypes.c_size_t()
     _check(_lib.swan_attend_workspace_bytes(descs, len(sources), B, nq, ns, ctypes.byref(need)))
     ws = _workspace(workspace, need.value, device, stream)
-    with _calls_on(device):
+    with _CallsOn(device, stream) as s:
         _check(_lib.swan_attend(descs, len(sources), B, nq, ns, _ptr(q), _ptr(P_qk), _ptr(P_vo),
                                 float(scale), _ptr(o), _ptr(lse), _ptr(ws),
-                                ws.numel() * ws.element_size(), _stream(stream, device.index)))
+                                ws.numel() * ws.element_size(), s))
     return o, lse
 
 
@@ -632,12 +643,12 @@ def decode_attention_prefix(prefix: Prefix, desc: CacheDesc, seq_len: Sequence[i
     if workspace is None or not workspace.is_contiguous():
         raise SwanError(SWAN_ERR_WORKSPACE, "workspace must be a contiguous GPU tensor")
     p = prefix._desc(desc.batch)
-    with _calls_on(device):
+    with _CallsOn(device, stream) as s:
         _check(_lib.swan_decode_attention_prefix(
             ctypes.byref(p), ctypes.byref(desc), _i32_array(seq_len), _i32_array(k_active),
             _opt_i32_array(k_value), _ptr(q), _ptr(P_qk), _ptr(P_vo), float(scale), _ptr(out),
             _ptr(workspace), workspace.numel() * workspace.element_size(),
-            _stream(stream, device.index)))
+            s))
 
 
 def decode_step_prefix(prefix: Prefix, desc: CacheDesc, seq_len: Sequence[int],
@@ -655,12 +666,12 @@ def decode_step_prefix(prefix: Prefix, desc: CacheDesc, seq_len: Sequence[int],
     if workspace is None or not workspace.is_contiguous():
         raise SwanError(SWAN_ERR_WORKSPACE, "workspace must be a contiguous GPU tensor")
     p = prefix._desc(desc.batch)
-    with _calls_on(device):
+    with _CallsOn(device, stream) as s:
         _check(_lib.swan_decode_step_prefix(
             ctypes.byref(p), ctypes.byref(desc), _i32_array(seq_len), _i32_array(k_active),
             _opt_i32_array(k_value), _ptr(k_new), _ptr(v_new), _ptr(q), _ptr(P_qk), _ptr(P_vo),
             float(scale), _ptr(out), _ptr(workspace),
-            workspace.numel() * workspace.element_size(), _stream(stream, device.index)))
+            workspace.numel() * workspace.element_size(), s))
 
 
 def prefix_workspace_bytes(prefix: Prefix, desc: CacheDesc, seq_len: Sequence[int],
