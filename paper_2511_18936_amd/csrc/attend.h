@@ -294,6 +294,10 @@ __device__ __forceinline__ float tile_max(const f16v (&S)[2]) {
   return max_halves(m);
 }
 
+// A unit: kv head, split and row tile (in grid order) of group j
+struct Unit {
+  int j, h, split, nsplit, tile;
+};
 // the group of a unit (uniform)
 __device__ __forceinline__ int group_of(const AttendLaunch& a, int unit) {
   int lo = 0, hi = a.groups;  // unit0[lo] <= unit < unit0[hi]
@@ -303,6 +307,27 @@ __device__ __forceinline__ int group_of(const AttendLaunch& a, int unit) {
     else hi = mid;
   }
   return lo;
+}
+
+// Unit u of a group: kv head u % Hkv (so that a head's tiles fall to few of the 8 XCDs and
+// its keys stay in their L2), then the split, then the row tile.
+__device__ __forceinline__ Unit unit_at(const AttendLaunch& a, int block) {
+  Unit n;
+  n.j = group_of(a, block);
+  const uint32_t u = (uint32_t)(block - a.unit0[n.j]), rest = a.by_hkv.of(u);
+  n.h = (int)(u - rest * a.by_hkv.d);
+  n.nsplit = a.nsplit[n.j];
+  n.tile = (int)rest;
+  n.split = 0;
+  if (n.nsplit > 1) {
+    n.tile = (int)(rest / (uint32_t)n.nsplit);
+    n.split = (int)(rest - (uint32_t)n.tile * (uint32_t)n.nsplit);
+  }
+  return n;
+}
+// first of nt tiles of a split (nt at most 2^23, splits 2^8)
+__device__ __forceinline__ int split_first(int nt, int split, int nsplit) {
+  return nsplit == 1 ? split * nt : (int)((uint32_t)nt * (uint32_t)split / (uint32_t)nsplit);
 }
 
 // sequence b and row i of it that token `tok` of group j is

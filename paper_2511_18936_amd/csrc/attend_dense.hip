@@ -64,9 +64,8 @@ __device__ __forceinline__ void add_nonfinite(uint64_t keys, const T* vp, int ke
   }
 }
 
-// Grid: a.units workgroups of 4 waves.  Unit u of a group: kv head u % Hkv (so that a
-// head's tiles fall to few of the 8 XCDs and its keys stay in their L2), then the split,
-// then the row tile, the last (of a causal prompt the longest) first.
+// Grid: a.units workgroups of 4 waves (unit_at), a group's last row tiles, of a causal prompt
+// the longest, first.
 template <typename T>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kernel(AttendLaunch a) {
   using Tl = Tile<T>;
@@ -74,35 +73,30 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kern
   __shared__ __align__(1024) char kbuf[2][R::kTile];
   __shared__ __align__(1024) char vbuf[2][R::kTile];
   __shared__ uint64_t odd_keys;  // keys of a tile with values that are no numbers
-  __shared__ int any_odd;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int G = a.Hq / a.Hkv;
-  const int j = group_of(a, blockIdx.x);
-  int u = blockIdx.x - a.unit0[j];
-  const int h = u % a.Hkv;
-  u /= a.Hkv;
-  const int nsplit = a.nsplit[j], split = u % nsplit;
-  const int toks = a.toks[j], keys = a.keys[j];
-  const int tiles = (int)(((int64_t)toks * G + kTileRows - 1) / kTileRows);
-  const int64_t row0 = (int64_t)(tiles - 1 - u / nsplit) * kTileRows;
-  const int b = a.cseq[j];
+  const int G = (int)a.by_g.d;
+  const Unit un = unit_at(a, blockIdx.x);
+  const int h = un.h, toks = a.toks[un.j], keys = a.keys[un.j], b = a.cseq[un.j];
+  const uint32_t rows = (uint32_t)toks * (uint32_t)G;  // below 2^31
+  const uint32_t row0 = ((rows + kTileRows - 1) / kTileRows - 1 - un.tile) * kTileRows;
 
   // this lane's row
-  const int64_t r = row0 + 32 * wave + (lane & 31);
-  const int tok = (int)(r / G), g = (int)(r % G);
+  const uint32_t r = row0 + 32 * wave + (lane & 31);
+  const int tok = (int)a.by_g.of(r), g = (int)(r - (uint32_t)tok * (uint32_t)G);
   const bool live = tok < toks;
   const int64_t row = ((int64_t)b * a.Hq + h * G + g) * a.n + tok;
-  const int shift = keys - toks;  // causal: row i sees keys up to i + shift
-  const int limit = !live ? 0 : a.causal ? min(keys, max(0, tok + shift + 1)) : keys;
-  // keys that every row of the wave sees, and that some row of the workgroup sees
-  const int tok_first = (int)((row0 + 32 * wave) / G);
-  const int64_t tok_last = min((int64_t)toks - 1, (row0 + kTileRows - 1) / G);
-  const int all_see = a.causal ? min(keys, max(0, tok_first + shift + 1)) : keys;
-  const int block_all = a.causal ? min(keys, max(0, (int)(row0 / G) + shift + 1)) : keys;
-  const int seen = a.causal ? (int)min((int64_t)keys, max((int64_t)0, tok_last + shift + 1)) : keys;
+  // Causal: row i sees the keys up to i + shift.  limit: those this lane's row sees; all_see,
+  // block_all: that every row of the wave, of the workgroup sees; seen: that some row does.
+  const int shift = keys - toks;
+  auto sees = [&](int tok) { return a.causal ? min(keys, max(0, tok + shift + 1)) : keys; };
+  const int limit = live ? sees(tok) : 0;
+  const int all_see = sees((int)a.by_g.of(row0 + 32 * wave));
+  const int block_all = sees((int)a.by_g.of(row0));
+  const int seen = sees(min(toks - 1, (int)a.by_g.of(row0 + kTileRows - 1)));
   const int nt = (seen + kTileKeys - 1) / kTileKeys;
-  const int t0 = (int)((int64_t)nt * split / nsplit), t1 = (int)((int64_t)nt * (split + 1) / nsplit);
+  const int t0 = split_first(nt, un.split, un.nsplit);
+  const int t1 = split_first(nt, un.split + 1, un.nsplit);
 
   const int64_t kv0 = ((int64_t)b * a.Hkv + h) * a.m * kD;
   const T* kp = (const T*)a.k + kv0;
@@ -119,9 +113,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kern
       dma_tile(vbuf[(t - t0) & 1], vp + (int64_t)t * kTileKeys * kD, keys - t * kTileKeys, from,
                wave);
   };
-  if (tid == 0) any_odd = 0;
   load_k(t0);
   load_v(t0);
+  load_k(t0 + 1);
 
   typename Tl::template Q<false> q;
   {
@@ -133,41 +127,28 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kern
       to[s] = live ? *(const u32x4*)(qr + 2 * E * s + E * (lane >> 5)) : u32x4{0u, 0u, 0u, 0u};
   }
   RowState rs;
-  rs.clear();
-  if (a.o0 && live && !a.part) {
-    const float lse = a.lse0[row] * kLog2e;
-    if (lse != -INFINITY) {
-      rs.ref = lse - kHead;
-      rs.l = lane < 32 ? 128.f : 0.f;  // 2^kHead
-      const float* o = a.o0 + row * kD + 4 * (lane >> 5);
-#pragma unroll
-      for (int d = 0; d < 4; ++d)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const f4v x = *(const f4v*)(o + 32 * d + 8 * i);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) rs.O[d][4 * i + e] = x[e] * 128.f;
-        }
-    }
-  }
   // A tile's scores are taken during the exponentials of the one before, so its keys are in
   // LDS one tile ahead of its values; a buffer is loaded again after the barrier behind its
   // last reads.
-  f16v S[2], next[2];
-  dma_wait();
-  __syncthreads();  // tile t0, any_odd
-  load_k(t0 + 1);
-  if (t0 < t1) Tl::template scores<false>(kbuf[0], q, lane, S);
-  dma_wait();
-  __syncthreads();
-  for (int t = t0; t < t1; ++t) {
-    const int key0 = t * kTileKeys, par = (t - t0) & 1;
-    load_k(t + 2);
-    load_v(t + 1);
-    if (key0 + kTileKeys > block_all) {  // only tiles that some row sees in part
-      if (take_nonfinite<T>(vbuf[par], tid)) any_odd = 1;
-      __syncthreads();
-    }
+  //
+  auto begin = [&]() {  // the state to continue from, or none
+    rs.clear();
+    if (!a.o0 || !live || a.part) return;
+    const float lse = a.lse0[row] * kLog2e;
+    if (lse == -INFINITY) return;
+    rs.ref = lse - kHead;
+    rs.l = lane < 32 ? 128.f : 0.f;  // 2^kHead
+    const float* o = a.o0 + row * kD + 4 * (lane >> 5);
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f4v x = *(const f4v*)(o + 32 * d + 8 * i);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) rs.O[d][4 * i + e] = x[e] * 128.f;
+      }
+  };
+  auto mask = [&](f16v (&S)[2], int key0) {
     if (key0 + kTileKeys > all_see) {
 #pragma unroll
       for (int x = 0; x < 2; ++x)
@@ -175,48 +156,74 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kern
         for (int i = 0; i < 16; ++i)
           if (key0 + key_of(x, i, lane) >= limit) S[x][i] = -INFINITY;
     }
+  };
+  begin();
+  f16v S[2], next[2];
+  dma_wait();
+  __syncthreads();
+  if (t0 < t1) Tl::template scores<false>(kbuf[0], q, lane, S);
+  __syncthreads();
+  for (int t = t0; t < t1 - 1; ++t) {
+    const int par = (t - t0) & 1;
+    load_k(t + 2);
+    load_v(t + 1);
+    mask(S, t * kTileKeys);
     rs.raise(tile_max(S) * a.qmult);
-    const float ref = rs.safe_ref();
-    if (t + 1 < t1) {
-      rs.l += Tl::template values<true>(vbuf[par], S, a.qmult, ref, lane, rs.O, kbuf[par ^ 1], q,
-                                        next);
-      S[0] = next[0];
-      S[1] = next[1];
-    } else {
-      rs.l += Tl::template values<false>(vbuf[par], S, a.qmult, ref, lane, rs.O, kbuf[0], q, next);
-    }
+    rs.l += Tl::template values<true>(vbuf[par], S, a.qmult, rs.safe_ref(), lane, rs.O,
+                                      kbuf[par ^ 1], q, next);
+    S[0] = next[0];
+    S[1] = next[1];
     dma_wait();
     __syncthreads();
   }
-  if (any_odd) {  // uniform: what take_nonfinite() took, with its keys' scores taken again
+  if (t0 < t1) {
+    mask(S, (t1 - 1) * kTileKeys);
+    rs.raise(tile_max(S) * a.qmult);
+    rs.l += Tl::template values<false>(vbuf[(t1 - 1 - t0) & 1], S, a.qmult, rs.safe_ref(), lane,
+                                       rs.O, kbuf[0], q, next);
+  }
+  // Values that are no numbers, of keys that only some rows see, make NaNs of the other rows
+  // (0 times them).  Where a row's result is no number the workgroup starts again, takes such
+  // values out of the tiles and adds them in the rows that see their key: slowly, but it
+  // costs the other calls one look at the result.
+  if (block_all < seen) {
+    f4v z = {0.f, 0.f, 0.f, 0.f};  // 0 times a result that is no number is none
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) z[d] = fmaf(rs.O[d][i], 0.f, z[d]);
+    if (__syncthreads_or(live && !(z[0] + z[1] + z[2] + z[3] == 0.f))) {  // (also: the tiles' last reads are done)
+      begin();
 #pragma unroll 1
-    for (int t = max(t0, block_all / kTileKeys); t < t1; ++t) {
-      const int key0 = t * kTileKeys;
-      if (tid == 0) odd_keys = 0;
-      dma_tile(kbuf[0], kp + (int64_t)key0 * kD, keys - key0, from, wave);
-      dma_tile(vbuf[0], vp + (int64_t)key0 * kD, keys - key0, from, wave);
-      dma_wait();
-      __syncthreads();
-      const uint64_t mine = take_nonfinite<T>(vbuf[0], tid);
-      if (mine) atomicOr((unsigned long long*)&odd_keys, (unsigned long long)mine);
-      __syncthreads();
-      const uint64_t odd = odd_keys;
-      if (odd) {
-        f16v P[2];
-        Tl::template scores<false>(kbuf[0], q, lane, P);
+      for (int t = t0; t < t1; ++t) {
+        const int key0 = t * kTileKeys;
+        if (tid == 0) odd_keys = 0;
+        dma_tile(kbuf[0], kp + (int64_t)key0 * kD, keys - key0, from, wave);
+        dma_tile(vbuf[0], vp + (int64_t)key0 * kD, keys - key0, from, wave);
+        dma_wait();
+        __syncthreads();
+        const uint64_t mine = take_nonfinite<T>(vbuf[0], tid);
+        if (mine) atomicOr((unsigned long long*)&odd_keys, (unsigned long long)mine);
+        __syncthreads();
+        Tl::template scores<false>(kbuf[0], q, lane, S);
+        mask(S, key0);
+        rs.raise(tile_max(S) * a.qmult);
         const float ref = rs.safe_ref();
+        rs.l += Tl::template values<false>(vbuf[0], S, a.qmult, ref, lane, rs.O, kbuf[0], q, next);
+        if (const uint64_t odd = odd_keys) {
 #pragma unroll
-        for (int x = 0; x < 2; ++x)
+          for (int x = 0; x < 2; ++x)
 #pragma unroll
-          for (int i = 0; i < 16; ++i)
-            P[x][i] = __builtin_amdgcn_exp2f(fmaf(P[x][i], a.qmult, -ref));
-        add_nonfinite(odd, vp, key0, limit, P, lane, rs.O);
+            for (int i = 0; i < 16; ++i)
+              S[x][i] = __builtin_amdgcn_exp2f(fmaf(S[x][i], a.qmult, -ref));
+          add_nonfinite(odd, vp, key0, limit, S, lane, rs.O);
+        }
+        __syncthreads();
       }
-      __syncthreads();
     }
   }
   if (a.part) {
-    write_partial(a, rs, row, split, live, lane);
+    write_partial(a, rs, row, un.split, live, lane);
     return;
   }
   const float l = sum_halves(rs.l);

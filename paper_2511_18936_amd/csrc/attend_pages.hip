@@ -93,24 +93,22 @@ attend_pages_kernel(AttendLaunch a) {
   __shared__ __align__(1024) char vbuf[2][R::kTile];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int G = a.Hq / a.Hkv;
-  const int j = group_of(a, blockIdx.x);
-  int u = blockIdx.x - a.unit0[j];
-  const int h = u % a.Hkv;
-  u /= a.Hkv;
-  const int nsplit = a.nsplit[j], split = u % nsplit;
+  const int G = (int)a.by_g.d;
+  const Unit un = unit_at(a, blockIdx.x);
+  const int j = un.j, h = un.h;
   const int toks = a.toks[j], L = a.keys[j], cs = a.cseq[j];
-  const int64_t r = (int64_t)(u / nsplit) * kTileRows + 32 * wave + (lane & 31);
-  const int tok = (int)(r / G), g = (int)(r % G);
+  const uint32_t r = (uint32_t)un.tile * kTileRows + 32 * wave + (lane & 31);
+  const int tok = (int)a.by_g.of(r), g = (int)(r - (uint32_t)tok * (uint32_t)G);
   const bool live = tok < toks;
-  const bool busy = ((int64_t)(u / nsplit) * kTileRows + 32 * wave) / G < toks;  // some row is
+  const bool busy = (int)a.by_g.of(un.tile * kTileRows + 32 * wave) < toks;  // some row is live
   int b = 0, i = 0;
   if (live) token_at(a, j, tok, b, i);
   const int64_t row = ((int64_t)b * a.Hq + h * G + g) * a.n + i;
 
   const int S = L > a.bb ? L - a.bb : 0, np = pages_for(S), nb = L < a.bb ? L : a.bb;
   const int nt = np + (nb + kTileKeys - 1) / kTileKeys;
-  const int t0 = (int)((int64_t)nt * split / nsplit), t1 = (int)((int64_t)nt * (split + 1) / nsplit);
+  const int t0 = split_first(nt, un.split, un.nsplit);
+  const int t1 = split_first(nt, un.split + 1, un.nsplit);
   const int nk = kpad_of(a.kact[0][j]) / 8, nv = kpad_of(a.kact[1][j]) / 8;
   const int64_t kbytes = page_bytes_of(Fmt<T>::kValBytes, 8 * nk);
   const int64_t vbytes = page_bytes_of(Fmt<T>::kValBytes, 8 * nv);
@@ -210,7 +208,10 @@ attend_pages_kernel(AttendLaunch a) {
     scatter(t + 1, t + 1);
     stage(t + 2, t + 2);
     if (busy) {
+      // (products first, where the other workgroup's wave has exponentials to do)
+      __builtin_amdgcn_s_setprio(1);
       Tl::template scores<true>(kbuf[par], q, lane, Sc);
+      __builtin_amdgcn_s_setprio(0);
       const int count = t < np ? S - t * kPage : nb - (t - np) * kTileKeys;
       if (count < kTileKeys) {
 #pragma unroll
@@ -226,7 +227,7 @@ attend_pages_kernel(AttendLaunch a) {
     if (ring_tile) dma_wait();
     __syncthreads();
   }
-  write_partial(a, rs, row, split, live, lane);
+  write_partial(a, rs, row, un.split, live, lane);
 }
 
 template <typename T>

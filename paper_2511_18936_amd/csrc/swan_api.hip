@@ -447,7 +447,7 @@ struct AttendCost {
   double tile, start;
 };
 AttendCost attend_cost(int32_t dtype, bool pages) {
-  if (dtype == SWAN_F32) return {256, pages ? 16.0 : 12.0, 8.0};
+  if (dtype == SWAN_F32) return {256, pages ? 10.0 : 7.5, 8.0};
   return {512, pages ? 3.9 : 2.3, 6.0};
 }
 
@@ -471,7 +471,9 @@ int plan_tiles(const AttendCost& c, int groups, const int64_t* base, const int* 
   };
   auto cost = [&](int per) {
     const int64_t u = units(per);
-    const double waves = (double)((u + c.slots - 1) / c.slots);
+    // (causal: of a row tile's parts about half have keys to see)
+    const double full = uneven ? 0.6 * (double)u : (double)u;
+    const double waves = ceil(full / c.slots);
     const int parts = (longest + per - 1) / per;
     double run = waves * per;
     if (uneven || u > 4 * c.slots) {  // the GPU stays full until the last ones
@@ -487,7 +489,8 @@ int plan_tiles(const AttendCost& c, int groups, const int64_t* base, const int* 
   int best = longest;
   double least = cost(longest);
   const int64_t fills[] = {256, c.slots, 2 * c.slots, 3 * c.slots, 4 * c.slots, 6 * c.slots};
-  for (const int64_t fill : fills) {
+  for (const int64_t f : fills) {
+    const int64_t fill = uneven ? f * 5 / 3 : f;
     int lo = 1, hi = longest;  // the fewest tiles with at most `fill` workgroups
     while (lo < hi) {
       const int mid = (lo + hi) / 2;
@@ -616,6 +619,8 @@ int plan_pages(const swan_prefix* s, int32_t batch, int32_t n, const int32_t* n_
   }
   a.unit0[a.groups] = (int32_t)units;
   a.units = units > INT32_MAX ? -1 : (int)units;
+  a.by_g.set((uint32_t)G);
+  a.by_hkv.set((uint32_t)c->n_kv_heads);
   a.B = batch;
   a.Hq = c->n_q_heads;
   a.Hkv = c->n_kv_heads;
@@ -749,6 +754,8 @@ swan_status prompt_prep(int32_t dtype, int32_t batch, int32_t n_q_heads, int32_t
   }
   a.unit0[count] = (int32_t)units;
   a.units = (int)units;
+  a.by_g.set((uint32_t)G);
+  a.by_hkv.set((uint32_t)n_kv_heads);
   a.B = batch;
   a.Hq = n_q_heads;
   a.Hkv = n_kv_heads;

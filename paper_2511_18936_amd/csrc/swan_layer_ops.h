@@ -36,6 +36,23 @@ constexpr int kTileRows = 128;   // query rows of a workgroup, 32 per wave
 constexpr int kTileKeys = 64;    // keys of a tile (a page)
 constexpr int kMaxSlots = 256;   // splits of the keys of a group, per source
 
+// n / d for 32-bit n by a multiplication and shifts (Granlund and Montgomery, 1994)
+struct Divisor {
+  uint32_t mul, sh1, sh2, d;
+  void set(uint32_t by) {
+    d = by;
+    uint32_t l = 0;
+    while (l < 32 && (1ull << l) < by) ++l;
+    mul = (uint32_t)(((1ull << 32) * ((1ull << l) - by)) / by + 1);
+    sh1 = l < 1 ? l : 1;
+    sh2 = l < 1 ? 0 : l - 1;
+  }
+  __device__ __forceinline__ uint32_t of(uint32_t n) const {
+    const uint32_t t = __umulhi(mul, n);
+    return (t + ((n - t) >> sh1)) >> sh2;
+  }
+};
+
 struct AttendLaunch {
   const void* q;       // dense: rows of the storage type; pages: float32, rotated, x qmult
   const float* o0;     // dense: the state to continue from (or NULL), as o / lse below
@@ -52,6 +69,7 @@ struct AttendLaunch {
   int bb, npc;         // pages: buffer tokens; page capacity of a (sequence, head)
   int slots, slot0;    // partials of a row, and the first of this source
   int dtype, groups;
+  Divisor by_g, by_hkv;  // of the query heads per kv head; of the kv heads
   int units;           // kv heads x row tiles x splits of all groups
   int32_t unit0[SWAN_MAX_BATCH + 1];  // first unit of a group
   int32_t tok0[SWAN_MAX_BATCH + 1];   // first token of a list entry, from its group's first
