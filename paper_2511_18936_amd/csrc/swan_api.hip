@@ -222,6 +222,12 @@ size_t decode_ws_bytes(const swan_cache* c, int ns) {
   return round256(qhat) + part;
 }
 
+// whether two ranges of bytes share one
+bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
+  return a && b && a_bytes > 0 && b_bytes > 0 && (const char*)a < (const char*)b + b_bytes &&
+         (const char*)b < (const char*)a + a_bytes;
+}
+
 swan_status hip_status(hipError_t e, const char* what) {
   if (e == hipSuccess) return ok();
   return fail(SWAN_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
@@ -1164,12 +1170,12 @@ swan_status swan_qkv_rows(const void* qkv, int64_t seq_stride, int64_t row_strid
   }
   // the outputs and the rows read share no byte
   const int64_t es = elem_bytes(dtype), each = (int64_t)batch * n * SWAN_HEAD_DIM * es;
-  const char* lo[4] = {(const char*)qkv, (const char*)q, (const char*)k, (const char*)v};
+  const void* lo[4] = {qkv, q, k, v};
   const int64_t size[4] = {((batch - 1) * seq_stride + (n - 1) * row_stride + width) * es,
                            each * n_q_heads, each * n_kv_heads, each * n_kv_heads};
   for (int x = 0; x < 4; ++x)
     for (int y = x + 1; y < 4; ++y)
-      if (size[x] && size[y] && lo[x] < lo[y] + size[y] && lo[y] < lo[x] + size[x])
+      if (overlap(lo[x], size[x], lo[y], size[y]))
         return fail(SWAN_ERR_INVALID_ARG, "qkv, q, k and v overlap");
   a.stream = (hipStream_t)stream;
   return hip_status(swan::launch_qkv_rows(a), "qkv_rows launch");
@@ -1312,6 +1318,11 @@ swan_status swan_prompt_attention(const void* q, const void* k, const void* v, i
     if (((uintptr_t)workspace & 255) != 0)
       return fail(SWAN_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
   }
+  const int64_t es = elem_bytes(dtype), row = (int64_t)batch * SWAN_HEAD_DIM;
+  const int64_t q_bytes = row * n_q_heads * n * es, kv_bytes = row * n_kv_heads * m * es;
+  if (overlap(out, q_bytes, q, q_bytes) || overlap(out, q_bytes, k, kv_bytes) ||
+      overlap(out, q_bytes, v, kv_bytes) || overlap(out, q_bytes, o0, row * n_q_heads * n * 4))
+    return fail(SWAN_ERR_INVALID_ARG, "out overlaps q, k, v or the state");
   swan::AttendLaunch& a = pl.a;
   a.q = q;
   a.o0 = o0;

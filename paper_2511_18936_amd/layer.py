@@ -8,17 +8,22 @@ leaves it rotated, straight into W_O_hat (Lemma 2).
 
 One call with n new tokens per sequence, on the current stream:
   [q | k | v_hat] = x . [W_Q | W_K | W_V_hat]    one dense GEMM (torch: the GEMM library)
-  swan_rope on q and k at each sequence's next positions
+  swan_qkv_rows: heads split, q and k normalised per head where the layer has norm weights,
+  RoPE at each sequence's next positions
   a prompt (n > 1): swan_compress_append(k, v_hat, P_QK, P_VO = NULL)
   a decode step (n = 1): swan_decode_step(k, v_hat, q, P_QK, P_VO = NULL) -> o_hat
   (the append, then the attention, in one call), and
   y = o_hat . W_O_hat                             dense GEMM
-The SWAN steps run in libswan's kernels; attention over a prompt is the dense,
-standard kind and is not part of this layer (a prompt call only fills the cache).
+A prompt call fills the cache; with attend=True it also returns the rows' attention: the
+dense, causal kind over the rows themselves (swan_prompt_attention), continued from
+swan_attend over what is cached before them (pruned tokens as they are stored).  Sequences
+can stand behind a prefix that another layer's cache holds once for all of them (fork).
+The SWAN steps run in libswan's kernels.
 Weights are [in][out] row-major, x . W.
 """
 from __future__ import annotations
 
+import copy
 from typing import Optional, Sequence
 
 from . import swan
@@ -109,10 +114,11 @@ class SwanAttentionLayer:
     def __init__(self, W_q, W_k, W_v, W_o, P_qk, P_vo, n_heads: int, n_kv_heads: int,
                  rope_base: float, batch: int, buffer_tokens: int, capacity: int,
                  k_active: Sequence[int], k_value: Optional[Sequence[int]] = None,
-                 sparse_values: str = "same"):
+                 sparse_values: str = "same", q_norm=None, k_norm=None, norm_eps: float = 1e-6):
         """W_q [hidden][n_heads*128], W_k and W_v [hidden][n_kv*128], W_o
         [n_heads*128][hidden] (float16 or float32, cuda); P_qk, P_vo [n_kv][128][128]
-        float32 (swan_calibrate_rotation of post-RoPE keys and of values)."""
+        float32 (swan_calibrate_rotation of post-RoPE keys and of values).  q_norm, k_norm:
+        weights of the heads' norms before RoPE ([128], or [heads][128]; None: no norm)."""
         import torch
 
         d = HEAD_DIM
@@ -132,49 +138,80 @@ class SwanAttentionLayer:
         # the three projections as one GEMM: [W_Q | W_K | W_V_hat], [hidden][(n_q + 2 n_kv) 128]
         self.W_qkv = torch.cat([W_q, W_k, Wv.to(self.dtype)], dim=1).contiguous()
         self.W_o_hat = Wo.to(self.dtype).contiguous()
+        self.q_norm = None if q_norm is None else q_norm.contiguous()
+        self.k_norm = None if k_norm is None else k_norm.contiguous()
+        self.norm_eps = float(norm_eps)
         self.cache = swan.SwanCache(batch, n_heads, n_kv_heads, buffer_tokens, capacity,
                                     k_active, self.dtype, W_q.device,
                                     sparse_values=sparse_values, k_value=k_value)
 
+    prefix: Optional[swan.Prefix] = None
+    q_norm = k_norm = None
+    norm_eps = 1e-6
+
+    def fork(self, of: Sequence[int], buffer_tokens: int, capacity: int,
+             k_active: Sequence[int], k_value: Optional[Sequence[int]] = None,
+             sparse_values: str = "same") -> "SwanAttentionLayer":
+        """A layer with the same weights for len(of) new sequences, sequence b behind the
+        tokens of this layer's sequence of[b], which are held, and read, once: their positions
+        follow them and their attention includes them.  The new layer refers to this one's
+        cache, which should not grow meanwhile (positions would move)."""
+        if self.prefix is not None:
+            raise ValueError("this layer's sequences stand behind a prefix themselves")
+        of = [int(p) for p in of]
+        if any(not 0 <= p < self.cache.batch for p in of):
+            raise ValueError(f"of must be sequences of this layer, 0..{self.cache.batch - 1}")
+        new = copy.copy(self)
+        new.cache = swan.SwanCache(len(of), self.n_heads, self.n_kv_heads, buffer_tokens,
+                                   capacity, k_active, self.dtype, self.cache.device,
+                                   sparse_values=sparse_values, k_value=k_value)
+        new.prefix = swan.Prefix(self.cache, of)
+        return new
+
+    def positions(self):
+        """The position of each sequence's next token."""
+        if self.prefix is None:
+            return self.cache.seq_len
+        before = self.prefix.cache.seq_len
+        return [L + before[p] for L, p in zip(self.cache.seq_len, self.prefix.of)]
+
     def project(self, x):
         """Post-RoPE q [B][H_q][n][128], k and v_hat [B][H_kv][n][128] of new rows x
         [B][n][hidden] at each sequence's next positions."""
-        qkv = x @ self.W_qkv
-        nq, nkv = self.n_heads * HEAD_DIM, self.n_kv_heads * HEAD_DIM
-        return (self._rows(qkv[..., :nq], self.n_heads, True),
-                self._rows(qkv[..., nq:nq + nkv], self.n_kv_heads, True),
-                self._rows(qkv[..., nq + nkv:], self.n_kv_heads, False))
-
-    def _rows(self, t, heads: int, rope: bool):
-        """[B][n][heads 128] projections as [B][heads][n][128], rotated by RoPE at the
-        sequences' next positions."""
-        B, n, _ = t.shape
-        t = t.reshape(B, n, heads, HEAD_DIM).transpose(1, 2).contiguous()
-        if rope:
-            swan.rope(t, self.cache.seq_len, self.rope_base, out=t)
-        return t
+        return swan.qkv_rows(x @ self.W_qkv, self.n_heads, self.n_kv_heads, self.positions(),
+                             self.rope_base, self.q_norm, self.k_norm, self.norm_eps)
 
     def _prompt_rows(self, x):
-        """project(x) without the queries: a prompt's attention is not part of this layer,
-        and for 32 query and 8 KV heads its keys and values are a third of the projections.
+        """project(x) without the queries, for a prompt whose attention is not asked for:
+        for 32 query and 8 KV heads its keys and values are a third of the projections.
         Any other project() than this class's own is called as it is."""
         if getattr(self.project, "__func__", None) is not _OWN_PROJECT:
             return self.project(x)[1:]
-        nq, nkv = self.n_heads * HEAD_DIM, self.n_kv_heads * HEAD_DIM
-        kv = x @ self.W_qkv[:, nq:]
-        return (self._rows(kv[..., :nkv], self.n_kv_heads, True),
-                self._rows(kv[..., nkv:], self.n_kv_heads, False))
+        kv = x @ self.W_qkv[:, self.n_heads * HEAD_DIM:]
+        return swan.qkv_rows(kv, 0, self.n_kv_heads, self.positions(), self.rope_base, None,
+                             self.k_norm, self.norm_eps)[1:]
 
-    def __call__(self, x):
+    def __call__(self, x, attend: bool = False):
         """x [B][n][hidden]: append the n rows of every sequence to the cache; for a
-        decode step (n = 1) return y [B][hidden], the layer's attention output."""
-        if x.shape[1] != 1:
+        decode step (n = 1) return y [B][hidden], the layer's attention output.  For a
+        prompt or a chunk of one (n > 1) return None, or with attend=True y [B][n][hidden]:
+        each row over the tokens before the call as the caches hold them, and over the rows
+        up to itself."""
+        B, n = x.shape[0], x.shape[1]
+        if n != 1 and not attend:
             k, v = self._prompt_rows(x)
             self.cache.append(k, v, self.P_qk, None)
             return None
         q, k, v = self.project(x)
-        B = x.shape[0]
-        o_hat = self.cache.step(k, v, q[:, :, 0].contiguous(), self.P_qk, None)
+        if n != 1:
+            state = None
+            if self.prefix is not None or any(self.cache.seq_len):
+                state = self.cache.attend(q, self.P_qk, None, prefix=self.prefix)
+            o_hat = swan.prompt_attention(q, k, v, state=state)
+            self.cache.append(k, v, self.P_qk, None)
+            return o_hat.transpose(1, 2).reshape(B, n, self.n_heads * HEAD_DIM) @ self.W_o_hat
+        o_hat = self.cache.step(k, v, q[:, :, 0].contiguous(), self.P_qk, None,
+                                prefix=self.prefix)
         return o_hat.view(B, self.n_heads * HEAD_DIM) @ self.W_o_hat
 
 
