@@ -325,9 +325,11 @@ __device__ __forceinline__ Unit unit_at(const AttendLaunch& a, int block) {
   }
   return n;
 }
-// first of nt tiles of a split (nt at most 2^23, splits 2^8)
+// first of nt tiles of a split: nt / nsplit of them each, the first ones one more
 __device__ __forceinline__ int split_first(int nt, int split, int nsplit) {
-  return nsplit == 1 ? split * nt : (int)((uint32_t)nt * (uint32_t)split / (uint32_t)nsplit);
+  if (nsplit == 1) return split * nt;
+  const int each = nt / nsplit;
+  return each * split + min(split, nt - each * nsplit);
 }
 
 // sequence b and row i of it that token `tok` of group j is

@@ -12,8 +12,8 @@ template <typename T>
 __global__ __launch_bounds__(256) void rotate_rows_kernel(RotateLaunch a) {
   const int tid = threadIdx.x, lane = tid & 63, hi = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int bh = blockIdx.x, b = bh / a.H, rows = a.rows[b];
-  const int row0 = blockIdx.y * kTileRows;
+  const int bh = blockIdx.x % (a.B * a.H), b = bh / a.H, rows = a.rows[b];
+  const int row0 = blockIdx.x / (a.B * a.H) * kTileRows;
   if (row0 >= rows) return;
   const float* P = a.P + (int64_t)(bh % a.H / (a.H / a.Hkv)) * kD * kD;
   const int j = 32 * wave + (lane & 31);  // the dim of the result that this lane's M^T row is
@@ -71,7 +71,7 @@ __global__ __launch_bounds__(256) void rotate_rows_kernel(RotateLaunch a) {
 }
 
 hipError_t launch_rotate_rows(const RotateLaunch& a) {
-  const dim3 grid(a.B * a.H, (a.n + kTileRows - 1) / kTileRows);
+  const dim3 grid(a.B * a.H * ((a.n + kTileRows - 1) / kTileRows));  // at most B H n
   if (a.x_dtype == SWAN_F32)
     hipLaunchKernelGGL(rotate_rows_kernel<float>, grid, dim3(256), 0, a.stream, a);
   else

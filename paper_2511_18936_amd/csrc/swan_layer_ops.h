@@ -83,6 +83,7 @@ struct AttendLaunch {
   uint8_t kact[2][SWAN_MAX_BATCH];    // pages: k of the group's keys / values
   hipStream_t stream;
 };
+static_assert(sizeof(AttendLaunch) <= 4096, "passed to the kernels by value");
 hipError_t launch_attend_pages(const AttendLaunch& a);
 hipError_t launch_attend_dense(const AttendLaunch& a);
 
@@ -121,6 +122,7 @@ struct JoinLaunch {
   int32_t rows[SWAN_MAX_BATCH];
   hipStream_t stream;
 };
+static_assert(sizeof(JoinLaunch) <= 4096, "passed to the kernels by value");
 hipError_t launch_join(const JoinLaunch& a);
 
 }  // namespace swan

@@ -173,7 +173,8 @@ class SwanAttentionLayer:
         if self.prefix is None:
             return self.cache.seq_len
         before = self.prefix.cache.seq_len
-        return [L + before[p] for L, p in zip(self.cache.seq_len, self.prefix.of)]
+        of = self.prefix.of or [0] * self.cache.batch
+        return [L + (before[p] if p >= 0 else 0) for L, p in zip(self.cache.seq_len, of)]
 
     def project(self, x):
         """Post-RoPE q [B][H_q][n][128], k and v_hat [B][H_kv][n][128] of new rows x

@@ -473,6 +473,11 @@ def _made(how: str, shape, dtype, device, stream):
         return make(shape, dtype=dtype, device=device)
 
 
+def _made_like(t, shape, stream):
+    """t.new_empty(shape), on the stream that the call is enqueued on (see _made)."""
+    return t.new_empty(shape) if stream is None else _made("empty", shape, t.dtype, t.device, stream)
+
+
 def qkv_rows(qkv, n_q_heads: int, n_kv_heads: int, pos0: Sequence[int], base: float,
              q_weight=None, k_weight=None, eps: float = 1e-6, out=None, stream=None):
     """A layer's projections qkv [B][n][(n_q + 2 n_kv) * 128] (float16 or float32, cuda; rows
@@ -481,49 +486,63 @@ def qkv_rows(qkv, n_q_heads: int, n_kv_heads: int, pos0: Sequence[int], base: fl
     qkv's type or float32; None: no norm), then rotated to positions pos0[b] + i as by
     rope(); v as it is.  out = (q, k, v) writes existing tensors; n_q_heads = 0 gives
     (None, k, v)."""
-    import torch
-
     if qkv.dim() != 3:
         raise SwanError(SWAN_ERR_INVALID_ARG, "qkv must be [B][n][(n_q + 2 n_kv) * 128]")
-    code = _storage_code(qkv.dtype)
+    dtype = qkv.dtype
+    code = _storage_code(dtype)
     B, n, width = qkv.shape
     if width != (n_q_heads + 2 * n_kv_heads) * HEAD_DIM or n_q_heads < 0 or n_kv_heads < 0:
         raise SwanError(SWAN_ERR_INVALID_ARG,
                         f"rows of {width} elements for {n_q_heads} + 2 x {n_kv_heads} heads")
-    if qkv.stride(2) != 1 and width > 1:
+    seq, row, last = qkv.stride()
+    if last != 1 and width > 1:
         raise SwanError(SWAN_ERR_INVALID_ARG, "qkv's last dimension must be contiguous")
-    w32 = per_head = None
+    per_head = w32 = False
+    if q_weight is not None or k_weight is not None:
+        w32, per_head = _norm_weights(dtype, n_q_heads, n_kv_heads, q_weight, k_weight)
+    if not qkv.is_cuda:
+        raise SwanError(SWAN_ERR_INVALID_ARG, f"qkv is on {qkv.device}, not on a GPU")
+    if out is None:
+        q = k = v = None
+        if n_q_heads:
+            q = _made_like(qkv, (B, n_q_heads, n, HEAD_DIM), stream)
+        if n_kv_heads:
+            k = _made_like(qkv, (B, n_kv_heads, n, HEAD_DIM), stream)
+            v = _made_like(qkv, (B, n_kv_heads, n, HEAD_DIM), stream)
+        device = _same_gpu(qkv=qkv, q_weight=q_weight, k_weight=k_weight)
+    else:
+        q, k, v = out
+        for name, t, heads in (("q", q, n_q_heads), ("k", k, n_kv_heads), ("v", v, n_kv_heads)):
+            if heads:
+                _tensor(t, name, dtype, (B, heads, n, HEAD_DIM))
+        device = _same_gpu(qkv=qkv, q=q, k=k, v=v, q_weight=q_weight, k_weight=k_weight)
+    # (a dimension of one element has no stride of its own)
+    with _CallsOn(device, stream) as s:
+        _check(_lib.swan_qkv_rows(_ptr(qkv), seq if B > 1 else 0, row if n > 1 else width, code, B,
+                                  n_q_heads, n_kv_heads, n, HEAD_DIM,
+                                  _per_sequence(pos0, B, "pos0"), base, _ptr(q_weight),
+                                  _ptr(k_weight), per_head, w32, eps, _ptr(q), _ptr(k), _ptr(v),
+                                  s))
+    return q, k, v
+
+
+def _norm_weights(dtype, n_q_heads: int, n_kv_heads: int, q_weight, k_weight):
+    """(float32 weights, weights per head) of the norm weights given, checked."""
+    import torch
+
+    form = None
     for name, w, heads in (("q_weight", q_weight, n_q_heads), ("k_weight", k_weight, n_kv_heads)):
         if w is None:
             continue
-        if w.dtype not in (qkv.dtype, torch.float32):
+        if w.dtype != dtype and w.dtype != torch.float32:
             raise SwanError(SWAN_ERR_INVALID_ARG,
-                            f"{name} has dtype {w.dtype}, expected {qkv.dtype} or float32")
-        _tensor(w, name, w.dtype, (HEAD_DIM,) if w.dim() == 1 else (heads, HEAD_DIM))
-        form = (w.dtype == torch.float32, w.dim() == 2)
-        if w32 is not None and form != (w32, per_head):
+                            f"{name} has dtype {w.dtype}, expected {dtype} or float32")
+        two = w.dim() == 2
+        _tensor(w, name, w.dtype, (heads, HEAD_DIM) if two else (HEAD_DIM,))
+        if form is not None and form != (w.dtype == torch.float32, two):
             raise SwanError(SWAN_ERR_INVALID_ARG, "q_weight and k_weight differ in form")
-        w32, per_head = form
-    shapes = [(B, h, n, HEAD_DIM) for h in (n_q_heads, n_kv_heads, n_kv_heads)]
-    if out is None:
-        _same_gpu(qkv=qkv)
-        out = [_made("empty", s, qkv.dtype, qkv.device, stream) if s[1] else None
-               for s in shapes]
-    else:
-        for name, t, s in zip("qkv", out, shapes):
-            if s[1]:
-                _tensor(t, name, qkv.dtype, s)
-    q, k, v = out
-    device = _same_gpu(qkv=qkv, q=q, k=k, v=v, q_weight=q_weight, k_weight=k_weight)
-    # a dimension of one element has no stride of its own
-    row = qkv.stride(1) if n > 1 else width
-    seq = qkv.stride(0) if B > 1 else 0
-    with _CallsOn(device, stream) as s:
-        _check(_lib.swan_qkv_rows(_ptr(qkv), seq, row, code, B, n_q_heads, n_kv_heads, n, HEAD_DIM,
-                                  _per_sequence(pos0, B, "pos0"), float(base), _ptr(q_weight),
-                                  _ptr(k_weight), int(bool(per_head)), int(bool(w32)), float(eps),
-                                  _ptr(q), _ptr(k), _ptr(v), s))
-    return q, k, v
+        form = (w.dtype == torch.float32, two)
+    return form
 
 
 def prompt_attention(q, k, v, causal: bool = True, n: Optional[Sequence[int]] = None,
@@ -783,7 +802,9 @@ class SwanCache:
         self._ws = None
 
     def workspace(self, seq_len: Optional[Sequence[int]] = None, prefix: Optional[Prefix] = None):
-        """The decode workspace for these lengths (default: the present ones) and prefix."""
+        """The decode workspace for these lengths (default: the present ones) and prefix.  A
+        call behind a prefix that is being captured gets one of its graph's own, which other
+        graphs and later calls neither use nor free."""
         import torch
 
         lens = self.seq_len if seq_len is None else seq_len
@@ -791,6 +812,8 @@ class SwanCache:
             need = decode_workspace_bytes(self.desc, lens, self.k_active, self.k_value)
         else:
             need = prefix_workspace_bytes(prefix, self.desc, lens, self.k_active, self.k_value)
+            if torch.cuda.is_current_stream_capturing():
+                return torch.empty(need, dtype=torch.uint8, device=self.device)
         if self._ws is None or self._ws.numel() < need:
             self._ws = torch.empty(need, dtype=torch.uint8, device=self.device)
         return self._ws

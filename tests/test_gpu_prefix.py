@@ -128,6 +128,8 @@ DECODE = [  # hq, hkv, prefix lengths, of, own lengths, buffer of prefix, own, k
     (4, 4, [200], [0, 0, 0], [1, 0, 40], 16, 16, [24] * 3),
     (8, 2, [1000, 64], [0, 1, -1, 0, 1], [300, 0, 77, 128, 1], 64, 128, [64] * 5),
     (16, 2, [300], [0] * 9, [5] * 9, 0, 0, [40] * 9),
+    (16, 1, [90], [0, 0], [3, 30], 16, 16, [20, 20]),
+    (12, 1, [700], [0] * 40, [1] * 40, 32, 16, [128] * 40),
     (32, 8, [2049], [0] * 4, [70, 71, 72, 0], 128, 64, [32, 48, 64, 96]),
     (6, 2, [0, 129], [0, 1], [9, 0], 128, 8, [33, 51]),
     (4, 4, [500], [0, 0, -1], [200, 0, 150], 32, 32, [32, 64, 96]),
