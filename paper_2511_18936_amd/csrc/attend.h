@@ -332,17 +332,27 @@ __device__ __forceinline__ int split_first(int nt, int split, int nsplit) {
   return each * split + min(split, nt - each * nsplit);
 }
 
-// sequence b and row i of it that token `tok` of group j is
-__device__ __forceinline__ void token_at(const AttendLaunch& a, int j, int tok, int& b, int& i) {
-  int lo = a.first[j], hi = a.first[j + 1];
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (tok >= a.tok0[mid]) lo = mid;
-    else hi = mid;
+// The sequence and row that a group's tokens are.  Lane l holds list entry l, read once: a
+// search through the launch's table itself would be a chain of loads, each with the whole
+// latency of memory.
+struct Tokens {
+  int tok0, seq;
+  __device__ __forceinline__ Tokens(const AttendLaunch& a, int lane)
+      : tok0(a.tok0[lane]), seq(a.seq[lane]) {}
+  // token tok of group j: sequence b and row i of it (every lane of the wave asks)
+  __device__ __forceinline__ void at(const AttendLaunch& a, int j, int tok, int& b, int& i) const {
+    int lo = a.first[j], hi = a.first[j + 1];  // uniform
+    while (__any(hi - lo > 1)) {
+      const int mid = (lo + hi) >> 1;
+      const int first = __shfl(tok0, mid, 64);  // (by every lane: each is read from)
+      const bool up = hi - lo > 1 && tok >= first;
+      lo = up ? mid : lo;
+      hi = up ? hi : mid > lo ? mid : lo + 1;
+    }
+    b = __shfl(seq, lo, 64);
+    i = tok - __shfl(tok0, lo, 64);
   }
-  b = a.seq[lo];
-  i = tok - a.tok0[lo];
-}
+};
 
 // the row's partial: reference, sum, accumulator
 __device__ __forceinline__ void write_partial(const AttendLaunch& a, const RowState& st,

@@ -70,9 +70,13 @@ template <typename T>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kernel(AttendLaunch a) {
   using Tl = Tile<T>;
   using R = Rows<T>;
-  __shared__ __align__(1024) char kbuf[2][R::kTile];
-  __shared__ __align__(1024) char vbuf[2][R::kTile];
-  __shared__ uint64_t odd_keys;  // keys of a tile with values that are no numbers
+  // (one struct, so that the tiles begin at 0: dma_tile reaches the first 64 KiB)
+  __shared__ struct alignas(1024) {
+    char k[2][R::kTile], v[2][R::kTile];
+    uint64_t odd_keys;  // keys of a tile with values that are no numbers
+  } sh;
+  auto &kbuf = sh.k, &vbuf = sh.v;
+  uint64_t& odd_keys = sh.odd_keys;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int G = (int)a.by_g.d;

@@ -12,57 +12,31 @@
 
 namespace swan {
 
-// Groups of 8 entries of a page of keys and one of values, numbered keys first, go to the 4
-// waves round robin; a lane holds its token's 8 values and indices of each.
-template <typename T, int NU>
-struct PageStage {
+// A lane's token in groups of 8 entries of a page: values and indices
+template <typename T, int N>
+struct Groups {
   using E = typename Fmt<T>::Elem;
   static constexpr int CB = Fmt<T>::kChunkBytes;
   static constexpr int VCH = 8 * Fmt<T>::kValBytes / CB;
   using Chunk = typename std::conditional<CB == 16, u32x4, u32x2>::type;
-  Chunk val[NU][VCH];
-  u32x2 idx[NU];
+  Chunk val[N][VCH];
+  u32x2 idx[N];
 
-  // kpage / vpage: NULL for a tile that is no page
-  __device__ __forceinline__ void load(const char* kpage, const char* vpage, int nk, int nv,
-                                       int wave, int lane) {
+  // group g of a page of n8 groups, as x
+  __device__ __forceinline__ void load(int x, const char* page, int n8, int g, int lane) {
 #pragma unroll
-    for (int x = 0; x < NU; ++x) {
-      const int u = wave + 4 * x;  // uniform
-      const bool key = u < nk;
-      const char* page = key ? kpage : vpage;
-      if (u < nk + nv && page) {
-        const int g = key ? u : u - nk, n8 = key ? nk : nv;
-#pragma unroll
-        for (int c = 0; c < VCH; ++c)
-          val[x][c] = *(const Chunk*)(page + (g * VCH + c) * 64 * CB + lane * CB);
-        idx[x] = *(const u32x2*)(page + n8 * VCH * 64 * CB + g * 512 + lane * 8);
-      }
-    }
+    for (int c = 0; c < VCH; ++c)
+      val[x][c] = *(const Chunk*)(page + (g * VCH + c) * 64 * CB + lane * CB);
+    idx[x] = *(const u32x2*)(page + n8 * VCH * 64 * CB + g * 512 + lane * 8);
   }
 
-  // into the (zeroed) tiles; ktoken / vtoken: this lane has a token there
-  __device__ __forceinline__ void scatter(char* kb, char* vb, int nk, int nv, int wave, int lane,
-                                          bool ktoken, bool vtoken) const {
-    using R = Rows<E>;
-    constexpr int N = 16 / (int)sizeof(E);
-    SWAN_LDS E* krow = (SWAN_LDS E*)((SWAN_LDS char*)kb + lane * R::kBytes);
-    SWAN_LDS E* vrow = (SWAN_LDS E*)((SWAN_LDS char*)vb + lane * R::kBytes);
-    const int turn = R::turn(lane) * N;
+  // group x into the token's (zeroed) row, whose pieces are turned by `turn` elements
+  __device__ __forceinline__ void scatter(int x, SWAN_LDS E* row, int turn) const {
 #pragma unroll
-    for (int x = 0; x < NU; ++x) {
-      const int u = wave + 4 * x;
-      if (u < nk + nv) {
-        SWAN_LDS E* to = u < nk ? krow : vrow;
-        if (u < nk ? ktoken : vtoken) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            // (the mask keeps a damaged page's indices inside the row)
-            const int d = ((e < 4 ? idx[x].x : idx[x].y) >> (8 * (e & 3))) & 0x7F;
-            to[d ^ turn] = value(x, e);
-          }
-        }
-      }
+    for (int e = 0; e < 8; ++e) {
+      // (the mask keeps a damaged page's indices inside the row)
+      const int d = ((e < 4 ? idx[x].x : idx[x].y) >> (8 * (e & 3))) & 0x7F;
+      row[d ^ turn] = value(x, e);
     }
   }
 
@@ -81,30 +55,150 @@ struct PageStage {
   }
 };
 
+// The row of `lane`'s token in a tile, and how its pieces are turned
+template <typename E>
+__device__ __forceinline__ SWAN_LDS E* token_row(char* tile, int lane) {
+  return (SWAN_LDS E*)((SWAN_LDS char*)tile + lane * Rows<E>::kBytes);
+}
+template <typename E>
+__device__ __forceinline__ int token_turn(int lane) {
+  return Rows<E>::turn(lane) * (16 / (int)sizeof(E));
+}
+
+// The groups of a page of keys and one of values, numbered keys first, go to the 4 waves
+// round robin: up to NU each.
+template <typename T, int NU>
+struct PageStage {
+  using E = typename Fmt<T>::Elem;
+  Groups<T, NU> groups;
+
+  // kpage / vpage: NULL for a tile that is no page
+  __device__ __forceinline__ void load(const char* kpage, const char* vpage, int nk, int nv,
+                                       int wave, int lane) {
+#pragma unroll
+    for (int x = 0; x < NU; ++x) {
+      const int u = wave + 4 * x;  // uniform
+      const bool key = u < nk;
+      const char* page = key ? kpage : vpage;
+      if (u < nk + nv && page) groups.load(x, page, key ? nk : nv, key ? u : u - nk, lane);
+    }
+  }
+
+  // into the (zeroed) tiles; token: this lane has one
+  __device__ __forceinline__ void scatter(char* kb, char* vb, int nk, int nv, int wave, int lane,
+                                          bool token) const {
+    SWAN_LDS E* krow = token_row<E>(kb, lane);
+    SWAN_LDS E* vrow = token_row<E>(vb, lane);
+    const int turn = token_turn<E>(lane);
+#pragma unroll
+    for (int x = 0; x < NU; ++x) {
+      const int u = wave + 4 * x;
+      if (u < nk + nv && token) groups.scatter(x, u < nk ? krow : vrow, turn);
+    }
+  }
+};
+
+// What a row of queries with this largest magnitude is multiplied by before it is split into
+// binary16 parts, and c, what its scores then are: 2^(13 - exponent) and the inverse; 1 for a
+// row of zeros, infinities or NaNs.
+__device__ __forceinline__ float row_scale(float top, float& c) {
+  const int ex = (int)((__float_as_uint(top) >> 23) & 0xFF) - 127;
+  const int up = top > 0.f && ex < 128 ? 13 - (ex < -100 ? -100 : ex) : 0;
+  c = __builtin_ldexpf(1.f, -up);
+  return __builtin_ldexpf(1.f, up);
+}
+
+// This lane's half of its row's rotated queries, from float32 at qr (zeros unless `live`), and
+// what their scores are multiplied by
+template <typename E>
+__device__ __forceinline__ float row_queries(const float* qr, bool live, int lane,
+                                             typename Tile<E>::template Q<true>& q) {
+  float c = 1.f;
+  if constexpr (sizeof(E) == 4) {
+#pragma unroll
+    for (int s = 0; s < 16; ++s)
+      q.hi[s] = live ? *(const f4v*)(qr + 8 * s + 4 * (lane >> 5)) : f4v{0.f, 0.f, 0.f, 0.f};
+  } else {
+    float x[64], top = 0.f;
+#pragma unroll
+    for (int s = 0; s < 16; ++s) {
+      const f4v v = live ? *(const f4v*)(qr + 16 * (s >> 1) + 8 * (lane >> 5) + 4 * (s & 1))
+                         : f4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        x[4 * s + e] = v[e];
+        top = fmaxf(top, fabsf(v[e]));
+      }
+    }
+    const float f = row_scale(max_halves(top), c);
+#pragma unroll
+    for (int s = 0; s < 8; ++s)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float y = x[8 * s + e] * f;
+        const _Float16 hi = (_Float16)y;
+        q.hi[s][e] = hi;
+        q.lo[s][e] = (_Float16)(y - (float)hi);
+      }
+  }
+  return c;
+}
+
+// A wave's 32 query rows, and their products with a tile
+template <typename E>
+struct QueryRows {
+  using Tl = Tile<E>;
+  int64_t row;
+  bool live, busy;  // this lane's row, some row of the wave is one
+  float c;
+  typename Tl::template Q<true> q;
+  RowState rs;
+
+  __device__ __forceinline__ QueryRows(const AttendLaunch& a, const Unit& un, const Tokens& tokens,
+                                      int wave, int lane) {
+    const uint32_t r = (uint32_t)un.tile * kTileRows + 32 * wave + (lane & 31);
+    const int G = (int)a.by_g.d, toks = a.toks[un.j];
+    const int tok = (int)a.by_g.of(r), g = (int)(r - (uint32_t)tok * (uint32_t)G);
+    live = tok < toks;
+    busy = (int)a.by_g.of(un.tile * kTileRows + 32 * wave) < toks;
+    int b, i;
+    tokens.at(a, un.j, live ? tok : 0, b, i);
+    row = ((int64_t)b * a.Hq + un.h * G + g) * a.n + i;
+    c = row_queries<E>((const float*)a.q + row * kD, live, lane, q);
+    rs.clear();
+  }
+  // one tile, of `count` keys (more: all)
+  __device__ __forceinline__ void tile(const char* kb, const char* vb, int count, int lane) {
+    f16v S[2];
+    // (products first, where the other workgroup's wave has exponentials to do)
+    __builtin_amdgcn_s_setprio(1);
+    Tl::template scores<true>(kb, q, lane, S);
+    __builtin_amdgcn_s_setprio(0);
+    if (count < kTileKeys) {
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (key_of(x, e, lane) >= count) S[x][e] = -INFINITY;
+    }
+    rs.raise(tile_max(S) * c);
+    rs.l += Tl::template values<false>(vb, S, c, rs.safe_ref(), lane, rs.O, kb, q, S);
+  }
+};
+
 // Grid as in attend_dense_kernel.  A group's keys are its pages, then tiles of its ring
 // (in slot order: the sum has none).
 template <typename T, int NU>
 __global__ __launch_bounds__(256, sizeof(typename Fmt<T>::Elem) == 2 ? 2 : 1) void
 attend_pages_kernel(AttendLaunch a) {
   using E = typename Fmt<T>::Elem;
-  using Tl = Tile<E>;
   using R = Rows<E>;
-  __shared__ __align__(1024) char kbuf[2][R::kTile];
-  __shared__ __align__(1024) char vbuf[2][R::kTile];
+  __shared__ __align__(1024) char buf[4][R::kTile];  // keys, values, each of two tiles
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int G = (int)a.by_g.d;
+  const Tokens tokens(a, lane);
   const Unit un = unit_at(a, blockIdx.x);
-  const int j = un.j, h = un.h;
-  const int toks = a.toks[j], L = a.keys[j], cs = a.cseq[j];
-  const uint32_t r = (uint32_t)un.tile * kTileRows + 32 * wave + (lane & 31);
-  const int tok = (int)a.by_g.of(r), g = (int)(r - (uint32_t)tok * (uint32_t)G);
-  const bool live = tok < toks;
-  const bool busy = (int)a.by_g.of(un.tile * kTileRows + 32 * wave) < toks;  // some row is live
-  int b = 0, i = 0;
-  if (live) token_at(a, j, tok, b, i);
-  const int64_t row = ((int64_t)b * a.Hq + h * G + g) * a.n + i;
-
+  const int j = un.j, h = un.h, L = a.keys[j], cs = a.cseq[j];
   const int S = L > a.bb ? L - a.bb : 0, np = pages_for(S), nb = L < a.bb ? L : a.bb;
   const int nt = np + (nb + kTileKeys - 1) / kTileKeys;
   const int t0 = split_first(nt, un.split, un.nsplit);
@@ -118,116 +212,57 @@ attend_pages_kernel(AttendLaunch a) {
 
   const DmaFrom<E> from = dma_from<E>(wave, lane);
   PageStage<T, NU> st;
-  // stage(k, v): the loads of tile k's keys and of tile v's values, where they are pages
-  auto stage = [&](int k, int v) {
-    st.load(k < t1 && k < np ? kpages + k * kbytes : nullptr,
-            v < t1 && v < np ? vpages + v * vbytes : nullptr, nk, nv, wave, lane);
+  // stage: the loads of tile t, where it is a page
+  auto stage = [&](int t) {
+    const bool page = t < t1 && t < np;
+    st.load(page ? kpages + t * kbytes : nullptr, page ? vpages + t * vbytes : nullptr, nk, nv, wave,
+            lane);
   };
-  // clear(k, v): zeros where those tiles are pages, the ring's rows where they are not
-  auto clear = [&](int k, int v) {
-    const u32x4 zero = {0u, 0u, 0u, 0u};
-    bool ring_tile = false;
-    if (k < t1 && k < np) {
+  // clear: zeros where tile t is a page, the ring's rows (true: to be waited for) where not
+  auto clear = [&](int t) {
+    char* kb = buf[(t - t0) & 1];
+    char* vb = buf[2 + ((t - t0) & 1)];
+    if (t >= t1) return false;
+    if (t < np) {
+      const u32x4 zero = {0u, 0u, 0u, 0u};
 #pragma unroll
-      for (int x = 0; x < R::kTile / 4096; ++x)
-        ((u32x4*)kbuf[(k - t0) & 1])[tid + 256 * x] = zero;
-    } else if (k < t1) {
-      dma_tile(kbuf[(k - t0) & 1], (const E*)a.k_ring + ring + (int64_t)(k - np) * kTileKeys * kD,
-               nb - (k - np) * kTileKeys, from, wave);
-      ring_tile = true;
-    }
-    if (v < t1 && v < np) {
-#pragma unroll
-      for (int x = 0; x < R::kTile / 4096; ++x)
-        ((u32x4*)vbuf[(v - t0) & 1])[tid + 256 * x] = zero;
-    } else if (v < t1) {
-      dma_tile(vbuf[(v - t0) & 1], (const E*)a.v_ring + ring + (int64_t)(v - np) * kTileKeys * kD,
-               nb - (v - np) * kTileKeys, from, wave);
-      ring_tile = true;
-    }
-    return ring_tile;
-  };
-  // scatter(k, v): what stage(k, v) loaded
-  auto scatter = [&](int k, int v) {
-    st.scatter(kbuf[(k - t0) & 1], vbuf[(v - t0) & 1], nk, nv, wave, lane,
-               k < t1 && k * kPage + lane < S, v < t1 && v * kPage + lane < S);
-  };
-  stage(t0, t0);
-
-  // the row's queries
-  typename Tl::template Q<true> q;
-  float c = 1.f;
-  {
-    const float* qr = (const float*)a.q + row * kD;
-    if constexpr (sizeof(E) == 4) {
-#pragma unroll
-      for (int s = 0; s < 16; ++s)
-        q.hi[s] = live ? *(const f4v*)(qr + 8 * s + 4 * (lane >> 5)) : f4v{0.f, 0.f, 0.f, 0.f};
-    } else {
-      float x[64], top = 0.f;
-#pragma unroll
-      for (int s = 0; s < 16; ++s) {
-        const f4v v = live ? *(const f4v*)(qr + 16 * (s >> 1) + 8 * (lane >> 5) + 4 * (s & 1))
-                           : f4v{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          x[4 * s + e] = v[e];
-          top = fmaxf(top, fabsf(v[e]));
-        }
+      for (int x = 0; x < R::kTile / 4096; ++x) {
+        ((u32x4*)kb)[tid + 256 * x] = zero;
+        ((u32x4*)vb)[tid + 256 * x] = zero;
       }
-      top = max_halves(top);
-      // 2^(13 - exponent); a row of zeros, infinities or NaNs as it is
-      const int ex = (int)((__float_as_uint(top) >> 23) & 0xFF) - 127;
-      const int up = top > 0.f && ex < 128 ? 13 - (ex < -100 ? -100 : ex) : 0;
-      const float f = __builtin_ldexpf(1.f, up);
-      c = __builtin_ldexpf(1.f, -up);
-#pragma unroll
-      for (int s = 0; s < 8; ++s)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float y = x[8 * s + e] * f;
-          const _Float16 hi = (_Float16)y;
-          q.hi[s][e] = hi;
-          q.lo[s][e] = (_Float16)(y - (float)hi);
-        }
+      return false;
     }
-  }
-  RowState rs;
-  rs.clear();
-  f16v Sc[2];
-  bool ring_tile = clear(t0, t0);
+    const int first = (t - np) * kTileKeys;
+    dma_tile(kb, (const E*)a.k_ring + ring + (int64_t)first * kD, nb - first, from, wave);
+    dma_tile(vb, (const E*)a.v_ring + ring + (int64_t)first * kD, nb - first, from, wave);
+    return true;
+  };
+  // scatter: what stage(t) loaded
+  auto scatter = [&](int t) {
+    st.scatter(buf[(t - t0) & 1], buf[2 + ((t - t0) & 1)], nk, nv, wave, lane,
+               t < t1 && t * kPage + lane < S);
+  };
+  stage(t0);
+
+  QueryRows<E> rows(a, un, tokens, wave, lane);
+  bool ring_tile = clear(t0);
   __syncthreads();
-  scatter(t0, t0);
-  stage(t0 + 1, t0 + 1);
+  scatter(t0);
+  stage(t0 + 1);
   if (ring_tile) dma_wait();
   __syncthreads();
   for (int t = t0; t < t1; ++t) {
     const int par = (t - t0) & 1;
-    ring_tile = clear(t + 1, t + 1);
+    ring_tile = clear(t + 1);
     __syncthreads();
-    scatter(t + 1, t + 1);
-    stage(t + 2, t + 2);
-    if (busy) {
-      // (products first, where the other workgroup's wave has exponentials to do)
-      __builtin_amdgcn_s_setprio(1);
-      Tl::template scores<true>(kbuf[par], q, lane, Sc);
-      __builtin_amdgcn_s_setprio(0);
-      const int count = t < np ? S - t * kPage : nb - (t - np) * kTileKeys;
-      if (count < kTileKeys) {
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (key_of(x, e, lane) >= count) Sc[x][e] = -INFINITY;
-      }
-      rs.raise(tile_max(Sc) * c);
-      rs.l += Tl::template values<false>(vbuf[par], Sc, c, rs.safe_ref(), lane, rs.O, kbuf[0], q,
-                                         Sc);
-    }
+    scatter(t + 1);
+    stage(t + 2);
+    if (rows.busy)
+      rows.tile(buf[par], buf[2 + par], t < np ? S - t * kPage : nb - (t - np) * kTileKeys, lane);
     if (ring_tile) dma_wait();
     __syncthreads();
   }
-  write_partial(a, rs, row, un.split, live, lane);
+  write_partial(a, rows.rs, rows.row, un.split, rows.live, lane);
 }
 
 template <typename T>
@@ -239,9 +274,11 @@ static hipError_t launch_pages_t(const AttendLaunch& a) {
     most = n > most ? n : most;
   }
   if (most <= 16)
-    hipLaunchKernelGGL((attend_pages_kernel<T, 4>), dim3(a.units), dim3(256), 0, a.stream, a);
+    hipLaunchKernelGGL((attend_pages_kernel<T, 4>), dim3(a.units), dim3(256), 0,
+                       a.stream, a);
   else
-    hipLaunchKernelGGL((attend_pages_kernel<T, 8>), dim3(a.units), dim3(256), 0, a.stream, a);
+    hipLaunchKernelGGL((attend_pages_kernel<T, 8>), dim3(a.units), dim3(256), 0,
+                       a.stream, a);
   return hipGetLastError();
 }
 

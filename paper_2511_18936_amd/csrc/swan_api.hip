@@ -593,18 +593,18 @@ int plan_pages(const swan_prefix* s, int32_t batch, int32_t n, const int32_t* n_
       toks += nb;
     }
     if (!toks) continue;
-    a.first[j] = (uint8_t)e0;
+    a.first[j] = e0;
     a.toks[j] = (int32_t)toks;
     a.keys[j] = s->seq_len_host[p];
-    a.cseq[j] = (uint8_t)p;
+    a.cseq[j] = p;
     for (int r = 0; r < 2; ++r) {
       a.off[r][j] = tab.page_off[r][p];
-      a.kact[r][j] = (uint8_t)tab.kact[r][p];
+      a.kact[r][j] = tab.kact[r][p];
     }
     row_tiles[j] = (toks * G + swan::kTileRows - 1) / swan::kTileRows;
     ++a.groups;
   }
-  a.first[a.groups] = (uint8_t)entries;
+  a.first[a.groups] = entries;
   int tiles[SWAN_MAX_BATCH];
   int64_t base[SWAN_MAX_BATCH], rows = 0;
   for (int j = 0; j < a.groups; ++j) {
@@ -617,7 +617,7 @@ int plan_pages(const swan_prefix* s, int32_t batch, int32_t n, const int32_t* n_
   int64_t units = 0;
   for (int j = 0; j < a.groups; ++j) {
     const int ns = (tiles[j] + per - 1) / per;
-    a.nsplit[j] = (int16_t)ns;
+    a.nsplit[j] = ns;
     a.unit0[j] = (int32_t)units;
     units += row_tiles[j] * ns * c->n_kv_heads;
     for (int e = a.first[j]; e < a.first[j + 1]; ++e) used[a.seq[e]] = (int16_t)ns;
@@ -735,8 +735,9 @@ swan_status prompt_prep(int32_t dtype, int32_t batch, int32_t n_q_heads, int32_t
   int64_t base[SWAN_MAX_BATCH], rows = 0;
   for (int j = 0; j < count; ++j) {
     const int b = order[j];
-    a.first[j] = (uint8_t)j;
-    a.seq[j] = a.cseq[j] = (uint8_t)b;
+    a.first[j] = j;
+    a.seq[j] = (uint8_t)b;
+    a.cseq[j] = b;
     a.tok0[j] = 0;
     a.toks[j] = n_host ? n_host[b] : n;
     a.keys[j] = m_host ? m_host[b] : m;
@@ -744,14 +745,14 @@ swan_status prompt_prep(int32_t dtype, int32_t batch, int32_t n_q_heads, int32_t
     base[j] = ((int64_t)a.toks[j] * G + swan::kTileRows - 1) / swan::kTileRows * n_kv_heads;
     rows += (int64_t)a.toks[j] * n_q_heads;
   }
-  a.first[count] = (uint8_t)count;
+  a.first[count] = count;
   a.groups = count;
   const int per = plan_tiles(attend_cost(dtype, false), count, base, tiles, rows, causal != 0, false);
   int64_t units = 0;
   int most = 1;
   for (int j = 0; j < count; ++j) {
     const int ns = tiles[j] > per ? (tiles[j] + per - 1) / per : 1;
-    a.nsplit[j] = (int16_t)ns;
+    a.nsplit[j] = ns;
     a.unit0[j] = (int32_t)units;
     units += base[j] * ns;
     most = ns > most ? ns : most;

@@ -76,11 +76,12 @@ struct AttendLaunch {
   int32_t keys[SWAN_MAX_BATCH];       // keys of a group
   int32_t toks[SWAN_MAX_BATCH];       // tokens of a group
   int64_t off[2][SWAN_MAX_BATCH];     // pages: byte offset of the group's key / value pages
-  int16_t nsplit[SWAN_MAX_BATCH];     // splits of a group's keys
-  uint8_t first[SWAN_MAX_BATCH + 1];  // first list entry of a group
+  // (32-bit, as a scalar load takes them)
+  int32_t nsplit[SWAN_MAX_BATCH];     // splits of a group's keys
+  int32_t first[SWAN_MAX_BATCH + 1];  // first list entry of a group
+  int32_t cseq[SWAN_MAX_BATCH];       // pages: cache sequence of a group; dense: its sequence
+  int32_t kact[2][SWAN_MAX_BATCH];    // pages: k of the group's keys / values
   uint8_t seq[SWAN_MAX_BATCH];        // sequence of a list entry
-  uint8_t cseq[SWAN_MAX_BATCH];       // pages: cache sequence of a group; dense: its sequence
-  uint8_t kact[2][SWAN_MAX_BATCH];    // pages: k of the group's keys / values
   hipStream_t stream;
 };
 static_assert(sizeof(AttendLaunch) <= 4096, "passed to the kernels by value");

@@ -37,17 +37,23 @@ def softmax_rows(q, k, v, seen=None, state=None):
     return o, safe + torch.log(total)
 
 
-def bound(dtype, q, k, v, o, keys, out_dtype=None):
+def bound(dtype, q, k, v, o, keys, out_dtype=None, turned=False):
     """A bound on |kernel - o|, elementwise for o [rows][D]: the output's rounding; p's
     rounding, which moves weights that sum to one by a factor within 2 u each; a score's
     error, 2^-16 of |q| |k| / sqrt(D) (128 terms summed in float32, twice: the rotation's and
     the product's), in the exponent; the accumulation of `keys` terms in float32, which
-    counts in full for float32 storage and is far below p's rounding for binary16."""
-    biggest = v.double().abs().max().item() if v.numel() else 0.0
+    counts in full for float32 storage and is far below p's rounding for binary16.  The
+    weights' errors multiply the values: an element's are at most the largest |v|, and after
+    a rotation (turned) the largest norm of a row of v."""
     norm = lambda x: x.double().norm(dim=-1).max().item() if x.numel() else 0.0  # noqa: E731
+    biggest = v.double().abs().max().item() if v.numel() else 0.0
+    if turned:
+        biggest = norm(v)
     score = norm(q) * norm(k) / math.sqrt(D) * 2.0 ** -16
     u = HALF[dtype] if dtype == "f16" else 2.0 ** -22  # (float32: exp2 within 2 ulp)
     rel = 2 * u + 2 * score + (keys + 16) * 2.0 ** -24
+    if turned:  # and the turn's own sum of 128 products in float32
+        rel += 128 * 2.0 ** -24
     return HALF[out_dtype or dtype] * o.abs() + biggest * rel + 2.0 ** -24
 
 

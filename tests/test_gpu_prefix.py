@@ -80,9 +80,7 @@ def test_attend_is_the_formula(gpu_device, swan_mod, torch_mod, hq, hkv, buffer,
                 assert torch.all(got == 0) and torch.all(glse == -math.inf)
                 continue
             # p is rounded as the format says, the state is float32
-            tol = R.bound(dtype, rows_b, K, V, want, len(K), "f32")
-            if not absorbed:  # the turn back sums 128 errors times a unit vector's entries
-                tol = math.sqrt(D) * tol.max() + 0 * tol
+            tol = R.bound(dtype, rows_b, K, V, want, len(K), "f32", turned=not absorbed)
             R.close(got, want, tol, f"sequence {b}, head {h}")
             norms = rows_b.double().norm(dim=-1).max() * K.norm(dim=-1).max() / math.sqrt(D)
             err = 2.0 ** -16 * norms.item() + 2.0 ** -10 * (dtype == "f16") + 2.0 ** -17
@@ -118,8 +116,7 @@ def test_two_sources_and_the_chunk_itself(gpu_device, swan_mod, torch_mod, dtype
             want, _ = R.softmax_rows(rows, kb, vb, seen, (o, lse))
             tol = R.bound(dtype, rows, kb, vb, want, len(K) + used[b])
             if len(K):
-                part = R.bound(dtype, rows, K, V, o, len(K), "f32")
-                tol = tol + math.sqrt(D) * part.max()
+                tol = tol + R.bound(dtype, rows, K, V, o, len(K), "f32", turned=True)
             R.close(got[b, h, :used[b]], want, tol, f"sequence {b}, head {h}")
 
 
@@ -159,9 +156,7 @@ def test_decode_behind_a_prefix(gpu_device, swan_mod, torch_mod, hq, hkv, plen, 
             for h in range(hq):
                 rows = q[b, h][None]
                 want, _, K, V = _want(sources, rows, b, h, hq // hkv, P_qk, P_vo)
-                tol = R.bound(dtype, rows, K, V, want, len(K))
-                if not absorbed:
-                    tol = math.sqrt(D) * tol.max() + 0 * tol
+                tol = R.bound(dtype, rows, K, V, want, len(K), turned=not absorbed)
                 R.close(out[b, h][None], want, tol, f"sequence {b}, head {h}")
 
     check(out, q)
