@@ -93,13 +93,13 @@ __device__ __forceinline__ DmaFrom<T> dma_from(int wave, int lane) {
   }
   return f;
 }
-template <typename T>
+template <typename T, bool kAsync = sizeof(T) == 2>
 __device__ __forceinline__ void dma_tile(char* lds, const T* p, int rows, const DmaFrom<T>& from,
                                          int wave) {
   typedef int i4v __attribute__((ext_vector_type(4)));
   const uint64_t base = (uint64_t)p;
   rows = rows > kTileKeys ? kTileKeys : rows < 0 ? 0 : rows;
-  if constexpr (sizeof(T) == 4) {
+  if constexpr (!kAsync) {
     u32x4 r[DmaFrom<T>::N];
 #pragma unroll
     for (int x = 0; x < DmaFrom<T>::N; ++x)

@@ -65,9 +65,9 @@ __device__ __forceinline__ int token_turn(int lane) {
   return Rows<E>::turn(lane) * (16 / (int)sizeof(E));
 }
 
-// The groups of a page of keys and one of values, numbered keys first, go to the 4 waves
+// The groups of a page of keys and one of values, numbered keys first, go to the W waves
 // round robin: up to NU each.
-template <typename T, int NU>
+template <typename T, int NU, int W>
 struct PageStage {
   using E = typename Fmt<T>::Elem;
   Groups<T, NU> groups;
@@ -77,7 +77,7 @@ struct PageStage {
                                        int wave, int lane) {
 #pragma unroll
     for (int x = 0; x < NU; ++x) {
-      const int u = wave + 4 * x;  // uniform
+      const int u = wave + W * x;  // uniform
       const bool key = u < nk;
       const char* page = key ? kpage : vpage;
       if (u < nk + nv && page) groups.load(x, page, key ? nk : nv, key ? u : u - nk, lane);
@@ -92,7 +92,7 @@ struct PageStage {
     const int turn = token_turn<E>(lane);
 #pragma unroll
     for (int x = 0; x < NU; ++x) {
-      const int u = wave + 4 * x;
+      const int u = wave + W * x;
       if (u < nk + nv && token) groups.scatter(x, u < nk ? krow : vrow, turn);
     }
   }
@@ -145,7 +145,7 @@ __device__ __forceinline__ float row_queries(const float* qr, bool live, int lan
 }
 
 // A wave's 32 query rows, and their products with a tile
-template <typename E>
+template <typename E, int W>
 struct QueryRows {
   using Tl = Tile<E>;
   int64_t row;
@@ -156,11 +156,11 @@ struct QueryRows {
 
   __device__ __forceinline__ QueryRows(const AttendLaunch& a, const Unit& un, const Tokens& tokens,
                                       int wave, int lane) {
-    const uint32_t r = (uint32_t)un.tile * kTileRows + 32 * wave + (lane & 31);
+    const uint32_t r = (uint32_t)un.tile * (32 * W) + 32 * wave + (lane & 31);
     const int G = (int)a.by_g.d, toks = a.toks[un.j];
     const int tok = (int)a.by_g.of(r), g = (int)(r - (uint32_t)tok * (uint32_t)G);
     live = tok < toks;
-    busy = (int)a.by_g.of(un.tile * kTileRows + 32 * wave) < toks;
+    busy = (int)a.by_g.of(un.tile * (32 * W) + 32 * wave) < toks;
     int b, i;
     tokens.at(a, un.j, live ? tok : 0, b, i);
     row = ((int64_t)b * a.Hq + un.h * G + g) * a.n + i;
@@ -171,9 +171,7 @@ struct QueryRows {
   __device__ __forceinline__ void tile(const char* kb, const char* vb, int count, int lane) {
     f16v S[2];
     // (products first, where the other workgroup's wave has exponentials to do)
-    __builtin_amdgcn_s_setprio(1);
     Tl::template scores<true>(kb, q, lane, S);
-    __builtin_amdgcn_s_setprio(0);
     if (count < kTileKeys) {
 #pragma unroll
       for (int x = 0; x < 2; ++x)
@@ -188,12 +186,13 @@ struct QueryRows {
 
 // Grid as in attend_dense_kernel.  A group's keys are its pages, then tiles of its ring
 // (in slot order: the sum has none).
-template <typename T, int NU>
-__global__ __launch_bounds__(256, sizeof(typename Fmt<T>::Elem) == 2 ? 2 : 1) void
+template <typename T, int NU, int W>
+__global__ __launch_bounds__(64 * W, sizeof(typename Fmt<T>::Elem) == 2 ? 2 : 1) void
 attend_pages_kernel(AttendLaunch a) {
   using E = typename Fmt<T>::Elem;
   using R = Rows<E>;
-  __shared__ __align__(1024) char buf[4][R::kTile];  // keys, values, each of two tiles
+  constexpr int N = W == 8 ? 3 : 2;
+  __shared__ __align__(1024) char buf[2 * N][R::kTile];  // keys and values of N tiles
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const Tokens tokens(a, lane);
@@ -210,8 +209,8 @@ attend_pages_kernel(AttendLaunch a) {
   const char* vpages = (const char*)a.v + a.off[1][j] + (int64_t)h * a.npc * vbytes;
   const int64_t ring = ((int64_t)cs * a.Hkv + h) * a.bb * kD;
 
-  const DmaFrom<E> from = dma_from<E>(wave, lane);
-  PageStage<T, NU> st;
+  const DmaFrom<E> from = dma_from<E>(wave & 3, lane);
+  PageStage<T, NU, W> st;
   // stage: the loads of tile t, where it is a page
   auto stage = [&](int t) {
     const bool page = t < t1 && t < np;
@@ -219,48 +218,74 @@ attend_pages_kernel(AttendLaunch a) {
             lane);
   };
   // clear: zeros where tile t is a page, the ring's rows (true: to be waited for) where not
-  auto clear = [&](int t) {
-    char* kb = buf[(t - t0) & 1];
-    char* vb = buf[2 + ((t - t0) & 1)];
+  auto clear = [&](int t, int at) {
+    char* kb = buf[at];
+    char* vb = buf[N + at];
     if (t >= t1) return false;
     if (t < np) {
       const u32x4 zero = {0u, 0u, 0u, 0u};
 #pragma unroll
-      for (int x = 0; x < R::kTile / 4096; ++x) {
-        ((u32x4*)kb)[tid + 256 * x] = zero;
-        ((u32x4*)vb)[tid + 256 * x] = zero;
+      for (int x = 0; x < R::kTile / (1024 * W); ++x) {
+        ((u32x4*)kb)[tid + 64 * W * x] = zero;
+        ((u32x4*)vb)[tid + 64 * W * x] = zero;
       }
       return false;
     }
     const int first = (t - np) * kTileKeys;
-    dma_tile(kb, (const E*)a.k_ring + ring + (int64_t)first * kD, nb - first, from, wave);
-    dma_tile(vb, (const E*)a.v_ring + ring + (int64_t)first * kD, nb - first, from, wave);
-    return true;
+    constexpr bool kAsync = sizeof(E) == 2 && W == 4;
+    if (W == 4 || wave < 4)
+      dma_tile<E, kAsync>(kb, (const E*)a.k_ring + ring + (int64_t)first * kD, nb - first, from,
+                          wave & 3);
+    if (W == 4 || wave >= 4)
+      dma_tile<E, kAsync>(vb, (const E*)a.v_ring + ring + (int64_t)first * kD, nb - first, from,
+                          wave & 3);
+    return kAsync;
   };
   // scatter: what stage(t) loaded
-  auto scatter = [&](int t) {
-    st.scatter(buf[(t - t0) & 1], buf[2 + ((t - t0) & 1)], nk, nv, wave, lane,
-               t < t1 && t * kPage + lane < S);
+  auto scatter = [&](int t, int at) {
+    st.scatter(buf[at], buf[N + at], nk, nv, wave, lane, t < t1 && t * kPage + lane < S);
   };
+  auto count = [&](int t) { return t < np ? S - t * kPage : nb - (t - np) * kTileKeys; };
   stage(t0);
 
-  QueryRows<E> rows(a, un, tokens, wave, lane);
-  bool ring_tile = clear(t0);
+  QueryRows<E, W> rows(a, un, tokens, wave, lane);
+  bool ring_tile = clear(t0, 0);
+  if constexpr (W == 8) clear(t0 + 1, 1);
   __syncthreads();
-  scatter(t0);
+  scatter(t0, 0);
   stage(t0 + 1);
   if (ring_tile) dma_wait();
   __syncthreads();
-  for (int t = t0; t < t1; ++t) {
-    const int par = (t - t0) & 1;
-    ring_tile = clear(t + 1);
-    __syncthreads();
-    scatter(t + 1);
-    stage(t + 2);
-    if (rows.busy)
-      rows.tile(buf[par], buf[2 + par], t < np ? S - t * kPage : nb - (t - np) * kTileKeys, lane);
-    if (ring_tile) dma_wait();
-    __syncthreads();
+  if constexpr (W == 4) {
+    for (int t = t0; t < t1; ++t) {
+      const int par = (t - t0) & 1;
+      ring_tile = clear(t + 1, par ^ 1);
+      __syncthreads();
+      scatter(t + 1, par ^ 1);
+      stage(t + 2);
+      if (rows.busy) rows.tile(buf[par], buf[N + par], count(t), lane);
+      if (ring_tile) dma_wait();
+      __syncthreads();
+    }
+  } else {
+    const bool late = wave >= 4;
+    if (late) __builtin_amdgcn_s_setprio(1);
+    int x0 = 0, x1 = 1, x2 = 2;
+    auto prepare = [&](int t) {
+      scatter(t + 1, x1);
+      stage(t + 2);
+      clear(t + 2, x2);
+    };
+    for (int t = t0; t < t1; ++t) {
+      if (!late) prepare(t);
+      if (rows.busy) rows.tile(buf[x0], buf[N + x0], count(t), lane);
+      if (late) prepare(t);
+      __syncthreads();
+      const int x = x0;
+      x0 = x1;
+      x1 = x2;
+      x2 = x;
+    }
   }
   write_partial(a, rows.rs, rows.row, un.split, rows.live, lane);
 }
@@ -273,12 +298,19 @@ static hipError_t launch_pages_t(const AttendLaunch& a) {
     const int n = kpad_of(a.kact[0][j]) / 8 + kpad_of(a.kact[1][j]) / 8;
     most = n > most ? n : most;
   }
-  if (most <= 16)
-    hipLaunchKernelGGL((attend_pages_kernel<T, 4>), dim3(a.units), dim3(256), 0,
-                       a.stream, a);
-  else
-    hipLaunchKernelGGL((attend_pages_kernel<T, 8>), dim3(a.units), dim3(256), 0,
-                       a.stream, a);
+  const dim3 grid(a.units), four(256), eight(512);
+  if (a.tile_rows > kTileRows) {
+    if constexpr (sizeof(typename Fmt<T>::Elem) == 2) {
+      if (most <= 16)
+        hipLaunchKernelGGL((attend_pages_kernel<T, 2, 8>), grid, eight, 0, a.stream, a);
+      else
+        hipLaunchKernelGGL((attend_pages_kernel<T, 4, 8>), grid, eight, 0, a.stream, a);
+    }
+  } else if (most <= 16) {
+    hipLaunchKernelGGL((attend_pages_kernel<T, 4, 4>), grid, four, 0, a.stream, a);
+  } else {
+    hipLaunchKernelGGL((attend_pages_kernel<T, 8, 4>), grid, four, 0, a.stream, a);
+  }
   return hipGetLastError();
 }
 

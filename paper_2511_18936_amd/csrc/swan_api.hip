@@ -452,8 +452,9 @@ struct AttendCost {
   int slots;
   double tile, start;
 };
-AttendCost attend_cost(int32_t dtype, bool pages) {
+AttendCost attend_cost(int32_t dtype, bool pages, bool many = false) {
   if (dtype == SWAN_F32) return {256, pages ? 10.0 : 7.5, 8.0};
+  if (many) return {256, 2.7, 6.0};
   return {512, pages ? 3.9 : 2.3, 6.0};
 }
 
@@ -462,8 +463,9 @@ AttendCost attend_cost(int32_t dtype, bool pages) {
 // in all.  Plans that fill the GPU 1/2 (a workgroup alone on a CU takes its tiles in 0.65 of
 // the time), 1, 2, ... times are compared.  uneven: a row tile may have fewer tiles than the
 // others of its group (causal), so workgroups even out; join: also one part has to be joined.
+// least: the cost.
 int plan_tiles(const AttendCost& c, int groups, const int64_t* base, const int* tiles,
-               int64_t rows, bool uneven, bool join) {
+               int64_t rows, bool uneven, bool join, double& least) {
   int longest = 1;
   double total = 0;
   for (int j = 0; j < groups; ++j) {
@@ -493,7 +495,7 @@ int plan_tiles(const AttendCost& c, int groups, const int64_t* base, const int* 
     return t;
   };
   int best = longest;
-  double least = cost(longest);
+  least = cost(longest);
   const int64_t fills[] = {256, c.slots, 2 * c.slots, 3 * c.slots, 4 * c.slots, 6 * c.slots};
   for (const int64_t f : fills) {
     const int64_t fill = uneven ? f * 5 / 3 : f;
@@ -578,7 +580,7 @@ int plan_pages(const swan_prefix* s, int32_t batch, int32_t n, const int32_t* n_
   fill_layout(c, s->k_active_host, s->k_value_host, tab, bytes);
   a.groups = 0;
   int entries = 0;
-  int64_t row_tiles[SWAN_MAX_BATCH];
+  bool many = false;  // a group fills more than a tile of kTileRows
   for (int b = 0; b < batch; ++b) used[b] = 0;
   for (int p = 0; p < c->batch; ++p) {
     if (s->seq_len_host[p] == 0) continue;
@@ -601,25 +603,38 @@ int plan_pages(const swan_prefix* s, int32_t batch, int32_t n, const int32_t* n_
       a.off[r][j] = tab.page_off[r][p];
       a.kact[r][j] = tab.kact[r][p];
     }
-    row_tiles[j] = (toks * G + swan::kTileRows - 1) / swan::kTileRows;
+    many |= c->dtype != SWAN_F32 && toks * G > swan::kTileRows;
     ++a.groups;
   }
   a.first[a.groups] = entries;
   int tiles[SWAN_MAX_BATCH];
-  int64_t base[SWAN_MAX_BATCH], rows = 0;
+  int64_t base[SWAN_MAX_BATCH], wide[SWAN_MAX_BATCH], rows = 0;  // row tiles x kv heads
   for (int j = 0; j < a.groups; ++j) {
+    const int64_t r = (int64_t)a.toks[j] * G;
     tiles[j] = key_tiles(c, a.keys[j]);
-    base[j] = row_tiles[j] * c->n_kv_heads;
+    base[j] = (r + swan::kTileRows - 1) / swan::kTileRows * c->n_kv_heads;
+    wide[j] = (r + swan::kManyRows - 1) / swan::kManyRows * c->n_kv_heads;
     rows += (int64_t)a.toks[j] * c->n_q_heads;
   }
-  const int per = plan_tiles(attend_cost(c->dtype, true), a.groups, base, tiles, rows, false, true);
+  double cost, cost_many;
+  int per = plan_tiles(attend_cost(c->dtype, true), a.groups, base, tiles, rows, false, true, cost);
+  a.tile_rows = swan::kTileRows;
+  if (many) {
+    const int p = plan_tiles(attend_cost(c->dtype, true, true), a.groups, wide, tiles, rows, false,
+                             true, cost_many);
+    if (cost_many < cost) {
+      per = p;
+      a.tile_rows = swan::kManyRows;
+      memcpy(base, wide, sizeof(base));
+    }
+  }
   int most = 0;
   int64_t units = 0;
   for (int j = 0; j < a.groups; ++j) {
     const int ns = (tiles[j] + per - 1) / per;
     a.nsplit[j] = ns;
     a.unit0[j] = (int32_t)units;
-    units += row_tiles[j] * ns * c->n_kv_heads;
+    units += base[j] * ns;
     for (int e = a.first[j]; e < a.first[j + 1]; ++e) used[a.seq[e]] = (int16_t)ns;
     most = ns > most ? ns : most;
   }
@@ -747,7 +762,9 @@ swan_status prompt_prep(int32_t dtype, int32_t batch, int32_t n_q_heads, int32_t
   }
   a.first[count] = count;
   a.groups = count;
-  const int per = plan_tiles(attend_cost(dtype, false), count, base, tiles, rows, causal != 0, false);
+  double cost;
+  const int per = plan_tiles(attend_cost(dtype, false), count, base, tiles, rows, causal != 0, false,
+                             cost);
   int64_t units = 0;
   int most = 1;
   for (int j = 0; j < count; ++j) {

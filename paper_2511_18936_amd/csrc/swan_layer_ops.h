@@ -33,6 +33,7 @@ hipError_t launch_qkv_rows(const QkvRowsLaunch& a);
 // sequences one sequence after another.
 // ---------------------------------------------------------------------------
 constexpr int kTileRows = 128;   // query rows of a workgroup, 32 per wave
+constexpr int kManyRows = 256;   // of one over pages for many rows
 constexpr int kTileKeys = 64;    // keys of a tile (a page)
 constexpr int kMaxSlots = 256;   // splits of the keys of a group, per source
 
@@ -69,6 +70,7 @@ struct AttendLaunch {
   int bb, npc;         // pages: buffer tokens; page capacity of a (sequence, head)
   int slots, slot0;    // partials of a row, and the first of this source
   int dtype, groups;
+  int tile_rows;       // pages: query rows of a workgroup, kTileRows or kManyRows
   Divisor by_g, by_hkv;  // of the query heads per kv head; of the kv heads
   int units;           // kv heads x row tiles x splits of all groups
   int32_t unit0[SWAN_MAX_BATCH + 1];  // first unit of a group

@@ -88,6 +88,29 @@ def test_attend_is_the_formula(gpu_device, swan_mod, torch_mod, hq, hkv, buffer,
 
 
 @pytest.mark.parametrize("dtype,values", FORMATS)
+@pytest.mark.parametrize("k,k_value", [(48, 64), (100, 96)])
+def test_many_rows_of_a_sequence(gpu_device, swan_mod, torch_mod, k, k_value, dtype, values):
+    """Chunks that fill workgroups of 256 rows, the last ones partly; few and many components
+    per page, and buffers that are not whole tiles."""
+    torch = torch_mod
+    hq, hkv, lengths, of = 32, 8, [1100, 1001, 1150, 60], [0, 1, 2, 0, 2, 1, 3, 2]
+    used = [100, 99, 130, 100, 1, 65, 128, 97]
+    cache, P_qk, P_vo = R.filled_cache(swan_mod, gpu_device, lengths, hq, hkv, 60, [k] * 4, dtype,
+                                       4, values, [k_value] * 4)
+    q = _queries(torch, gpu_device, (8, hq, 130, D), dtype, 9)
+    o, lse = cache.attend(q, P_qk, P_vo, of=of, n=used)
+    for b in range(8):
+        for h in range(0, hq, 3):
+            rows = q[b, h, :used[b]]
+            want, wlse, K, V = _want([(cache, of)], rows, b, h, hq // hkv, P_qk, P_vo)
+            tol = R.bound(dtype, rows, K, V, want, len(K), "f32", turned=True)
+            R.close(o[b, h, :used[b]], want, tol, f"sequence {b}, head {h}")
+            norms = rows.double().norm(dim=-1).max() * K.norm(dim=-1).max() / math.sqrt(D)
+            err = 2.0 ** -16 * norms.item() + 2.0 ** -10 * (dtype == "f16") + 2.0 ** -17
+            R.close(lse[b, h, :used[b]], wlse, err + 0 * wlse, "lse")
+
+
+@pytest.mark.parametrize("dtype,values", FORMATS)
 def test_two_sources_and_the_chunk_itself(gpu_device, swan_mod, torch_mod, dtype, values):
     """A shared prefix, the sequences' own tokens, then the chunk's rows, causal: as the
     softmax over all of them; the prefix of another format of the same element type."""
