@@ -16,6 +16,11 @@
 // (2^kLag at most) uses the upper part of its range: p below 2^-14 of the largest would be
 // subnormal without it.  p is rounded to binary16 there (2^-11 relative, and the sum is
 // taken of the rounded values, so the weights still sum to one); everything else is float32.
+//
+// Why 32 rows a wave and 64 keys a tile: the accumulator (64 registers a lane), the queries
+// (32, or 64 in two parts) and the scores of a tile (32) fill the 256 registers that two
+// waves per SIMD leave each, so one wave's products run while the other takes exponentials;
+// the wider MFMA shape halves the operand reads of the 16 x 16 one; and 64 keys are a page.
 #pragma once
 
 #include "swan_device.h"

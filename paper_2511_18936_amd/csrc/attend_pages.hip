@@ -171,7 +171,9 @@ struct QueryRows {
   __device__ __forceinline__ void tile(const char* kb, const char* vb, int count, int lane) {
     f16v S[2];
     // (products first, where the other workgroup's wave has exponentials to do)
+    if constexpr (W == 4) __builtin_amdgcn_s_setprio(1);
     Tl::template scores<true>(kb, q, lane, S);
+    if constexpr (W == 4) __builtin_amdgcn_s_setprio(0);
     if (count < kTileKeys) {
 #pragma unroll
       for (int x = 0; x < 2; ++x)
@@ -186,6 +188,23 @@ struct QueryRows {
 
 // Grid as in attend_dense_kernel.  A group's keys are its pages, then tiles of its ring
 // (in slot order: the sum has none).
+//
+// W = 4: two workgroups of 128 rows share a CU, each with two tiles in LDS; a tile is
+// cleared, filled after a barrier while the one before is multiplied, and a second barrier
+// ends both.  W = 8, for many rows: one workgroup of 256, so a page is scattered once where
+// two did it, and a third tile saves a barrier: t + 2 is cleared and t + 1 filled beside the
+// products of t.  The second wave of each SIMD multiplies first and has priority, so that one
+// scatters while the other multiplies (measured: without the priority 4 % more).  The ring's
+// tiles pass through registers there, as the third is past what dma_tile reaches.
+//
+// Bound by a wave's chain per tile: of 6400 cycles for 256 rows MFMA works in 3070 (two
+// parts of q make 48 instructions of 32 cycles), the rest is scattering (1200), waiting for
+// its LDS reads and exponentials.  Measured, k = 64 of 128: 4 x 256 rows of 32 heads on 8 over
+// 4 x 8192 keys 229 us with the other kernels of the chunk (250 with W = 4); 8 x 100 rows
+// over 16384 shared keys, E4M3 values, 361 us; 32 tokens over 32768 keys 48 us, 2.1 TB/s of
+// pages; 4 tokens of 32 heads over 4095 keys 17 us, where workgroups start and load for
+// longer than they multiply.  Without the low part of q
+// 15 % less, but not the float32 queries' 22 bits.
 template <typename T, int NU, int W>
 __global__ __launch_bounds__(64 * W, sizeof(typename Fmt<T>::Elem) == 2 ? 2 : 1) void
 attend_pages_kernel(AttendLaunch a) {
@@ -292,7 +311,9 @@ attend_pages_kernel(AttendLaunch a) {
 
 template <typename T>
 static hipError_t launch_pages_t(const AttendLaunch& a) {
-  // registers for 4 or 8 groups a wave in flight: up to 128 components of both roles, or 256
+  // registers for the groups that a wave has in flight: those of up to 128 components in both
+  // roles, or of 256 (4 tokens of 32 heads over 4095 keys, k = 48: 35.7 us with room for 128
+  // components, 39.3 for 256)
   int most = 0;
   for (int j = 0; j < a.groups; ++j) {
     const int n = kpad_of(a.kact[0][j]) / 8 + kpad_of(a.kact[1][j]) / 8;

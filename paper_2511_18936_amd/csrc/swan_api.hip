@@ -447,21 +447,25 @@ swan_status step_prep(const swan_cache* c, const int32_t* seq_len_host,
 // attention of several rows per sequence, and of decode steps behind a prefix
 // ---------------------------------------------------------------------------
 // What a plan of the attend kernels costs, in microseconds as measured: a workgroup's
-// start, and a tile of 64 keys of a workgroup on a full GPU (`slots` workgroups).
+// start, a tile of 64 keys of a workgroup on a full GPU (`slots` workgroups), and what share
+// of that a tile of a workgroup alone on its CU takes.  Pages, binary16, with workgroups of
+// 128 rows (two on a CU) or of 256 (`many`): 2.7 against 2 x 1.65 us for a tile of 256 rows,
+// so the larger ones where rows fill them (4 x 256 rows over 4 x 8192 keys: 232 against 250
+// us), the smaller ones where not (4 tokens of 32 heads over 4095 keys: 36 against 43 us).
 struct AttendCost {
   int slots;
-  double tile, start;
+  double tile, start, alone;
 };
 AttendCost attend_cost(int32_t dtype, bool pages, bool many = false) {
-  if (dtype == SWAN_F32) return {256, pages ? 10.0 : 7.5, 8.0};
-  if (many) return {256, 2.7, 6.0};
-  return {512, pages ? 3.9 : 2.3, 6.0};
+  if (dtype == SWAN_F32) return {256, pages ? 10.0 : 7.5, 8.0, 1.0};
+  if (many) return {256, 2.7, 6.0, 1.0};
+  if (pages) return {512, 3.3, 6.0, 0.72};
+  return {512, 2.3, 6.0, 0.65};
 }
 
 // Tiles of keys per workgroup, so that the launch and the join of its partials are
 // shortest: tiles[j] of keys for base[j] row tiles (times kv heads) of group j, `rows` rows
-// in all.  Plans that fill the GPU 1/2 (a workgroup alone on a CU takes its tiles in 0.65 of
-// the time), 1, 2, ... times are compared.  uneven: a row tile may have fewer tiles than the
+// in all.  Plans that fill the GPU 1/2 (a workgroup alone on a CU), 1, 2, ... times are compared.  uneven: a row tile may have fewer tiles than the
 // others of its group (causal), so workgroups even out; join: also one part has to be joined.
 // least: the cost.
 int plan_tiles(const AttendCost& c, int groups, const int64_t* base, const int* tiles,
@@ -489,7 +493,7 @@ int plan_tiles(const AttendCost& c, int groups, const int64_t* base, const int* 
       run = even < run ? even : run;
     }
     if (run < per) run = per;
-    if (c.slots > 256 && u <= 256) run *= 0.65;
+    if (u <= 256) run *= c.alone;
     double t = waves * c.start + run * c.tile;
     if (join || parts > 1) t += 4.0 + (double)rows * parts * (2.0 * 528 / 4e6);
     return t;
