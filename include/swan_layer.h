@@ -87,7 +87,7 @@ typedef struct swan_prefix {
  *  q             [batch][n_q_heads][n][head_dim] of the caches' element type (post-RoPE);
  *  P_qk, P_vo, scale  as in swan_decode_attention (P_vo NULL: o stays rotated);
  *                a scale given is at least 2^-64;
- *  o, lse        the state (float32);
+ *  o, lse        the state (float32), apart from each other;
  *  workspace     as swan_attend_workspace_bytes says, 256-byte aligned.
  */
 swan_status swan_attend_workspace_bytes(const swan_prefix* sources, int32_t n_sources,

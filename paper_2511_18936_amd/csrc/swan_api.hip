@@ -1237,6 +1237,9 @@ swan_status swan_attend(const swan_prefix* sources, int32_t n_sources, int32_t b
   if (((uintptr_t)workspace & 255) != 0)
     return fail(SWAN_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
   const swan_cache* c = sources[0].cache;
+  const int64_t n_rows = (int64_t)batch * c->n_q_heads * n;
+  if (overlap(o, n_rows * SWAN_HEAD_DIM * 4, lse, n_rows * 4))
+    return fail(SWAN_ERR_INVALID_ARG, "o and lse overlap");
   float* qhat = (float*)workspace;
   float* part = (float*)((char*)workspace + pl.qhat);
   swan::RotateLaunch r;
@@ -1343,7 +1346,8 @@ swan_status swan_prompt_attention(const void* q, const void* k, const void* v, i
   const int64_t es = elem_bytes(dtype), row = (int64_t)batch * SWAN_HEAD_DIM;
   const int64_t q_bytes = row * n_q_heads * n * es, kv_bytes = row * n_kv_heads * m * es;
   if (overlap(out, q_bytes, q, q_bytes) || overlap(out, q_bytes, k, kv_bytes) ||
-      overlap(out, q_bytes, v, kv_bytes) || overlap(out, q_bytes, o0, row * n_q_heads * n * 4))
+      overlap(out, q_bytes, v, kv_bytes) || overlap(out, q_bytes, o0, row * n_q_heads * n * 4) ||
+      overlap(out, q_bytes, lse0, (int64_t)batch * n_q_heads * n * 4))
     return fail(SWAN_ERR_INVALID_ARG, "out overlaps q, k, v or the state");
   swan::AttendLaunch& a = pl.a;
   a.q = q;

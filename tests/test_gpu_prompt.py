@@ -164,6 +164,19 @@ def test_scale_and_repeatability(gpu_device, swan_mod, torch_mod):
         assert torch.equal(a, swan_mod.prompt_attention(q, k, v, scale=0.25))
 
 
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_a_row_has_its_bits_whatever_its_neighbours_are(gpu_device, swan_mod, torch_mod, dtype):
+    """Rows beside it that are much larger, no numbers, or infinite."""
+    torch = torch_mod
+    q, k, v = _inputs(torch, gpu_device, 1, 2, 1, 150, 300, dtype, 12)
+    want = swan_mod.prompt_attention(q, k, v)
+    for other in (60.0, math.nan, math.inf):
+        changed = q.clone()
+        changed[:, :, 1::2] = changed[:, :, 1::2] * other
+        got = swan_mod.prompt_attention(changed, k, v)
+        assert torch.equal(got[:, :, 0::2], want[:, :, 0::2]), other
+
+
 def test_on_another_stream_and_captured(gpu_device, swan_mod, torch_mod):
     """Single tokens (a workspace) and a prompt (none), captured in two graphs that are
     replayed in turn with eager calls between."""

@@ -96,6 +96,15 @@ def test_prompt_attention_refuses(kw, status):
     assert _prompt(**kw) == status and swan.last_error()
 
 
+@pytest.mark.parametrize("name", ["q", "k", "v", "o0", "lse0"])
+def test_prompt_attention_refuses_an_out_over_its_inputs(name):
+    """The last bytes of an input, 2 x 8 x 4 rows of q, 2 x 2 x 9 of k, or the state's."""
+    far = {x: FAKE + (i << 24) for i, x in enumerate(("q", "k", "v", "o0", "lse0"), 1)}
+    size = {"q": 64 * 256, "k": 36 * 256, "v": 36 * 256, "o0": 64 * 512, "lse0": 64 * 4}[name]
+    assert _prompt(**far, out=far[name] + size - 16) == INVALID
+    assert "overlaps" in swan.last_error()
+
+
 def test_no_rows_of_a_prompt_are_fine():
     none = dict(q=None, k=None, v=None, out=None)
     assert _prompt(n=0, **none) == swan.SWAN_OK
@@ -164,6 +173,11 @@ def test_attend_refuses_a_bad_source(kw, status):
 ])
 def test_attend_refuses(kw, status):
     assert _attend([_prefix()], **kw) == status and swan.last_error()
+
+
+def test_attend_refuses_a_state_over_itself():
+    assert _attend([_prefix()], o=FAKE, lse=FAKE + 3 * 8 * 4 * 512 - 4) == INVALID
+    assert "overlap" in swan.last_error()
 
 
 def test_attend_refuses_sources_that_differ():
