@@ -117,65 +117,81 @@ struct Parts {
   }
 };
 
-// Decode: a workgroup per row.  The weights of its parts once, in LDS; then a quarter of the
-// threads (32 lanes of 4 dims) adds up every fourth part, and the result is turned back.
-// 1024 rows of 67 parts 15 us (2.4 TB/s of parts), 128 rows of 18 6 us: latency, of
-// the parts' references, of their accumulators, of P_vo's rows.
+// Decode: a workgroup per row.  The weights of its parts once, in LDS; then each of the groups
+// of 32 threads (lanes of 4 dims) adds up its share of the parts, and the result is turned
+// back.  P_vo is read in whole rows, on their way while the parts are added; its products
+// are summed over a group's lanes through LDS (1024 rows: 4 us less than a row of P_vo per
+// thread, 18 less than exchanges between the lanes).  Twice the threads gain nothing.
 constexpr int kMaxJoin = kMaxSplits + 1 + 2 * kMaxSlots + 1;
+constexpr int kJoinGroups = 4;
+constexpr int kJoinThreads = 32 * kJoinGroups;
 template <typename T>
-__global__ __launch_bounds__(128) void join_decode_kernel(JoinLaunch a) {
+__global__ __launch_bounds__(kJoinThreads) void join_decode_kernel(JoinLaunch a) {
+  constexpr int NG = kJoinGroups, NT = kJoinThreads, NR = kD / NG;
   __shared__ float wts[kMaxJoin];
-  __shared__ f4v sums[4][kD / 4];
-  __shared__ float oh[kD];
-  __shared__ float red[4];
-  const int t = threadIdx.x, bh = blockIdx.x, b = bh / a.H;
+  __shared__ f4v sums[NG][kD / 4];
+  __shared__ __align__(16) float oh[kD];
+  __shared__ float red[2 * NG];
+  __shared__ float turn[kD][33];
+  const int t = threadIdx.x, g = t >> 5, lane = t & 31, bh = blockIdx.x, b = bh / a.H;
   const Parts ps(a, b, bh);
-  float mloc = -INFINITY;
-  for (int x = t; x < ps.n2; x += 128) mloc = fmaxf(mloc, ps.at(x)[0]);
-  mloc = wave_max(mloc);
-  if ((t & 63) == 0) red[t >> 6] = mloc;
+  float m = -INFINITY;
+  for (int x = t; x < ps.n2; x += NT) m = fmaxf(m, ps.at(x)[0]);
+  m = wave_max(m);
+  if (lane == 0) red[g] = m;
   __syncthreads();
-  const float m = fmaxf(red[0], red[1]);
-  float lloc = 0.f;
-  for (int x = t; x < ps.n2; x += 128) {
+#pragma unroll
+  for (int x = 0; x < NG; ++x) m = fmaxf(m, red[x]);
+  float l = 0.f;
+  for (int x = t; x < ps.n2; x += NT) {
     const float* part = ps.at(x);
     const float w = part[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(part[0] - m);
     wts[x] = w;
-    lloc += w * part[1];
+    l += w * part[1];
   }
-  lloc = wave_sum(lloc);
-  if ((t & 63) == 0) red[2 + (t >> 6)] = lloc;
+  l = wave_sum(l);
+  if (lane == 0) red[NG + g] = l;  // (both halves of a wave have its sum)
   __syncthreads();
-  const float l = red[2] + red[3];
+  l = 0.f;
+#pragma unroll
+  for (int x = 0; x < NG; x += 2) l += red[NG + x];
   f4v o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-  for (int x = t >> 5; x < ps.n2; x += 4) {
-    const f4v acc = *(const f4v*)(ps.at(x) + 4 + 4 * (t & 31));
+  for (int x = g; x < ps.n2; x += NG) {
+    const f4v acc = *(const f4v*)(ps.at(x) + 4 + 4 * lane);
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[e] = fmaf(wts[x], acc[e], o[e]);
   }
-  sums[t >> 5][t & 31] = o;
-  __syncthreads();
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  const float* s = (const float*)sums;
-  const float mine = ((s[t] + s[kD + t]) + (s[2 * kD + t] + s[3 * kD + t])) * inv;
-  if (!a.P_vo) {
-    ((T*)a.out)[(int64_t)bh * kD + t] = (T)mine;
-    return;
+  f4v P[NR];
+  if (a.P_vo) {
+    const float* p0 = a.P_vo + ((int64_t)(bh % a.H / (a.H / a.Hkv)) * kD + NR * g) * kD + 4 * lane;
+#pragma unroll
+    for (int i = 0; i < NR; ++i) P[i] = *(const f4v*)(p0 + i * kD);
   }
-  oh[t] = mine;
+  sums[g][lane] = o;
   __syncthreads();
-  const float4* P = (const float4*)(a.P_vo + ((int64_t)(bh % a.H / (a.H / a.Hkv)) * kD + t) * kD);
-  float r = 0.f;
-#pragma unroll 8
-  for (int j4 = 0; j4 < kD / 4; ++j4) {
-    const float4 p = P[j4];
-    r = fmaf(p.x, oh[4 * j4], r);
-    r = fmaf(p.y, oh[4 * j4 + 1], r);
-    r = fmaf(p.z, oh[4 * j4 + 2], r);
-    r = fmaf(p.w, oh[4 * j4 + 3], r);
+  if (t < kD) {
+    const float* s = (const float*)sums + t;
+    float mine = 0.f;
+#pragma unroll
+    for (int x = 0; x < NG; x += 2) mine += s[x * kD] + s[(x + 1) * kD];
+    mine *= l == 0.f ? 0.f : 1.f / l;
+    if (!a.P_vo) ((T*)a.out)[(int64_t)bh * kD + t] = (T)mine;
+    oh[t] = mine;
   }
-  ((T*)a.out)[(int64_t)bh * kD + t] = (T)r;
+  if (!a.P_vo) return;
+  __syncthreads();
+  const f4v o4 = *(const f4v*)(oh + 4 * lane);
+#pragma unroll
+  for (int i = 0; i < NR; ++i)
+    turn[NR * g + i][lane] =
+        fmaf(P[i].w, o4.w, fmaf(P[i].z, o4.z, fmaf(P[i].y, o4.y, P[i].x * o4.x)));
+  __syncthreads();
+  if (t >= kD) return;
+  float r[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < 32; ++i) r[i & 3] += turn[t][i];
+  ((T*)a.out)[(int64_t)bh * kD + t] = (T)((r[0] + r[1]) + (r[2] + r[3]));
 }
 
 // Many rows: half a wave per row, a lane 4 dims; 32 parts' weights at a time are the lanes'.
@@ -240,7 +256,8 @@ template <typename T>
 static hipError_t launch_join_t(const JoinLaunch& a) {
   const int64_t rows = (int64_t)a.B * a.H * a.n;
   if (a.own)
-    hipLaunchKernelGGL(join_decode_kernel<T>, dim3((unsigned)rows), dim3(128), 0, a.stream, a);
+    hipLaunchKernelGGL(join_decode_kernel<T>, dim3((unsigned)rows), dim3(kJoinThreads), 0, a.stream,
+                       a);
   else
     hipLaunchKernelGGL(join_rows_kernel<T>, dim3((unsigned)((rows + 7) / 8)), dim3(256), 0,
                        a.stream, a);
