@@ -70,8 +70,8 @@ __device__ __forceinline__ void add_nonfinite(uint64_t keys, const T* vp, int ke
 // Two workgroups of 64 KiB of LDS share a CU.  Tiles go to LDS without passing registers, keys
 // one tile ahead of values, and the scores of a tile are taken in steps between the
 // exponentials of the one before: MFMA bounds long prompts.  Measured, binary16: 32 query
-// heads on 8, 4096 causal rows 155 us, 888 TFLOP/s where a large matrix product reaches
-// 1200; 8 prompts of up to 1009 rows, 32 heads 58 us (448 TFLOP/s: short rows of tiles, 6 us
+// heads on 8, 4096 causal rows 153-161 us by machine, 855-900 TFLOP/s where a large matrix
+// product reaches 1200; 8 prompts of up to 1009 rows, 32 heads 58 us (448 TFLOP/s: short rows of tiles, 6 us
 // to start and end each).  Few rows split the keys until the GPU is full and are bound by
 // memory: single tokens of 16 heads over up to 1500 keys of 16 sequences 25 us, 4.2 TB/s,
 // and 4 us to join.  Float32 (no double use of a CU: its tiles take 128 KiB): 2 x 333 rows,

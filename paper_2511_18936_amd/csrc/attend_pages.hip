@@ -201,7 +201,7 @@ struct QueryRows {
 // parts of q make 48 instructions of 32 cycles), the rest is scattering (1200), waiting for
 // its LDS reads and exponentials.  Measured, k = 64 of 128: 4 x 256 rows of 32 heads on 8 over
 // 4 x 8192 keys 229 us with the other kernels of the chunk (250 with W = 4); 8 x 100 rows
-// over 16384 shared keys, E4M3 values, 361 us; 32 tokens over 32768 keys 48 us, 2.1 TB/s of
+// over 16384 shared keys, E4M3 values, 361 us; 32 tokens over 32768 keys 47 us, 2.1 TB/s of
 // pages; 4 tokens of 32 heads over 4095 keys 17 us, where workgroups start and load for
 // longer than they multiply.  Without the low part of q
 // 15 % less, but not the float32 queries' 22 bits.

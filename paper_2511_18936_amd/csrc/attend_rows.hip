@@ -121,7 +121,9 @@ struct Parts {
 // of 32 threads (lanes of 4 dims) adds up its share of the parts, and the result is turned
 // back.  P_vo is read in whole rows, on their way while the parts are added; its products
 // are summed over a group's lanes through LDS (1024 rows: 4 us less than a row of P_vo per
-// thread, 18 less than exchanges between the lanes).  Twice the threads gain nothing.
+// thread, 18 less than exchanges between the lanes).  Twice the threads gain nothing.  1024 rows of 67
+// parts 11 us (3.3 TB/s of parts), 128 rows of 18 4.7 us: the latencies of the parts'
+// references, of their accumulators, of P_vo, one after another.
 constexpr int kMaxJoin = kMaxSplits + 1 + 2 * kMaxSlots + 1;
 constexpr int kJoinGroups = 4;
 constexpr int kJoinThreads = 32 * kJoinGroups;
