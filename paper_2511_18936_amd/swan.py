@@ -801,19 +801,19 @@ class SwanCache:
         self.k_active, self.k_value = k_active, k_value
         self._ws = None
 
-    def workspace(self, seq_len: Optional[Sequence[int]] = None, prefix: Optional[Prefix] = None):
-        """The decode workspace for these lengths (default: the present ones) and prefix.  A
-        call behind a prefix that is being captured gets one of its graph's own, which other
-        graphs and later calls neither use nor free."""
+    def workspace(self, seq_len: Optional[Sequence[int]] = None, prefix: Optional[Prefix] = None,
+                  stream=None):
+        """The decode workspace for these lengths (default: the present ones): one for all
+        calls of this cache without a prefix, so they are made on one stream at a time.  A
+        call behind a prefix gets one of its own, of the caching allocator's memory for
+        `stream` (or, captured, for its graph)."""
         import torch
 
         lens = self.seq_len if seq_len is None else seq_len
-        if prefix is None:
-            need = decode_workspace_bytes(self.desc, lens, self.k_active, self.k_value)
-        else:
+        if prefix is not None:
             need = prefix_workspace_bytes(prefix, self.desc, lens, self.k_active, self.k_value)
-            if torch.cuda.is_current_stream_capturing():
-                return torch.empty(need, dtype=torch.uint8, device=self.device)
+            return _made("empty", (need,), "uint8", self.device, stream)
+        need = decode_workspace_bytes(self.desc, lens, self.k_active, self.k_value)
         if self._ws is None or self._ws.numel() < need:
             self._ws = torch.empty(need, dtype=torch.uint8, device=self.device)
         return self._ws
@@ -830,16 +830,14 @@ class SwanCache:
     def decode(self, q, P_qk, P_vo, out=None, scale: float = 0.0, stream=None,
                prefix: Optional[Prefix] = None):
         """Attention of q ([B][H_q][d]) over the cache, behind a prefix where one is given."""
-        import torch
-
         if out is None:
-            out = torch.empty_like(q)
+            out = _made_like(q, q.shape, stream)
         if prefix is None:
             decode_attention(self.desc, self.seq_len, self.k_active, q, P_qk, P_vo, out,
                              self.workspace(), scale, stream, self.k_value)
         else:
             decode_attention_prefix(prefix, self.desc, self.seq_len, self.k_active, q, P_qk, P_vo,
-                                    out, self.workspace(prefix=prefix), scale, stream,
+                                    out, self.workspace(None, prefix, stream), scale, stream,
                                     self.k_value)
         return out
 
@@ -848,12 +846,10 @@ class SwanCache:
         """One decode step (swan_decode_step): append k_new / v_new ([B][H_kv][1][d]),
         advance the lengths, and return the attention of q ([B][H_q][d]) over the cache,
         behind a prefix where one is given."""
-        import torch
-
         if out is None:
-            out = torch.empty_like(q)
+            out = _made_like(q, q.shape, stream)
         after = [L + 1 for L in self.seq_len]
-        ws = self.workspace(after, prefix)
+        ws = self.workspace(after, prefix, stream)
         if prefix is None:
             decode_step(self.desc, self.seq_len, self.k_active, k_new, v_new, q, P_qk, P_vo, out,
                         ws, scale, stream, self.k_value)

@@ -287,3 +287,26 @@ def test_streams_graphs_and_repeats(gpu_device, swan_mod, torch_mod):
         assert torch.equal(kept[0], own.decode(q, P_qk, P_vo, prefix=prefix)), turn
         for a, b in zip(kept[1:], own.attend(rows, P_qk, P_vo, prefix=prefix)):
             assert torch.equal(a, b), turn
+
+
+def test_calls_on_two_streams_at_once(gpu_device, swan_mod, torch_mod):
+    """Decode calls behind a prefix of one cache, enqueued on two streams without waiting:
+    each has a workspace of its own."""
+    torch = torch_mod
+    hq, hkv, B = 8, 2, 3
+    own, P_qk, P_vo = R.filled_cache(swan_mod, gpu_device, [300, 3, 50], hq, hkv, 16, [32, 64, 32],
+                                     "f16", 41)
+    past, _, _ = R.filled_cache(swan_mod, gpu_device, [4000], hq, hkv, 64, [48], "f16", 42,
+                                P=(P_qk, P_vo))
+    prefix = swan_mod.Prefix(past)
+    qs = [_queries(torch, gpu_device, (B, hq, D), "f16", 43 + i) for i in range(2)]
+    want = [own.decode(q, P_qk, P_vo, prefix=prefix) for q in qs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in qs]
+    got = [[], []]
+    for _ in range(20):
+        for i, s in enumerate(streams):
+            got[i].append(own.decode(qs[i], P_qk, P_vo, prefix=prefix, stream=s))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(g, want[i]) for g in got[i]), i
