@@ -310,3 +310,26 @@ def test_calls_on_two_streams_at_once(gpu_device, swan_mod, torch_mod):
     torch.cuda.synchronize()
     for i in range(2):
         assert all(torch.equal(g, want[i]) for g in got[i]), i
+
+
+def test_pages_beyond_32_bit_offsets(gpu_device, swan_mod, torch_mod):
+    """Arrays of 13 GB: the second sequence's pages lie beyond 6.4 GB of each."""
+    torch = torch_mod
+    hq, hkv = 16, 8
+    past, P_qk, P_vo = R.filled_cache(swan_mod, gpu_device, [70, 333], hq, hkv, 16, [128, 128], "f16",
+                                      51, spare=2 ** 21)
+    assert past.k_pages.numel() > 12 * 2 ** 30
+    own, _, _ = R.filled_cache(swan_mod, gpu_device, [90, 1], hq, hkv, 16, [40, 40], "f16", 52,
+                               P=(P_qk, P_vo))
+    of = [1, 0]
+    q = _queries(torch, gpu_device, (2, hq, 33, D), "f16", 53)
+    o, lse = past.attend(q, P_qk, P_vo, of=of)
+    out = own.decode(q[:, :, 0].contiguous(), P_qk, P_vo, prefix=swan_mod.Prefix(past, of))
+    for b in range(2):
+        for h in (0, 7, 15):
+            want, _, K, V = _want([(past, of)], q[b, h], b, h, 2, P_qk, P_vo)
+            tol = R.bound("f16", q[b, h], K, V, want, len(K), "f32", turned=True)
+            R.close(o[b, h], want, tol, f"rows {b} {h}")
+            want, _, K, V = _want([(past, of), (own, [0, 1])], q[b, h, :1], b, h, 2, P_qk, P_vo)
+            tol = R.bound("f16", q[b, h, :1], K, V, want, len(K), turned=True)
+            R.close(out[b, h][None], want, tol, f"decode {b} {h}")
