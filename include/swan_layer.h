@@ -58,8 +58,8 @@ swan_status swan_qkv_rows(const void* qkv, int64_t seq_stride, int64_t row_strid
  * [batch][n_q_heads][n]).  A row that has seen no key has o = 0 and lse = -infinity.  The
  * states of two sets of keys join to the state of both, so a chunk of a prompt attends
  * over the cached tokens first (swan_attend) and then over itself (swan_prompt_attention).
- * On the binary16 formats probabilities are rounded to binary16 before their product with
- * the values; sums, states and accumulators are float32 in every case.
+ * On the binary16 formats probabilities meet the values as two binary16 parts, within 2^-23
+ * of their float32 value; sums, states and accumulators are float32 in every case.
  * Rows past a sequence's n_host[b] are neither read nor written.
  */
 

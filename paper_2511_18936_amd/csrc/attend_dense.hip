@@ -69,13 +69,15 @@ __device__ __forceinline__ void add_nonfinite(uint64_t keys, const T* vp, int ke
 //
 // Two workgroups of 64 KiB of LDS share a CU.  Tiles go to LDS without passing registers, keys
 // one tile ahead of values, and the scores of a tile are taken in steps between the
-// exponentials of the one before: MFMA bounds long prompts.  Measured, binary16: 32 query
-// heads on 8, 4096 causal rows 153-161 us by machine, 855-900 TFLOP/s where a large matrix
-// product reaches 1200; 8 prompts of up to 1009 rows, 32 heads 58 us (448 TFLOP/s: short rows of tiles, 6 us
-// to start and end each).  Few rows split the keys until the GPU is full and are bound by
-// memory: single tokens of 16 heads over up to 1500 keys of 16 sequences 25 us, 4.2 TB/s,
-// and 4 us to join.  Float32 (no double use of a CU: its tiles take 128 KiB): 2 x 333 rows,
-// 8 heads on 2, 23 us and 6 to join, the latency of few workgroups.
+// exponentials of the one before: MFMA bounds long prompts, at three products of which p's
+// second part is one.  Measured, binary16: 32 query heads on 8, 4096 causal rows 213-222 us by
+// machine, 935-970 TFLOP/s of products done (a large matrix product reaches 1200); 8 prompts of
+// up to 1009 rows, 32 heads 69 us (short rows of tiles, 6 us to start and end each).  Few rows
+// split the keys until the GPU is full and are bound by memory: single tokens of 16 heads over
+// up to 1500 keys of 16 sequences 25 us, 4.2 TB/s, and 4 us to join; the waves without a row
+// leave LDS to the others (28.6 us with the join; 34.7 if they multiply too).  Float32 (no
+// double use of a CU: its tiles take 128 KiB): 2 x 333 rows, 8 heads on 2, 23 us and 6 to join,
+// the latency of few workgroups.
 //
 // The last tile stands behind the loop, without scores to take ahead: as a condition inside
 // the loop it made registers spill.
@@ -102,6 +104,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kern
   const uint32_t r = row0 + 32 * wave + (lane & 31);
   const int tok = (int)a.by_g.of(r), g = (int)(r - (uint32_t)tok * (uint32_t)G);
   const bool live = tok < toks;
+  const bool busy = (int)a.by_g.of(row0 + 32 * wave) < toks;  // some row of the wave is one
   const int64_t row = ((int64_t)b * a.Hq + h * G + g) * a.n + tok;
   // Causal: row i sees the keys up to i + shift.  limit: those this lane's row sees; all_see,
   // block_all: that every row of the wave, of the workgroup sees; seen: that some row does.
@@ -178,38 +181,36 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kern
   f16v S[2], next[2];
   dma_wait();
   __syncthreads();
-  if (t0 < t1) Tl::template scores<false>(kbuf[0], q, lane, S);
+  if (busy && t0 < t1) Tl::template scores<false>(kbuf[0], q, lane, S);
   __syncthreads();
   for (int t = t0; t < t1 - 1; ++t) {
     const int par = (t - t0) & 1;
     load_k(t + 2);
     load_v(t + 1);
-    mask(S, t * kTileKeys);
-    rs.raise(tile_max(S) * a.qmult);
-    rs.l += Tl::template values<true>(vbuf[par], S, a.qmult, rs.safe_ref(), lane, rs.O,
-                                      kbuf[par ^ 1], q, next);
-    S[0] = next[0];
-    S[1] = next[1];
+    if (busy) {
+      mask(S, t * kTileKeys);
+      rs.raise(tile_max(S) * a.qmult);
+      rs.l += Tl::template values<true, false>(vbuf[par], S, a.qmult, rs.safe_ref(), lane, rs.O,
+                                               kbuf[par ^ 1], q, next);
+      S[0] = next[0];
+      S[1] = next[1];
+    }
     dma_wait();
     __syncthreads();
   }
-  if (t0 < t1) {
+  if (busy && t0 < t1) {
     mask(S, (t1 - 1) * kTileKeys);
     rs.raise(tile_max(S) * a.qmult);
-    rs.l += Tl::template values<false>(vbuf[(t1 - 1 - t0) & 1], S, a.qmult, rs.safe_ref(), lane,
+    rs.l += Tl::template values<false, false>(vbuf[(t1 - 1 - t0) & 1], S, a.qmult, rs.safe_ref(), lane,
                                        rs.O, kbuf[0], q, next);
   }
   // Values that are no numbers, of keys that only some rows see, make NaNs of the other rows
-  // (0 times them).  Where a row's result is no number the workgroup starts again, takes such
+  // (0 times them), and infinite ones of any key in binary16, where the parts of p may be 0 or
+  // of both signs.  Where a row's result is no number the workgroup starts again, takes such
   // values out of the tiles and adds them in the rows that see their key: slowly, but it
   // costs the other calls one look at the result.
-  if (block_all < seen) {
-    f4v z = {0.f, 0.f, 0.f, 0.f};  // 0 times a result that is no number is none
-#pragma unroll
-    for (int d = 0; d < 4; ++d)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) z[d] = fmaf(rs.O[d][i], 0.f, z[d]);
-    if (__syncthreads_or(live && !(z[0] + z[1] + z[2] + z[3] == 0.f))) {  // (also: the tiles' last reads are done)
+  if (sizeof(T) == 2 || block_all < seen) {
+    if (__syncthreads_or(live && rs.odd())) {  // (also: the tiles' last reads are done)
       begin();
 #pragma unroll 1
       for (int t = t0; t < t1; ++t) {
@@ -226,7 +227,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kern
         mask(S, key0);
         rs.raise(tile_max(S) * a.qmult);
         const float ref = rs.safe_ref();
-        rs.l += Tl::template values<false>(vbuf[0], S, a.qmult, ref, lane, rs.O, kbuf[0], q, next);
+        rs.l += Tl::template values<false, false>(vbuf[0], S, a.qmult, ref, lane, rs.O, kbuf[0], q, next);
         if (const uint64_t odd = odd_keys) {
 #pragma unroll
           for (int x = 0; x < 2; ++x)

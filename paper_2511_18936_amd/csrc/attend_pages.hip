@@ -167,7 +167,8 @@ struct QueryRows {
     c = row_queries<E>((const float*)a.q + row * kD, live, lane, q);
     rs.clear();
   }
-  // one tile, of `count` keys (more: all)
+  // one tile, of `count` keys (more: all); kOdd: with infinite values, as in Tile::values
+  template <bool kOdd>
   __device__ __forceinline__ void tile(const char* kb, const char* vb, int count, int lane) {
     f16v S[2];
     // (products first, where the other workgroup's wave has exponentials to do)
@@ -182,7 +183,7 @@ struct QueryRows {
           if (key_of(x, e, lane) >= count) S[x][e] = -INFINITY;
     }
     rs.raise(tile_max(S) * c);
-    rs.l += Tl::template values<false>(vb, S, c, rs.safe_ref(), lane, rs.O, kb, q, S);
+    rs.l += Tl::template values<false, kOdd>(vb, S, c, rs.safe_ref(), lane, rs.O, kb, q, S);
   }
 };
 
@@ -197,21 +198,24 @@ struct QueryRows {
 // scatters while the other multiplies (measured: without the priority 4 % more).  The ring's
 // tiles pass through registers there, as the third is past what dma_tile reaches.
 //
-// Bound by a wave's chain per tile: of 6400 cycles for 256 rows MFMA works in 3070 (two
-// parts of q make 48 instructions of 32 cycles), the rest is scattering (1200), waiting for
-// its LDS reads and exponentials.  Measured, k = 64 of 128: 4 x 256 rows of 32 heads on 8 over
-// 4 x 8192 keys 229 us with the other kernels of the chunk (250 with W = 4); 8 x 100 rows
-// over 16384 shared keys, E4M3 values, 361 us; 32 tokens over 32768 keys 47 us, 2.1 TB/s of
-// pages; 4 tokens of 32 heads over 4095 keys 17 us, where workgroups start and load for
-// longer than they multiply.  Without the low part of q
-// 15 % less, but not the float32 queries' 22 bits.
+// Bound by a wave's chain per tile: MFMA (two parts of q and of p make 64 instructions of 32
+// cycles for 32 rows), and the scattering, its LDS reads and the exponentials beside it.
+// Measured, k = 64 of 128: 4 x 256 rows of 32 heads on 8 over 4 x 8192 keys 277 us with the
+// other kernels of the chunk; 8 x 100 rows over 16384 shared keys, E4M3 values, 450 us; 32
+// tokens over 32768 keys 93 us and 4 tokens of 32 heads over 4095 keys 36 us with the own
+// tokens' and the other kernels.
 template <typename T, int NU, int W>
 __global__ __launch_bounds__(64 * W, sizeof(typename Fmt<T>::Elem) == 2 ? 2 : 1) void
 attend_pages_kernel(AttendLaunch a) {
   using E = typename Fmt<T>::Elem;
   using R = Rows<E>;
   constexpr int N = W == 8 ? 3 : 2;
-  __shared__ __align__(1024) char buf[2 * N][R::kTile];  // keys and values of N tiles
+  // (one struct, so that the tiles begin at 0: dma_tile reaches the first 64 KiB)
+  __shared__ struct alignas(1024) {
+    char buf[2 * N][R::kTile];  // keys and values of N tiles
+    int odd;                    // some row's sum is no number
+  } sh;
+  auto& buf = sh.buf;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const Tokens tokens(a, lane);
@@ -268,42 +272,59 @@ attend_pages_kernel(AttendLaunch a) {
   stage(t0);
 
   QueryRows<E, W> rows(a, un, tokens, wave, lane);
-  bool ring_tile = clear(t0, 0);
-  if constexpr (W == 8) clear(t0 + 1, 1);
-  __syncthreads();
-  scatter(t0, 0);
-  stage(t0 + 1);
-  if (ring_tile) dma_wait();
-  __syncthreads();
-  if constexpr (W == 4) {
-    for (int t = t0; t < t1; ++t) {
-      const int par = (t - t0) & 1;
-      ring_tile = clear(t + 1, par ^ 1);
-      __syncthreads();
-      scatter(t + 1, par ^ 1);
-      stage(t + 2);
-      if (rows.busy) rows.tile(buf[par], buf[N + par], count(t), lane);
-      if (ring_tile) dma_wait();
-      __syncthreads();
+  if (tid == 0) sh.odd = 0;
+  // all tiles, of which the first is staged
+  auto attend = [&](auto odd) {
+    constexpr bool kOdd = decltype(odd)::value;
+    bool ring_tile = clear(t0, 0);
+    if constexpr (W == 8) clear(t0 + 1, 1);
+    __syncthreads();
+    scatter(t0, 0);
+    stage(t0 + 1);
+    if (ring_tile) dma_wait();
+    __syncthreads();
+    if constexpr (W == 4) {
+      for (int t = t0; t < t1; ++t) {
+        const int par = (t - t0) & 1;
+        ring_tile = clear(t + 1, par ^ 1);
+        __syncthreads();
+        scatter(t + 1, par ^ 1);
+        stage(t + 2);
+        if (rows.busy) rows.template tile<kOdd>(buf[par], buf[N + par], count(t), lane);
+        if (ring_tile) dma_wait();
+        __syncthreads();
+      }
+    } else {
+      const bool late = wave >= 4;
+      if (late) __builtin_amdgcn_s_setprio(1);
+      int x0 = 0, x1 = 1, x2 = 2;
+      auto prepare = [&](int t) {
+        scatter(t + 1, x1);
+        stage(t + 2);
+        clear(t + 2, x2);
+      };
+      for (int t = t0; t < t1; ++t) {
+        if (!late) prepare(t);
+        if (rows.busy) rows.template tile<kOdd>(buf[x0], buf[N + x0], count(t), lane);
+        if (late) prepare(t);
+        __syncthreads();
+        const int x = x0;
+        x0 = x1;
+        x1 = x2;
+        x2 = x;
+      }
     }
-  } else {
-    const bool late = wave >= 4;
-    if (late) __builtin_amdgcn_s_setprio(1);
-    int x0 = 0, x1 = 1, x2 = 2;
-    auto prepare = [&](int t) {
-      scatter(t + 1, x1);
-      stage(t + 2);
-      clear(t + 2, x2);
-    };
-    for (int t = t0; t < t1; ++t) {
-      if (!late) prepare(t);
-      if (rows.busy) rows.tile(buf[x0], buf[N + x0], count(t), lane);
-      if (late) prepare(t);
-      __syncthreads();
-      const int x = x0;
-      x0 = x1;
-      x1 = x2;
-      x2 = x;
+  };
+  attend(std::false_type());
+  if constexpr (sizeof(E) == 2) {
+    // An infinite value's products with the parts of p may have made NaNs: once more, with
+    // care.  (The barrier is also behind the tiles' last reads.)
+    if (rows.live && rows.rs.odd()) sh.odd = 1;
+    __syncthreads();
+    if (sh.odd) {
+      rows.rs.clear();
+      stage(t0);
+      attend(std::true_type());
     }
   }
   write_partial(a, rows.rs, rows.row, un.split, rows.live, lane);
