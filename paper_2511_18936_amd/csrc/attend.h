@@ -286,6 +286,7 @@ struct RowState {
   // kLag (of no other row: a row's bits do not depend on its neighbours'); mx: the
   // maximum of the row's scores x c
   __device__ __forceinline__ void raise(float mx) {
+#pragma clang fp contract(off)
     const bool up = mx - ref > kLag;
     if (__any(up)) {
       const float to = up ? mx - kHead : ref;
@@ -317,6 +318,31 @@ __device__ __forceinline__ float tile_max(const f16v (&S)[2]) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) m = fmaxf(m, S[t][i]);
   return max_halves(m);
+}
+
+// Raises the reference for the scores S x c of a tile, of which values() takes S c - ref: c and
+// ref as it needs them.  It rounds the difference once, the reference is made of rounded
+// products; from 2^28 on these are further apart than kHead, so where they pass kFar S itself
+// becomes the difference of the rounded product (a power of two as c has none to round).
+constexpr float kFar = 0x1p20f;
+__device__ __forceinline__ float take_scores(RowState& rs, f16v (&S)[2], float& c) {
+#pragma clang fp contract(off)
+  const float mx = tile_max(S) * c;
+  rs.raise(mx);
+  float ref = rs.safe_ref();
+  const bool far = fabsf(mx) > kFar && mx != -INFINITY;  // (of this row alone)
+  if (__any(far)) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float x = S[t][i] * c;
+        S[t][i] = far ? x - ref : S[t][i];
+      }
+    c = far ? 1.f : c;
+    ref = far ? 0.f : ref;
+  }
+  return ref;
 }
 
 // A unit: kv head, split and row tile (in grid order) of group j

@@ -152,12 +152,14 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kern
   // last reads.
   //
   auto begin = [&]() {  // the state to continue from, or none
+#pragma clang fp contract(off)
     rs.clear();
     if (!a.o0 || !live || a.part) return;
     const float lse = a.lse0[row] * kLog2e;
     if (lse == -INFINITY) return;
     rs.ref = lse - kHead;
-    rs.l = lane < 32 ? 128.f : 0.f;  // 2^kHead
+    const float w = __builtin_amdgcn_exp2f(lse - rs.ref);  // (2^kHead but for a rounded ref)
+    rs.l = lane < 32 ? w : 0.f;
     const float* o = a.o0 + row * kD + 4 * (lane >> 5);
 #pragma unroll
     for (int d = 0; d < 4; ++d)
@@ -165,7 +167,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kern
       for (int i = 0; i < 4; ++i) {
         const f4v x = *(const f4v*)(o + 32 * d + 8 * i);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) rs.O[d][4 * i + e] = x[e] * 128.f;
+        for (int e = 0; e < 4; ++e) rs.O[d][4 * i + e] = x[e] * w;
       }
   };
   auto mask = [&](f16v (&S)[2], int key0) {
@@ -189,9 +191,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kern
     load_v(t + 1);
     if (busy) {
       mask(S, t * kTileKeys);
-      rs.raise(tile_max(S) * a.qmult);
-      rs.l += Tl::template values<true, false>(vbuf[par], S, a.qmult, rs.safe_ref(), lane, rs.O,
-                                               kbuf[par ^ 1], q, next);
+      float c = a.qmult;
+      const float ref = take_scores(rs, S, c);
+      rs.l += Tl::template values<true, false>(vbuf[par], S, c, ref, lane, rs.O, kbuf[par ^ 1], q,
+                                               next);
       S[0] = next[0];
       S[1] = next[1];
     }
@@ -200,9 +203,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kern
   }
   if (busy && t0 < t1) {
     mask(S, (t1 - 1) * kTileKeys);
-    rs.raise(tile_max(S) * a.qmult);
-    rs.l += Tl::template values<false, false>(vbuf[(t1 - 1 - t0) & 1], S, a.qmult, rs.safe_ref(), lane,
-                                       rs.O, kbuf[0], q, next);
+    float c = a.qmult;
+    const float ref = take_scores(rs, S, c);
+    rs.l += Tl::template values<false, false>(vbuf[(t1 - 1 - t0) & 1], S, c, ref, lane, rs.O,
+                                              kbuf[0], q, next);
   }
   // Values that are no numbers, of keys that only some rows see, make NaNs of the other rows
   // (0 times them), and infinite ones of any key in binary16, where the parts of p may be 0 or
@@ -225,15 +229,15 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kern
         __syncthreads();
         Tl::template scores<false>(kbuf[0], q, lane, S);
         mask(S, key0);
-        rs.raise(tile_max(S) * a.qmult);
-        const float ref = rs.safe_ref();
-        rs.l += Tl::template values<false, false>(vbuf[0], S, a.qmult, ref, lane, rs.O, kbuf[0], q, next);
+        float c = a.qmult;
+        const float ref = take_scores(rs, S, c);
+        rs.l += Tl::template values<false, false>(vbuf[0], S, c, ref, lane, rs.O, kbuf[0], q, next);
         if (const uint64_t odd = odd_keys) {
 #pragma unroll
           for (int x = 0; x < 2; ++x)
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-              S[x][i] = __builtin_amdgcn_exp2f(fmaf(S[x][i], a.qmult, -ref));
+              S[x][i] = __builtin_amdgcn_exp2f(fmaf(S[x][i], c, -ref));
           add_nonfinite(odd, vp, key0, limit, S, lane, rs.O);
         }
         __syncthreads();

@@ -113,6 +113,7 @@ struct Parts {
     return part + (x < n1 ? base0 + x : base1 + x) * kPartFloats;
   }
   __device__ __forceinline__ float m_of(int x) const {  // x < total
+#pragma clang fp contract(off)  // (rounded, as the maximum of all that it is compared with)
     return x < n2 ? at(x)[0] : *lse0 * kLog2e;
   }
 };
