@@ -12,13 +12,15 @@
 // exchange with lane +- 32, its sum one at the end.
 //
 // The reference `ref` lags behind the maximum: it moves when a score exceeds it by more
-// than kLag, and is set kHead below the maximum.  On the 16-bit path p goes to the second
-// product as two binary16 parts, p rounded and what that left: within 2^-23 of p (and 2^-25
-// absolutely, where a row's largest p is 2^kHead at least and none is above 2^kLag).  So the
-// weights are float32's but for a bit, and the sum is taken of the float32 p.  One part alone
-// leaves an error of up to 2^-11 in each weight, as much as the rounding of a binary16 result,
-// for less time (32 query heads on 8, 4096 causal rows: 161 us against 220; 4 x 256 rows over
-// 4 x 8192 cached keys 230 against 277; 32 tokens behind 32768 keys 86 against 93).
+// than Lag::kBy, and is set Lag::kHead below the maximum.  Binary16: by more than 15, then 7
+// below, so p (2^15 at most, below 65504) uses the upper part of its type's range.  It goes to
+// the second product as two parts, p rounded and what that left: within 2^-23 of p (and 2^-25
+// absolutely, where a row's largest p is 2^7 at least).  So the weights are float32's but for a
+// bit, and the sum is taken of the float32 p.  One part alone leaves an error of up to 2^-11 in
+// each weight, as much as the rounding of a binary16 result, for less time (32 query heads on
+// 8, 4096 causal rows: 161 us against 217; 4 x 256 rows over 4 x 8192 cached keys 230 against
+// 277; 32 tokens behind 32768 keys 86 against 93).  Float32: whenever a score exceeds it, then
+// 15 above the score, so p is 1 at most and the sums reach no further than the values do.
 //
 // Why 32 rows a wave and 64 keys a tile: the accumulator (64 registers a lane), the queries
 // (32, or 64 in two parts) and the scores of a tile (32) fill the 256 registers that two
@@ -37,8 +39,10 @@ typedef _Float16 h8v __attribute__((ext_vector_type(8)));
 typedef float f4v __attribute__((ext_vector_type(4)));
 typedef float f16v __attribute__((ext_vector_type(16)));
 
-constexpr float kHead = 7.f;
-constexpr float kLag = 15.f;  // 2^15 < 65504
+template <typename T>
+struct Lag {
+  static constexpr float kHead = sizeof(T) == 2 ? 7.f : -15.f, kBy = sizeof(T) == 2 ? 15.f : 0.f;
+};
 constexpr float kLog2e = 1.4426950408889634f;
 
 // v of this lane and of lane +- 32: {the lower half's, the upper half's}
@@ -270,6 +274,7 @@ __device__ __forceinline__ int key_of(int t, int i, int lane) {
 }
 
 // A wave's running softmax: a lane's row, dims 32 d + 8 (i / 4) + 4 (lane / 32) + i % 4
+template <typename T>
 struct RowState {
   float ref;  // log2 units; -inf: no key yet
   float l;    // this lane's half of the sum
@@ -283,13 +288,13 @@ struct RowState {
       for (int i = 0; i < 16; ++i) O[d][i] = 0.f;
   }
   // moves the reference of the rows in which a score of this tile exceeds it by more than
-  // kLag (of no other row: a row's bits do not depend on its neighbours'); mx: the
+  // Lag::kBy (of no other row: a row's bits do not depend on its neighbours'); mx: the
   // maximum of the row's scores x c
   __device__ __forceinline__ void raise(float mx) {
 #pragma clang fp contract(off)
-    const bool up = mx - ref > kLag;
+    const bool up = mx - ref > Lag<T>::kBy;
     if (__any(up)) {
-      const float to = up ? mx - kHead : ref;
+      const float to = up ? mx - Lag<T>::kHead : ref;
       const float f = up ? __builtin_amdgcn_exp2f(ref - to) : 1.f;
       ref = to;
       l *= f;
@@ -322,10 +327,11 @@ __device__ __forceinline__ float tile_max(const f16v (&S)[2]) {
 
 // Raises the reference for the scores S x c of a tile, of which values() takes S c - ref: c and
 // ref as it needs them.  It rounds the difference once, the reference is made of rounded
-// products; from 2^28 on these are further apart than kHead, so where they pass kFar S itself
+// products; from 2^28 on these are further apart than Lag::kHead, so where they pass kFar S itself
 // becomes the difference of the rounded product (a power of two as c has none to round).
 constexpr float kFar = 0x1p20f;
-__device__ __forceinline__ float take_scores(RowState& rs, f16v (&S)[2], float& c) {
+template <typename T>
+__device__ __forceinline__ float take_scores(RowState<T>& rs, f16v (&S)[2], float& c) {
 #pragma clang fp contract(off)
   const float mx = tile_max(S) * c;
   rs.raise(mx);
@@ -406,7 +412,8 @@ struct Tokens {
 };
 
 // the row's partial: reference, sum, accumulator
-__device__ __forceinline__ void write_partial(const AttendLaunch& a, const RowState& st,
+template <typename T>
+__device__ __forceinline__ void write_partial(const AttendLaunch& a, const RowState<T>& st,
                                               int64_t row, int split, bool live, int lane) {
   const float l = sum_halves(st.l);
   if (!live) return;

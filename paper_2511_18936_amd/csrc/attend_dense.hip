@@ -146,7 +146,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kern
     for (int s = 0; s < N; ++s)
       to[s] = live ? *(const u32x4*)(qr + 2 * E * s + E * (lane >> 5)) : u32x4{0u, 0u, 0u, 0u};
   }
-  RowState rs;
+  RowState<T> rs;
   // A tile's scores are taken during the exponentials of the one before, so its keys are in
   // LDS one tile ahead of its values; a buffer is loaded again after the barrier behind its
   // last reads.
@@ -157,8 +157,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kern
     if (!a.o0 || !live || a.part) return;
     const float lse = a.lse0[row] * kLog2e;
     if (lse == -INFINITY) return;
-    rs.ref = lse - kHead;
-    const float w = __builtin_amdgcn_exp2f(lse - rs.ref);  // (2^kHead but for a rounded ref)
+    rs.ref = lse - Lag<T>::kHead;
+    const float w = __builtin_amdgcn_exp2f(lse - rs.ref);  // (2^Lag::kHead but for a rounded ref)
     rs.l = lane < 32 ? w : 0.f;
     const float* o = a.o0 + row * kD + 4 * (lane >> 5);
 #pragma unroll

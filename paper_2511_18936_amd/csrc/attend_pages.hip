@@ -152,7 +152,7 @@ struct QueryRows {
   bool live, busy;  // this lane's row, some row of the wave is one
   float c;
   typename Tl::template Q<true> q;
-  RowState rs;
+  RowState<E> rs;
 
   __device__ __forceinline__ QueryRows(const AttendLaunch& a, const Unit& un, const Tokens& tokens,
                                       int wave, int lane) {

@@ -120,3 +120,42 @@ def test_a_far_row_beside_others(gpu_device, swan_mod, torch_mod):
     got = swan_mod.prompt_attention(changed, k * 1, v)
     assert torch.equal(got[:, :, 0::2], want[:, :, 0::2])
     assert torch.isfinite(got).all()
+
+
+@pytest.mark.parametrize("n,m", [(3, 20), (150, 100), (2, 1500), (140, 5)])
+def test_float32_values_near_the_end_of_their_range(gpu_device, swan_mod, torch_mod, n, m):
+    """Values and states of up to 3e38 whose weighted means are as large and finite: over a
+    prompt's keys, cached ones, and single tokens behind a prefix."""
+    torch = torch_mod
+    g = torch.Generator().manual_seed(11)
+    q, k = (torch.randn(1, 1, r, D, generator=g).to(gpu_device) for r in (n, m))
+    v = torch.zeros(1, 1, m, D, device=gpu_device)
+    v[0, 0, 2] = 3e38
+    v[0, 0, 3] = -1e38
+    o = torch.full((1, 1, n, D), 3e38, device=gpu_device)
+    lse = torch.full((1, 1, n), math.log(m), device=gpu_device)
+    eye = torch.eye(D, device=gpu_device)[None].contiguous()
+    cache = swan_mod.SwanCache(1, 1, 1, 8, m, [D], torch.float32, gpu_device)
+    cache.append(k, v, eye, None)
+    B = min(n, 64)  # a batch's sequences
+    own = swan_mod.SwanCache(B, 1, 1, 8, 8, [D] * B, torch.float32, gpu_device)
+    own.append(k[:, :, :1].expand(B, 1, 1, D).contiguous(),
+               v[:, :, :1].expand(B, 1, 1, D).contiguous(), eye, None)
+    # 2^-60 of the values for the formula, which adds them up first
+    small = (v[0, 0].double() * 2.0 ** -60)
+    for name, got, state, keys, values in (
+            ("prompt", swan_mod.prompt_attention(q, k, v, causal=False)[0, 0], None, k[0, 0], small),
+            ("state", swan_mod.prompt_attention(q, k, v, causal=False, state=(o, lse))[0, 0],
+             (o[0, 0].double() * 2.0 ** -60, lse[0, 0]), k[0, 0], small),
+            ("cached", cache.attend(q, eye, None)[0][0, 0], None, k[0, 0], small),
+            ("decode", own.decode(q[0, :, :B].transpose(0, 1).contiguous(), eye, None,
+                                  prefix=swan_mod.Prefix(cache))[:, 0], None,
+             torch.cat([k[0, 0], k[0, 0, :1]]), torch.cat([small, small[:1]]))):
+        want, _ = R.softmax_rows(q[0, 0, :len(got)], keys, values, None, state)
+        # as float32 attention anywhere: scores of 128 products of up to |q| |k| / sqrt(D) in
+        # the exponent, twice, sums of m terms
+        most = q.norm(dim=-1).max().item() * k.norm(dim=-1).max().item() / math.sqrt(D)
+        rel = 2 * most * 130 * 2.0 ** -24 + (m + 64) * 2.0 ** -24
+        tol = values.abs().max() * rel if state is None else 3e38 * 2.0 ** -60 * rel
+        assert torch.isfinite(got).all(), name
+        assert ((got.double() * 2.0 ** -60 - want).abs() <= tol).all(), name
