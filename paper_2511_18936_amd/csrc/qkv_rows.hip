@@ -38,12 +38,13 @@ __device__ __forceinline__ void one_nan_of(T& y) {
   if constexpr (sizeof(T) == 2) y = __builtin_bit_cast(T, one_nan(__builtin_bit_cast(uint16_t, y)));
 }
 
-// 1 / sqrt(ms).  Binary16 rows: their mean square lies within float32's range, so the
-// float32 estimate and one step of Newton's method (error squared, below 2^-44).
+// 1 / sqrt(ms).  Binary16 rows: the float64 estimate, within 2^-22, and one step of Newton's
+// method (error squared, below 2^-43).  Not the float32 one: ms may be below or above its
+// range, for a row of zeros with a tiny eps or any row with a huge one.
 template <typename T>
 __device__ __forceinline__ double inv_root(double ms) {
   if constexpr (sizeof(T) == 2) {
-    const double r = (double)__builtin_amdgcn_rsqf((float)ms);
+    const double r = __builtin_amdgcn_rsq(ms);
     return r == 0.0 ? 0.0 : r * (1.5 - 0.5 * ms * r * r);  // an infinity in the row: 0
   } else {
     return 1.0 / sqrt(ms);
