@@ -60,6 +60,17 @@ __device__ __forceinline__ float sum_halves(float v) {
   return b.x + b.y;
 }
 
+// What numbers with this largest magnitude are multiplied by before they are split into two
+// binary16 parts (within 2^-23 of them, and 2^-38 of the largest: its parts would be subnormal
+// as they are), and c, what that leaves to multiply results by: 2^(13 - exponent) and the
+// inverse; 1 for zeros, infinities or NaNs.
+__device__ __forceinline__ float split_scale(float top, float& c) {
+  const int ex = (int)((__float_as_uint(top) >> 23) & 0xFF) - 127;
+  const int up = top > 0.f && ex < 128 ? 13 - (ex < -100 ? -100 : ex) : 0;
+  c = __builtin_ldexpf(1.f, -up);
+  return __builtin_ldexpf(1.f, up);
+}
+
 #define SWAN_LDS __attribute__((address_space(3)))
 
 // A tile in LDS: 64 keys' rows of K or V, row-major as in memory, so that they can be

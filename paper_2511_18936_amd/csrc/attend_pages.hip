@@ -4,8 +4,8 @@
 //
 // The rotated queries are float32.  On the binary16 formats each row is brought by a power
 // of two to 2^13 .. 2^14 at its largest component and split into two binary16 parts, whose
-// products with the keys are both taken: 22 bits, as the decode kernels' float32 queries
-// against binary16 keys but for the last two.
+// products with the keys are both taken: within 2^-23 of the decode kernels' float32 queries,
+// a bit less than these.
 #include <type_traits>
 
 #include "attend.h"
@@ -98,16 +98,6 @@ struct PageStage {
   }
 };
 
-// What a row of queries with this largest magnitude is multiplied by before it is split into
-// binary16 parts, and c, what its scores then are: 2^(13 - exponent) and the inverse; 1 for a
-// row of zeros, infinities or NaNs.
-__device__ __forceinline__ float row_scale(float top, float& c) {
-  const int ex = (int)((__float_as_uint(top) >> 23) & 0xFF) - 127;
-  const int up = top > 0.f && ex < 128 ? 13 - (ex < -100 ? -100 : ex) : 0;
-  c = __builtin_ldexpf(1.f, -up);
-  return __builtin_ldexpf(1.f, up);
-}
-
 // This lane's half of its row's rotated queries, from float32 at qr (zeros unless `live`), and
 // what their scores are multiplied by
 template <typename E>
@@ -130,7 +120,7 @@ __device__ __forceinline__ float row_queries(const float* qr, bool live, int lan
         top = fmaxf(top, fabsf(v[e]));
       }
     }
-    const float f = row_scale(max_halves(top), c);
+    const float f = split_scale(max_halves(top), c);
 #pragma unroll
     for (int s = 0; s < 8; ++s)
 #pragma unroll

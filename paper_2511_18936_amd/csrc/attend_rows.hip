@@ -6,10 +6,10 @@ namespace swan {
 
 // y = mult * x . M, M = P (or its transpose) of the row's kv head, as M^T . x^T on MFMA: a
 // workgroup takes 128 rows of one (sequence, head), wave w has dims 32 w .. + 31 of the
-// result and holds that part of M^T.  Binary16 rows: M as two binary16 parts (22 bits);
-// float32 rows: float32 MFMA.  The matrix is read once per 128 rows, strided, as its 64 KiB
-// stay in L2; the rows' float32 results are most of the traffic: 32768 binary16 rows 11 us,
-// 2.2 TB/s.
+// result and holds that part of M^T.  Binary16 rows: M as two binary16 parts (split_scale by
+// the largest entry of the wave's part); float32 rows: float32 MFMA.  The matrix is read once
+// per 128 rows, strided, as its 64 KiB stay in L2; the rows' float32 results are most of the
+// traffic: 32768 binary16 rows 11 us, 2.2 TB/s.
 template <typename T>
 __global__ __launch_bounds__(256) void rotate_rows_kernel(RotateLaunch a) {
   const int tid = threadIdx.x, lane = tid & 63, hi = lane >> 5;
@@ -23,14 +23,22 @@ __global__ __launch_bounds__(256) void rotate_rows_kernel(RotateLaunch a) {
   constexpr bool k16 = sizeof(T) == 2;
   h8v mh[k16 ? 8 : 1], ml[k16 ? 8 : 1];
   f4v mf[k16 ? 1 : 16];
+  float c = 1.f;
   if constexpr (k16) {
+    float top = 0.f, x[kD / 2];
+#pragma unroll
+    for (int i = 0; i < kD / 2; ++i) {
+      x[i] = m(16 * (i >> 3) + 8 * hi + (i & 7));
+      top = fmaxf(top, fabsf(x[i]));
+    }
+    const float f = split_scale(wave_max(top), c);
 #pragma unroll
     for (int s = 0; s < 8; ++s)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float x = m(16 * s + 8 * hi + e);
-        mh[s][e] = (_Float16)x;
-        ml[s][e] = (_Float16)(x - (float)mh[s][e]);
+        const float y = x[8 * s + e] * f;
+        mh[s][e] = (_Float16)y;
+        ml[s][e] = (_Float16)(y - (float)mh[s][e]);
       }
   } else {
 #pragma unroll
@@ -66,8 +74,8 @@ __global__ __launch_bounds__(256) void rotate_rows_kernel(RotateLaunch a) {
       float* y = a.y + at + 32 * wave + 4 * hi;
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        *(f4v*)(y + 8 * e) = f4v{acc[4 * e] * a.mult, acc[4 * e + 1] * a.mult,
-                                 acc[4 * e + 2] * a.mult, acc[4 * e + 3] * a.mult};
+        *(f4v*)(y + 8 * e) = f4v{acc[4 * e] * c * a.mult, acc[4 * e + 1] * c * a.mult,
+                                 acc[4 * e + 2] * c * a.mult, acc[4 * e + 3] * c * a.mult};
     }
   }
 }

@@ -142,3 +142,19 @@ def test_values_that_are_no_numbers(gpu_device, swan_mod, torch_mod, what, far):
         for d in (5, 9):
             x = got[name][..., d]
             assert torch.isnan(x).all() if math.isnan(what) else (x == what).all(), (name, d)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("power", [-60, -20, -10, 12])
+def test_rotations_of_any_size(gpu_device, swan_mod, torch_mod, dtype, power):
+    """P_qk times a power of two and the scale times its inverse: the same bits, few or many
+    rows."""
+    torch = torch_mod
+    cache, P_qk, P_vo = R.filled_cache(swan_mod, gpu_device, [300, 77], 8, 2, 16, [64, 128], dtype, 5)
+    g = torch.Generator().manual_seed(6)
+    q = torch.randn(2, 8, 70, D, generator=g).to(cache.dtype).to(gpu_device)
+    for rows in (q, q[:, :, :1].contiguous()):
+        want = cache.attend(rows, P_qk, P_vo, scale=0.11)
+        got = cache.attend(rows, P_qk * 2.0 ** power, P_vo, scale=0.11 * 2.0 ** -power)
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
