@@ -473,9 +473,22 @@ def _made(how: str, shape, dtype, device, stream):
         return make(shape, dtype=dtype, device=device)
 
 
-def _made_like(t, shape, stream):
-    """t.new_empty(shape), on the stream that the call is enqueued on (see _made)."""
-    return t.new_empty(shape) if stream is None else _made("empty", shape, t.dtype, t.device, stream)
+def _result(how: str, shape, dtype, device, stream):
+    """_made() for what a call returns: the caller may use it on the current stream and drop
+    it, so a block of another stream's is not used again before that work is done."""
+    import torch
+
+    t = _made(how, shape, dtype, device, stream)
+    if stream is not None and t.is_cuda:
+        current = torch.cuda.current_stream(t.device)
+        if current != stream:
+            t.record_stream(current)
+    return t
+
+
+def _result_like(t, shape, stream):
+    """An empty result of t's type beside it."""
+    return t.new_empty(shape) if stream is None else _result("empty", shape, t.dtype, t.device, stream)
 
 
 def qkv_rows(qkv, n_q_heads: int, n_kv_heads: int, pos0: Sequence[int], base: float,
@@ -505,10 +518,10 @@ def qkv_rows(qkv, n_q_heads: int, n_kv_heads: int, pos0: Sequence[int], base: fl
     if out is None:
         q = k = v = None
         if n_q_heads:
-            q = _made_like(qkv, (B, n_q_heads, n, HEAD_DIM), stream)
+            q = _result_like(qkv, (B, n_q_heads, n, HEAD_DIM), stream)
         if n_kv_heads:
-            k = _made_like(qkv, (B, n_kv_heads, n, HEAD_DIM), stream)
-            v = _made_like(qkv, (B, n_kv_heads, n, HEAD_DIM), stream)
+            k = _result_like(qkv, (B, n_kv_heads, n, HEAD_DIM), stream)
+            v = _result_like(qkv, (B, n_kv_heads, n, HEAD_DIM), stream)
         device = _same_gpu(qkv=qkv, q_weight=q_weight, k_weight=k_weight)
     else:
         q, k, v = out
@@ -565,7 +578,7 @@ def prompt_attention(q, k, v, causal: bool = True, n: Optional[Sequence[int]] = 
     o0, lse0 = _state(state, B, hq, nq)
     if out is None:
         _same_gpu(q=q)
-        out = _made("empty" if n is None else "zeros", q.shape, q.dtype, q.device, stream)
+        out = _result("empty" if n is None else "zeros", q.shape, q.dtype, q.device, stream)
     _tensor(out, "out", q.dtype, (B, hq, nq, HEAD_DIM))
     device = _same_gpu(q=q, k=k, v=v, out=out, o=o0, lse=lse0)
     ns, ms = _per_sequence(n, B, "n"), _per_sequence(m, B, "m")
@@ -633,8 +646,8 @@ def attend(sources, q, P_qk, P_vo, n: Optional[Sequence[int]] = None, scale: flo
     if out is None:
         _same_gpu(q=q)
         how = "empty" if n is None else "zeros"
-        out = (_made(how, (B, hq, nq, HEAD_DIM), "float32", q.device, stream),
-               _made(how, (B, hq, nq), "float32", q.device, stream))
+        out = (_result(how, (B, hq, nq, HEAD_DIM), "float32", q.device, stream),
+               _result(how, (B, hq, nq), "float32", q.device, stream))
     o, lse = _state(out, B, hq, nq)
     pages = {f"source {i}": s.cache.k_pages for i, s in enumerate(sources)}
     device = _same_gpu(q=q, P_qk=P_qk, P_vo=P_vo, o=o, lse=lse, **pages)
@@ -831,7 +844,7 @@ class SwanCache:
                prefix: Optional[Prefix] = None):
         """Attention of q ([B][H_q][d]) over the cache, behind a prefix where one is given."""
         if out is None:
-            out = _made_like(q, q.shape, stream)
+            out = _result_like(q, q.shape, stream)
         if prefix is None:
             decode_attention(self.desc, self.seq_len, self.k_active, q, P_qk, P_vo, out,
                              self.workspace(), scale, stream, self.k_value)
@@ -847,7 +860,7 @@ class SwanCache:
         advance the lengths, and return the attention of q ([B][H_q][d]) over the cache,
         behind a prefix where one is given."""
         if out is None:
-            out = _made_like(q, q.shape, stream)
+            out = _result_like(q, q.shape, stream)
         after = [L + 1 for L in self.seq_len]
         ws = self.workspace(after, prefix, stream)
         if prefix is None:
