@@ -774,7 +774,6 @@ class SwanCache:
         self.desc.v_pages = self.v_pages.data_ptr()
         self.desc.k_ring = self.k_ring.data_ptr() if buffer_tokens > 0 else None
         self.desc.v_ring = self.v_ring.data_ptr() if buffer_tokens > 0 else None
-        self._ws = None
 
     @property
     def batch(self) -> int:
@@ -812,24 +811,19 @@ class SwanCache:
         (stream or torch.cuda.current_stream()).synchronize()
         self.desc, self.k_pages, self.v_pages = dst, k_pages, v_pages
         self.k_active, self.k_value = k_active, k_value
-        self._ws = None
 
     def workspace(self, seq_len: Optional[Sequence[int]] = None, prefix: Optional[Prefix] = None,
                   stream=None):
-        """The decode workspace for these lengths (default: the present ones): one for all
-        calls of this cache without a prefix, so they are made on one stream at a time.  A
-        call behind a prefix gets one of its own, of the caching allocator's memory for
-        `stream` (or, captured, for its graph)."""
-        import torch
-
+        """A decode workspace for these lengths (default: the present ones), of the caching
+        allocator's memory for `stream` (or, captured, for its graph).  decode() and step()
+        take one for each call, so calls on several streams, and graphs that are replayed
+        beside them, share none."""
         lens = self.seq_len if seq_len is None else seq_len
-        if prefix is not None:
+        if prefix is None:
+            need = decode_workspace_bytes(self.desc, lens, self.k_active, self.k_value)
+        else:
             need = prefix_workspace_bytes(prefix, self.desc, lens, self.k_active, self.k_value)
-            return _made("empty", (need,), "uint8", self.device, stream)
-        need = decode_workspace_bytes(self.desc, lens, self.k_active, self.k_value)
-        if self._ws is None or self._ws.numel() < need:
-            self._ws = torch.empty(need, dtype=torch.uint8, device=self.device)
-        return self._ws
+        return _made("empty", (need,), "uint8", self.k_pages.device, stream)
 
     def attend(self, q, P_qk, P_vo, of: Optional[Sequence[int]] = None,
                n: Optional[Sequence[int]] = None, scale: float = 0.0,
@@ -847,7 +841,7 @@ class SwanCache:
             out = _result_like(q, q.shape, stream)
         if prefix is None:
             decode_attention(self.desc, self.seq_len, self.k_active, q, P_qk, P_vo, out,
-                             self.workspace(), scale, stream, self.k_value)
+                             self.workspace(None, None, stream), scale, stream, self.k_value)
         else:
             decode_attention_prefix(prefix, self.desc, self.seq_len, self.k_active, q, P_qk, P_vo,
                                     out, self.workspace(None, prefix, stream), scale, stream,

@@ -59,3 +59,83 @@ def test_a_result_used_on_the_current_stream_and_dropped(gpu_device, swan_mod, t
     assert all(t.data_ptr() != place for t in others)
     assert torch.equal(kept, want)
     del keep
+
+
+def test_plain_calls_on_two_streams_at_once(gpu_device, swan_mod, torch_mod):
+    """Decode calls of one cache, enqueued on two streams without waiting."""
+    torch = torch_mod
+    own, _, P_qk, P_vo = _caches(swan_mod, gpu_device)
+    g = torch.Generator().manual_seed(2)
+    qs = [torch.randn(3, 8, D, generator=g).half().to(gpu_device) for _ in range(2)]
+    want = [own.decode(q, P_qk, P_vo) for q in qs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in qs]
+    got = [[], []]
+    for _ in range(20):
+        for i, s in enumerate(streams):
+            got[i].append(own.decode(qs[i], P_qk, P_vo, stream=s))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(x, want[i]) for x in got[i]), i
+
+
+def test_a_plan_that_grows_on_a_side_stream(gpu_device, swan_mod, torch_mod):
+    """Decode calls on a side stream alone, of lengths that need more workspace from call to
+    call, while the current stream makes, fills and reads tensors."""
+    torch = torch_mod
+    cache, P_qk, P_vo = R.filled_cache(swan_mod, gpu_device, [6000, 3000], 8, 8, 16, [32] * 2, "f16",
+                                       73)
+    g = torch.Generator().manual_seed(3)
+    q = torch.randn(2, 8, D, generator=g).half().to(gpu_device)
+    lengths = [[n, n // 2] for n in (20, 100, 300, 1000, 3000, 6000)]
+    want = []
+    for cache.seq_len in lengths:
+        want.append(cache.decode(q, P_qk, P_vo))
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for turn in range(3):
+        got, mine = [], []
+        for i, cache.seq_len in enumerate(lengths):
+            for _ in range(4):
+                got.append((i, cache.decode(q, P_qk, P_vo, stream=side)))
+                mine.append(torch.full((300, 1000), float(len(mine)), device=gpu_device))
+        assert all(bool((t == n).all()) for n, t in enumerate(mine))
+        side.synchronize()
+        assert all(torch.equal(x, want[i]) for i, x in got), turn
+
+
+def test_a_graph_beside_a_plan_that_grows(gpu_device, swan_mod, torch_mod):
+    """Two captured decode calls of one cache, replayed on two streams at once, with eager
+    calls that need more workspace, and other tensors, between."""
+    torch = torch_mod
+    cache, P_qk, P_vo = R.filled_cache(swan_mod, gpu_device, [6000, 3000], 8, 8, 16, [32] * 2, "f16",
+                                       74)
+    g = torch.Generator().manual_seed(4)
+    qs = [torch.randn(2, 8, D, generator=g).half().to(gpu_device) for _ in range(2)]
+    cache.seq_len = [300, 200]
+    want = [cache.decode(q, P_qk, P_vo) for q in qs]
+    torch.cuda.synchronize()
+    outs, graphs = [torch.zeros_like(q) for q in qs], []
+    for q, out in zip(qs, outs):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            cache.decode(q, P_qk, P_vo, out=out)
+        graphs.append(graph)
+    cache.seq_len = [6000, 3000]
+    longer = cache.decode(qs[0], P_qk, P_vo)
+    streams = [torch.cuda.Stream() for _ in qs]
+    torch.cuda.synchronize()
+    for turn in range(4):
+        for out in outs:
+            out.zero_()
+        torch.cuda.synchronize()
+        for graph, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                graph.replay()
+        again = cache.decode(qs[0], P_qk, P_vo)
+        mine = [torch.full((100, 1000), 3.0, device=gpu_device) for _ in range(8)]
+        torch.cuda.synchronize()
+        assert torch.equal(again, longer), turn
+        assert all(bool((t == 3).all()) for t in mine), turn
+        for out, x in zip(outs, want):
+            assert torch.equal(out, x), turn
