@@ -265,12 +265,9 @@ def calibrate_workspace_bytes(d: int = HEAD_DIM) -> int:
 
 def calibrate_rotation(rows, P_out, sigma_out=None, workspace=None, stream=None) -> None:
     """Sec. 4.1.2 basis of `rows` ([n][d] float32, cuda) into P_out ([d][d] float32)."""
-    import torch
-
     n, d = rows.shape
     if workspace is None:
-        workspace = torch.empty(calibrate_workspace_bytes(d), dtype=torch.uint8,
-                                device=rows.device)
+        workspace = _made("empty", (calibrate_workspace_bytes(d),), "uint8", rows.device, stream)
     _check(_lib.swan_calibrate_rotation(_ptr(rows), n, d, _ptr(P_out), _ptr(sigma_out),
                                         _ptr(workspace), workspace.numel(), _stream(stream)))
 
@@ -289,8 +286,8 @@ def calibrate_rotations(rows, n_rows: Sequence[int], P_out, sigma_out=None, work
         _tensor(sigma_out, "sigma_out", torch.float32, (count, d))
     _on_gpu(rows=rows, P_out=P_out, sigma_out=sigma_out)
     if workspace is None:
-        workspace = torch.empty(count * calibrate_workspace_bytes(d), dtype=torch.uint8,
-                                device=rows.device)
+        workspace = _made("empty", (count * calibrate_workspace_bytes(d),), "uint8", rows.device,
+                          stream)
     _check(_lib.swan_calibrate_rotations(_ptr(rows), count, (ctypes.c_int64 * count)(*n_rows), d,
                                          _ptr(P_out), _ptr(sigma_out), _ptr(workspace),
                                          workspace.numel(), _stream(stream, rows.get_device())))
@@ -392,7 +389,7 @@ def rope(x, pos0: Sequence[int], base: float, out=None, stream=None):
     import torch
 
     if out is None:
-        out = torch.empty_like(x)
+        out = torch.empty_like(x) if stream is None else _result_like(x, x.shape, stream)
     B, H, n, d = x.shape
     code = SWAN_F16 if x.dtype == torch.float16 else SWAN_F32
     _check(_lib.swan_rope(_ptr(x), _ptr(out), code, B, H, n, d, _i32_array(pos0), float(base),
@@ -801,8 +798,8 @@ class SwanCache:
         k_value = None if k_value is None else [int(k) for k in k_value]
         dst = CacheDesc(*[getattr(self.desc, f) for f, _ in CacheDesc._fields_])
         kb, vb, _ = cache_bytes(dst, k_active, k_value)
-        k_pages = torch.zeros(max(kb, 16), dtype=torch.uint8, device=self.device)
-        v_pages = torch.zeros(max(vb, 16), dtype=torch.uint8, device=self.device)
+        k_pages, v_pages = (_result("zeros", (max(n, 16),), "uint8", self.k_pages.device, stream)
+                            for n in (kb, vb))
         dst.k_pages = k_pages.data_ptr()
         dst.v_pages = v_pages.data_ptr()
         change_k(self.desc, self.k_active, self.k_value, dst, k_active, k_value, self.seq_len,

@@ -139,3 +139,23 @@ def test_a_graph_beside_a_plan_that_grows(gpu_device, swan_mod, torch_mod):
         assert all(bool((t == 3).all()) for t in mine), turn
         for out, x in zip(outs, want):
             assert torch.equal(out, x), turn
+
+
+def test_change_k_and_rope_on_a_side_stream(gpu_device, swan_mod, torch_mod):
+    """While the current stream is busy: pages cleared and converted on the side stream."""
+    torch = torch_mod
+    caches = []
+    for stream in (None, torch.cuda.Stream()):
+        cache, P_qk, P_vo = R.filled_cache(swan_mod, gpu_device, [2000, 300], 8, 2, 16, [64] * 2,
+                                           "f16", 75)
+        x = torch.randn(2, 8, 50, D, generator=torch.Generator().manual_seed(5)).half().to(gpu_device)
+        torch.cuda.synchronize()
+        keep = _busy(torch, gpu_device)
+        turned = swan_mod.rope(x, [3, 900], 10000.0, stream=stream)
+        cache.change_k([40, 32], stream=stream)
+        torch.cuda.synchronize()
+        caches.append((cache, turned))
+        del keep
+    (a, x), (b, y) = caches
+    assert torch.equal(x, y)
+    assert torch.equal(a.k_pages, b.k_pages) and torch.equal(a.v_pages, b.v_pages)

@@ -71,3 +71,44 @@ def test_a_call_has_a_workspace_of_its_own_stream(monkeypatch, call):
     assert [t.numel() for t in spaces] == [n for n, _ in made]
     assert len({t.data_ptr() for t in spaces}) == 3 and spaces[0].numel() < spaces[2].numel()
     assert all("side" in args for args in used)
+
+
+@pytest.mark.parametrize("call", ["calibrate_rotation", "calibrate_rotations", "change_k", "rope"])
+def test_other_calls_make_their_memory_on_their_stream(monkeypatch, call):
+    """Workspaces, cleared pages and results of the calls that are not decode steps."""
+    import torch
+
+    cache, made = _cache(), []
+
+    class Stream:
+        cuda_stream = 0
+
+        def synchronize(self):
+            pass
+
+    side = Stream()
+
+    def make(how, shape, dtype, device, stream):
+        made.append(stream)
+        dtype = getattr(torch, dtype) if isinstance(dtype, str) else dtype
+        return getattr(torch, how)(shape, dtype=dtype)
+
+    class Lib:
+        def __getattr__(self, name):
+            return (lambda *args: 0) if name != "swan_calibrate_workspace_bytes" and \
+                name != "swan_cache_bytes" else getattr(real, name)
+
+    real = swan._lib
+    monkeypatch.setattr(swan, "_made", make)
+    monkeypatch.setattr(swan, "_lib", Lib())
+    monkeypatch.setattr(swan, "_on_gpu", lambda **tensors: None)
+    rows, P = torch.zeros(300, 128), torch.zeros(2, 128, 128)
+    if call == "calibrate_rotation":
+        swan.calibrate_rotation(rows, P[0], stream=side)
+    elif call == "calibrate_rotations":
+        swan.calibrate_rotations(rows, [100, 200], P, stream=side)
+    elif call == "change_k":
+        cache.change_k([32, 64], stream=side)
+    else:
+        swan.rope(torch.zeros(2, 1, 3, 128), [0, 5], 10000.0, stream=side)
+    assert made and all(s is side for s in made)
