@@ -24,6 +24,7 @@ Weights are [in][out] row-major, x . W.
 from __future__ import annotations
 
 import copy
+import types
 from typing import Optional, Sequence
 
 from . import swan
@@ -110,6 +111,11 @@ def calibrate_joint(q, k, v, W_o, n_kv_heads: int, P_qk_out, P_vo_out, stream=No
     on.synchronize()  # the rotations are in place on return, for any stream
 
 
+def _no_project(self, x):
+    raise ValueError("the layer that this one was forked from has a project() of its own, a "
+                     "function that may use that layer's positions: set this one's project")
+
+
 class SwanAttentionLayer:
     def __init__(self, W_q, W_k, W_v, W_o, P_qk, P_vo, n_heads: int, n_kv_heads: int,
                  rope_base: float, batch: int, buffer_tokens: int, capacity: int,
@@ -155,7 +161,8 @@ class SwanAttentionLayer:
         """A layer with the same weights for len(of) new sequences, sequence b behind the
         tokens of this layer's sequence of[b], which are held, and read, once: their positions
         follow them and their attention includes them.  The new layer refers to this one's
-        cache, which should not grow meanwhile (positions would move)."""
+        cache, which should not grow meanwhile (positions would move).  A project() replaced on this object goes over where it is a method of it; any
+        other function is to be replaced on the new layer too."""
         if self.prefix is not None:
             raise ValueError("this layer's sequences stand behind a prefix themselves")
         of = [int(p) for p in of]
@@ -166,6 +173,10 @@ class SwanAttentionLayer:
                                    capacity, k_active, self.dtype, self.cache.device,
                                    sparse_values=sparse_values, k_value=k_value)
         new.prefix = swan.Prefix(self.cache, of)
+        own = vars(self).get("project")
+        if own is not None:
+            mine = getattr(own, "__self__", None) is self
+            new.project = types.MethodType(own.__func__ if mine else _no_project, new)
         return new
 
     def positions(self):
