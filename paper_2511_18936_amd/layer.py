@@ -152,6 +152,7 @@ class SwanAttentionLayer:
                                     sparse_values=sparse_values, k_value=k_value)
 
     prefix: Optional[swan.Prefix] = None
+    _prefix_len: Optional[Sequence[int]] = None  # of the prefix's cache, at the fork
     q_norm = k_norm = None
     norm_eps = 1e-6
 
@@ -161,7 +162,8 @@ class SwanAttentionLayer:
         """A layer with the same weights for len(of) new sequences, sequence b behind the
         tokens of this layer's sequence of[b], which are held, and read, once: their positions
         follow them and their attention includes them.  The new layer refers to this one's
-        cache, which should not grow meanwhile (positions would move).  A project() replaced on this object goes over where it is a method of it; any
+        cache: where that grows, the new layer's positions would move, and it refuses to go
+        on.  A project() replaced on this object goes over where it is a method of it; any
         other function is to be replaced on the new layer too."""
         if self.prefix is not None:
             raise ValueError("this layer's sequences stand behind a prefix themselves")
@@ -173,6 +175,7 @@ class SwanAttentionLayer:
                                    capacity, k_active, self.dtype, self.cache.device,
                                    sparse_values=sparse_values, k_value=k_value)
         new.prefix = swan.Prefix(self.cache, of)
+        new._prefix_len = list(self.cache.seq_len)
         own = vars(self).get("project")
         if own is not None:
             mine = getattr(own, "__self__", None) is self
@@ -185,6 +188,10 @@ class SwanAttentionLayer:
             return self.cache.seq_len
         before = self.prefix.cache.seq_len
         of = self.prefix.of or [0] * self.cache.batch
+        if self._prefix_len is not None and any(p >= 0 and before[p] != self._prefix_len[p]
+                                                for p in of):
+            raise ValueError(f"the layer that this one was forked from has grown: its lengths "
+                             f"were {self._prefix_len}, are {before}")
         return [L + (before[p] if p >= 0 else 0) for L, p in zip(self.cache.seq_len, of)]
 
     def project(self, x):
@@ -210,6 +217,8 @@ class SwanAttentionLayer:
         each row over the tokens before the call as the caches hold them, and over the rows
         up to itself."""
         B, n = x.shape[0], x.shape[1]
+        if self.prefix is not None:
+            self.positions()  # (refuses a prefix that has grown, whatever project() asks)
         if n != 1 and not attend:
             k, v = self._prompt_rows(x)
             self.cache.append(k, v, self.P_qk, None)

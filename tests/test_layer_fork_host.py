@@ -61,3 +61,23 @@ def test_a_function_of_the_parent_is_not_used_for_the_fork(n, attend):
     assert fork.cache.seq_len == [0, 0, 0] and layer.project(None)[0] == [30, 40]
     fork.project = lambda x: (fork.positions(), x, x)
     assert fork.project(None)[0] == [30, 40, 40]
+
+
+@pytest.mark.parametrize("own", [False, True])
+@pytest.mark.parametrize("n,attend", [(1, False), (5, False), (5, True)])
+def test_a_parent_that_grows_is_refused(n, attend, own):
+    """Positions behind it would move; sequences that no fork stands behind may grow."""
+    import torch
+
+    layer = _layer()
+    fork = _fork(layer, [1, 1, 1])
+    if own:
+        fork.project = lambda x: (x, x, x)
+    layer.cache.seq_len = [31, 40]
+    assert fork.positions() == [40, 40, 40]
+    layer.cache.seq_len = [31, 41]
+    with pytest.raises(ValueError, match="grown"):
+        fork.positions()
+    with pytest.raises(ValueError, match="grown"):
+        fork(torch.zeros(3, n, 4), attend=attend)
+    assert fork.cache.seq_len == [0, 0, 0]
