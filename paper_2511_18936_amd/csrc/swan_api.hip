@@ -449,18 +449,18 @@ swan_status step_prep(const swan_cache* c, const int32_t* seq_len_host,
 // What a plan of the attend kernels costs, in microseconds as measured: a workgroup's
 // start, a tile of 64 keys of a workgroup on a full GPU (`slots` workgroups), and what share
 // of that a tile of a workgroup alone on its CU takes.  Pages, binary16, with workgroups of
-// 128 rows (two on a CU) or of 256 (`many`): 2.7 against 2 x 1.65 us for a tile of 256 rows,
-// so the larger ones where rows fill them (4 x 256 rows over 4 x 8192 keys: 232 against 250
-// us), the smaller ones where not (4 tokens of 32 heads over 4095 keys: 36 against 43 us).
+// 128 rows (two on a CU) or of 256 (`many`): 3.5 against 2 x 2.0 us for a tile of 256 rows,
+// so the larger ones where rows fill them (4 x 256 rows over 4 x 8192 keys: 290 against 319
+// us on one machine; 8 x 100 rows over 16384 keys 447 against 466).
 struct AttendCost {
   int slots;
   double tile, start, alone;
 };
 AttendCost attend_cost(int32_t dtype, bool pages, bool many = false) {
   if (dtype == SWAN_F32) return {256, pages ? 10.0 : 7.5, 8.0, 1.0};
-  if (many) return {256, 2.7, 6.0, 1.0};
-  if (pages) return {512, 3.3, 6.0, 0.72};
-  return {512, 2.3, 6.0, 0.65};
+  if (many) return {256, 3.5, 6.0, 1.0};
+  if (pages) return {512, 4.0, 6.0, 0.72};
+  return {512, 3.1, 6.0, 0.65};
 }
 
 // Tiles of keys per workgroup, so that the launch and the join of its partials are
