@@ -6,11 +6,13 @@
 // in float64 and rounded once, so that without weights the bits are swan_rope's.
 //
 // Bound by memory for long prompts: 8 x 8190 positions of 32 + 2 x 32 heads without norms
-// 614 us, 5.2 TB/s read and written (a large copy: 4.8).  In between float64 counts: 1999
-// positions of 32 + 2 x 8 heads with norms 14 us, 3.6 TB/s (a float64 product or sum takes a
-// wave 5.4 cycles, so 16 lanes have a row and 4 pairs each, and the sines are shared by the
-// heads); 3 x 517 positions of 12 + 2 x 4 float32 heads 9 us.  Single tokens (4 x 48 heads)
-// 3 us, the chain of pow and sincos.
+// 615 us, 5.2 TB/s read and written (a large copy: 4.8).  In between latency counts: 1999
+// positions of 32 + 2 x 8 heads with norms 13.7 us, 3.6 TB/s, where waves wait for half of
+// their time (pow, sincos and a barrier come before a row's load, and the workgroups are few)
+// and vector instructions, most of them float64, are issued in 28 % of the cycles; 16 lanes
+// have a row and 4 pairs each, and the sines are shared by the heads; 3 x 517 positions of
+// 12 + 2 x 4 float32 heads 9.6 us.  Single tokens (4 x 48 heads) 3 us, the chain of pow and
+// sincos.
 #include "swan_cache_ops.h"
 #include "swan_layer_ops.h"
 
@@ -261,11 +263,13 @@ static hipError_t launch_qkv_rows_t(const QkvRowsLaunch& a) {
     hipLaunchKernelGGL(qkv_rows_few_kernel<T>, dim3(a.n, H, a.B), dim3(64), 0, a.stream, a);
     return hipGetLastError();
   }
-  // Few positions split their heads, 4 at least to each, over 512 workgroups: more of them
-  // only repeat the sines and cosines (32 + 2 x 8 heads x 1999 positions, binary16: 14.7 us
-  // with 512, 16.2 with 1100, 19.6 with 2048).
+  // Few positions split their heads, 4 at least to each, over 768 workgroups: fewer leave
+  // processors idle, more repeat the sines and cosines.  Binary16 with norms, us with 512, 768
+  // and 1024: 32 + 2 x 8 heads x 300 positions 5.4, 5.4, 7.0, x 1100 12.9, 11.4, 12.3, x 1999
+  // 13.7, 13.7, 15.2; 32 + 2 x 32 heads x 500 9.7, 9.3, 10.8, x 1500 19.6, 16.5, 16.5; 16 + 2
+  // heads x 1000 6.4, 6.8, 6.9; float32, 12 + 2 x 4 heads, 3 x 517 9.6, 9.6, 10.4.
   const int64_t tiles = (positions + kTilePos - 1) / kTilePos;
-  int64_t chunks = 512 / tiles;
+  int64_t chunks = 768 / tiles;
   chunks = chunks < 1 ? 1 : chunks > (H + 3) / 4 ? (H + 3) / 4 : chunks;
   const int heads = (int)(((H + chunks - 1) / chunks + 3) / 4 * 4);
   const dim3 grid((unsigned)(tiles < 2048 ? tiles : 2048), (unsigned)((H + heads - 1) / heads));
