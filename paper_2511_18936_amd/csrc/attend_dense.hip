@@ -69,15 +69,16 @@ __device__ __forceinline__ void add_nonfinite(uint64_t keys, const T* vp, int ke
 //
 // Two workgroups of 64 KiB of LDS share a CU.  Tiles go to LDS without passing registers, keys
 // one tile ahead of values, and the scores of a tile are taken in steps between the
-// exponentials of the one before: MFMA bounds long prompts, at three products of which p's
-// second part is one.  Measured, binary16: 32 query heads on 8, 4096 causal rows 213-222 us by
-// machine, 935-970 TFLOP/s of products done (a large matrix product reaches 1200); 8 prompts of
-// up to 1009 rows, 32 heads 69 us (short rows of tiles, 6 us to start and end each).  Few rows
-// split the keys until the GPU is full and are bound by memory: single tokens of 16 heads over
-// up to 1500 keys of 16 sequences 25 us, 4.2 TB/s, and 4 us to join; the waves without a row
-// leave LDS to the others (28.6 us with the join; 34.7 if they multiply too).  Float32 (no
-// double use of a CU: its tiles take 128 KiB): 2 x 333 rows, 8 heads on 2, 23 us and 6 to join,
-// the latency of few workgroups.
+// exponentials of the one before.  Long prompts are bound by what a SIMD's two waves issue: of
+// the cycles MFMA is busy in 46 %, other vector instructions are issued in 38 %, seldom both.
+// Measured, binary16: 32 query heads on 8, 4096 causal rows 213-235 us by machine, 880-970
+// TFLOP/s of products done, p's second part among them (a large matrix product reaches 1200); 8
+// prompts of up to 1009 rows, 32 heads 69-77 us (short rows of tiles, 6 us to start and end
+// each).  Few rows split the keys until the GPU is full and are bound by memory: single tokens
+// of 16 heads over up to 1500 keys of 16 sequences 24 us, 4.3 TB/s, and 4 us to join; the
+// waves without a row leave LDS to the others (28.6 us with the join; 34.7 if they multiply
+// too).  Float32 (no double use of a CU: its tiles take 128 KiB): 2 x 333 rows, 8 heads on 2,
+// 23 us and 6 to join, the latency of few workgroups.
 //
 // The last tile stands behind the loop, without scores to take ahead: as a condition inside
 // the loop it made registers spill.

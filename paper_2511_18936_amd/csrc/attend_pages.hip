@@ -188,12 +188,14 @@ struct QueryRows {
 // scatters while the other multiplies (measured: without the priority 4 % more).  The ring's
 // tiles pass through registers there, as the third is past what dma_tile reaches.
 //
-// Bound by a wave's chain per tile: MFMA (two parts of q and of p make 64 instructions of 32
-// cycles for 32 rows), and the scattering, its LDS reads and the exponentials beside it.
-// Measured, k = 64 of 128: 4 x 256 rows of 32 heads on 8 over 4 x 8192 keys 277 us with the
-// other kernels of the chunk; 8 x 100 rows over 16384 shared keys, E4M3 values, 450 us; 32
-// tokens over 32768 keys 93 us and 4 tokens of 32 heads over 4095 keys 36 us with the own
-// tokens' and the other kernels.
+// Bound by a wave's chain per tile of products, scattering and exponentials.  Measured under
+// the profiler, k = 64 of 128: 4 x 256 rows of 32 heads on 8 over 4 x 8192 keys 266 us (with
+// workgroups of 128 rows 10 % more), where MFMA (two parts of q and of p: 64 instructions of
+// 32 cycles for 32 rows and 64 keys) is busy in 48 % of the cycles and other vector
+// instructions are issued in 32 %; 8 x 100 rows over 16384 shared keys, E4M3 values, 441 us,
+// 44 % and 31 %.  Few rows: 32 tokens over 32768 keys 55 us, 1.9 TB/s of pages, MFMA 26 %; 4
+// tokens of 32 heads over 4095 keys 20 us, where workgroups start and load for longer than
+// they multiply.
 template <typename T, int NU, int W>
 __global__ __launch_bounds__(64 * W, sizeof(typename Fmt<T>::Elem) == 2 ? 2 : 1) void
 attend_pages_kernel(AttendLaunch a) {
