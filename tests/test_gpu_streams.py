@@ -159,3 +159,33 @@ def test_change_k_and_rope_on_a_side_stream(gpu_device, swan_mod, torch_mod):
     (a, x), (b, y) = caches
     assert torch.equal(x, y)
     assert torch.equal(a.k_pages, b.k_pages) and torch.equal(a.v_pages, b.v_pages)
+
+
+def test_captured_on_a_stream_beside_the_capturing_one(gpu_device, swan_mod, torch_mod):
+    """Calls on a side stream that joins a capture, results and workspaces of the graph's
+    memory; one result is dropped inside the capture."""
+    torch = torch_mod
+    own, past, P_qk, P_vo = _caches(swan_mod, gpu_device)
+    g = torch.Generator().manual_seed(6)
+    q = torch.randn(3, 8, D, generator=g).half().to(gpu_device)
+    prefix = swan_mod.Prefix(past)
+    own.decode(q, P_qk, P_vo), own.decode(q, P_qk, P_vo, prefix=prefix)
+    torch.cuda.synchronize()
+    out, side, graph = torch.zeros(2, *q.shape, device=gpu_device).half(), torch.cuda.Stream(), \
+        torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        current = torch.cuda.current_stream()
+        side.wait_stream(current)
+        a = own.decode(q, P_qk, P_vo, stream=side)
+        b = own.decode(q, P_qk, P_vo, stream=side, prefix=prefix)
+        current.wait_stream(side)
+        out[0].copy_(a)
+        out[1].copy_(b)
+        del a
+    for turn in range(4):
+        q.mul_(0.9)
+        out.zero_()
+        graph.replay()
+        want = own.decode(q, P_qk, P_vo), own.decode(q, P_qk, P_vo, prefix=prefix)
+        torch.cuda.synchronize()
+        assert torch.equal(out[0], want[0]) and torch.equal(out[1], want[1]), turn
