@@ -20,7 +20,8 @@ BENCH_SOURCES = ["stream_ceiling.hip"]
 SOURCES = ["swan_api.hip", "decode.hip", "decode_gqa.hip", "decode_asym.hip",
            "decode_gqa_asym.hip", "decode_fused.hip", "compress.hip", "prefill.hip",
            "change_k.hip", "rope.hip", "calibrate.hip", "qkv_rows.hip", "attend_pages.hip",
-           "attend_dense.hip", "attend_rows.hip"]
+           "attend_dense.hip", "attend_rows.hip", "window_decode_gqa.hip", "window_decode.hip",
+           "copy_sequences.hip", "swan_long_api.hip"]
 ARCH = "gfx950"
 # per-source flags: the GQA and several-row attention kernels and the prefill rotation
 # keep their MFMA accumulators in VGPRs (the default puts them in AGPRs and copies them across
@@ -28,6 +29,7 @@ ARCH = "gfx950"
 SOURCE_FLAGS = {
     "decode_gqa.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "decode_gqa_asym.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+    "window_decode_gqa.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "prefill.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "attend_pages.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "attend_dense.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],

@@ -284,6 +284,66 @@ __device__ __forceinline__ int key_of(int t, int i, int lane) {
   return 32 * t + 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3);
 }
 
+// Values of a tile that are no numbers leave it (0 times them would be NaN in the rows that
+// must not see their key): zeros in their place, and the keys of this thread's that had one.
+template <typename T, int kThreads>
+__device__ __forceinline__ uint64_t take_nonfinite(char* vb, int tid) {
+  using R = Rows<T>;
+  uint64_t keys = 0;
+#pragma unroll 1
+  for (int piece = tid; piece < R::kTile / 16; piece += kThreads) {
+    u32x4 x = *(u32x4*)(vb + 16 * piece);
+    bool odd = false;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      if constexpr (sizeof(T) == 4) {
+        const bool a = (x[w] & 0x7F800000u) == 0x7F800000u;
+        x[w] = a ? 0u : x[w];
+        odd |= a;
+      } else {
+        const bool a = (x[w] & 0x7C00u) == 0x7C00u, b = (x[w] & 0x7C000000u) == 0x7C000000u;
+        x[w] &= (a ? 0xFFFF0000u : ~0u) & (b ? 0xFFFFu : ~0u);
+        odd |= a || b;
+      }
+    }
+    if (odd) {
+      *(u32x4*)(vb + 16 * piece) = x;
+      keys |= 1ull << (piece / R::kPieces);
+    }
+  }
+  return keys;
+}
+
+// O += p v for the values that take_nonfinite() took out of the tile, key by key, in the
+// rows that see the key: value(key, dim), sees(key).  Rare: the loops are for size, not for
+// speed.
+template <typename V, typename Sees>
+__device__ __forceinline__ void add_nonfinite(uint64_t keys, V value, Sees sees,
+                                              const f16v (&P)[2], int lane, f16v (&O)[4]) {
+#pragma unroll 1
+  while (keys) {
+    const int key = __builtin_ctzll(keys);
+    keys &= keys - 1;
+    float mine = 0.f;  // p of key 8 (key / 8) + 4 (lane / 32) + key % 4
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (key_of(t, i, 0) == (key & ~4)) mine = P[t][i];
+    const f4v both = both_halves(mine);
+    const float p = key & 4 ? both.y : both.x;
+    if (sees(key)) {
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float v = value(key, 32 * d + 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3));
+          if (!(v - v == 0.f)) O[d][i] += p * v;
+        }
+    }
+  }
+}
+
 // A wave's running softmax: a lane's row, dims 32 d + 8 (i / 4) + 4 (lane / 32) + i % 4
 template <typename T>
 struct RowState {
@@ -407,8 +467,9 @@ struct Tokens {
   int tok0, seq;
   __device__ __forceinline__ Tokens(const AttendLaunch& a, int lane)
       : tok0(a.tok0[lane]), seq(a.seq[lane]) {}
-  // token tok of group j: sequence b and row i of it (every lane of the wave asks)
-  __device__ __forceinline__ void at(const AttendLaunch& a, int j, int tok, int& b, int& i) const {
+  // token tok of group j: list entry e, sequence b and row i of it (every lane of the wave asks)
+  __device__ __forceinline__ void at(const AttendLaunch& a, int j, int tok, int& e, int& b,
+                                     int& i) const {
     int lo = a.first[j], hi = a.first[j + 1];  // uniform
     while (__any(hi - lo > 1)) {
       const int mid = (lo + hi) >> 1;
@@ -417,6 +478,7 @@ struct Tokens {
       lo = up ? mid : lo;
       hi = up ? hi : mid > lo ? mid : lo + 1;
     }
+    e = lo;
     b = __shfl(seq, lo, 64);
     i = tok - __shfl(tok0, lo, 64);
   }

@@ -4,66 +4,6 @@
 
 namespace swan {
 
-// Values of a tile that are no numbers leave it (0 times them would be NaN in the rows that
-// must not see their key): zeros in their place, and the keys of this thread's that had one.
-template <typename T>
-__device__ __forceinline__ uint64_t take_nonfinite(char* vb, int tid) {
-  using R = Rows<T>;
-  uint64_t keys = 0;
-#pragma unroll 1
-  for (int piece = tid; piece < R::kTile / 16; piece += 256) {
-    u32x4 x = *(u32x4*)(vb + 16 * piece);
-    bool odd = false;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      if constexpr (sizeof(T) == 4) {
-        const bool a = (x[w] & 0x7F800000u) == 0x7F800000u;
-        x[w] = a ? 0u : x[w];
-        odd |= a;
-      } else {
-        const bool a = (x[w] & 0x7C00u) == 0x7C00u, b = (x[w] & 0x7C000000u) == 0x7C000000u;
-        x[w] &= (a ? 0xFFFF0000u : ~0u) & (b ? 0xFFFFu : ~0u);
-        odd |= a || b;
-      }
-    }
-    if (odd) {
-      *(u32x4*)(vb + 16 * piece) = x;
-      keys |= 1ull << (piece / R::kPieces);
-    }
-  }
-  return keys;
-}
-
-// O += p v for the values that take_nonfinite() took out of the tile, key by key, in the
-// rows that see the key.  Rare: the loops are for size, not for speed.
-template <typename T>
-__device__ __forceinline__ void add_nonfinite(uint64_t keys, const T* vp, int key0, int limit,
-                                              const f16v (&P)[2], int lane, f16v (&O)[4]) {
-#pragma unroll 1
-  while (keys) {
-    const int key = __builtin_ctzll(keys);
-    keys &= keys - 1;
-    float mine = 0.f;  // p of key 8 (key / 8) + 4 (lane / 32) + key % 4
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (key_of(t, i, 0) == (key & ~4)) mine = P[t][i];
-    const f4v both = both_halves(mine);
-    const float p = key & 4 ? both.y : both.x;
-    const T* row = vp + (int64_t)(key0 + key) * kD + 4 * (lane >> 5);
-    if (key0 + key < limit) {
-#pragma unroll
-      for (int d = 0; d < 4; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float v = (float)row[32 * d + 8 * (i >> 2) + (i & 3)];
-          if (!(v - v == 0.f)) O[d][i] += p * v;
-        }
-    }
-  }
-}
-
 // Grid: a.units workgroups of 4 waves (unit_at), a group's last row tiles, of a causal prompt
 // the longest, first.
 //
@@ -82,7 +22,11 @@ __device__ __forceinline__ void add_nonfinite(uint64_t keys, const T* vp, int ke
 //
 // The last tile stands behind the loop, without scores to take ahead: as a condition inside
 // the loop it made registers spill.
-template <typename T>
+//
+// kWin: with a sliding window.  A row tile takes the tiles that hold the first keys, then
+// those from its first row's window on; the tiles' numbers go over the gap (key_tile), and
+// only tiles that some row of a wave does not see whole are masked.
+template <typename T, bool kWin>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kernel(AttendLaunch a) {
   using Tl = Tile<T>;
   using R = Rows<T>;
@@ -115,9 +59,21 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kern
   const int all_see = sees((int)a.by_g.of(row0 + 32 * wave));
   const int block_all = sees((int)a.by_g.of(row0));
   const int seen = sees(min(toks - 1, (int)a.by_g.of(row0 + kTileRows - 1)));
-  const int nt = (seen + kTileKeys - 1) / kTileKeys;
+  // The window: this lane's row sees no key between `sink` and limit - window.  first, full:
+  // the workgroup's first row's first key, the wave's last row's.
+  const int sink = kWin ? a.sink[un.j] : 0;
+  const int first = kWin ? max(0, block_all - a.window) : 0;
+  const int full = kWin ? sees(min(toks - 1, (int)a.by_g.of(row0 + 32 * wave + 31))) - a.window : 0;
+  const int all_tiles = (seen + kTileKeys - 1) / kTileKeys;
+  const int skip = min(first / kTileKeys, all_tiles);  // (tiles before the window)
+  const int sink_tiles = kWin ? min((sink + kTileKeys - 1) / kTileKeys, skip) : 0;
+  const int nt = all_tiles - skip + sink_tiles;
   const int t0 = split_first(nt, un.split, un.nsplit);
   const int t1 = split_first(nt, un.split + 1, un.nsplit);
+  // the first key of tile t of these nt
+  auto key_tile = [&](int t) {
+    return kWin && t >= sink_tiles ? (t - sink_tiles + skip) * kTileKeys : t * kTileKeys;
+  };
 
   const int64_t kv0 = ((int64_t)b * a.Hkv + h) * a.m * kD;
   const T* kp = (const T*)a.k + kv0;
@@ -126,13 +82,11 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kern
   // tile t is tile t - t0 of its buffers' turns; past the last, nothing
   auto load_k = [&](int t) {
     if (t < t1)
-      dma_tile(kbuf[(t - t0) & 1], kp + (int64_t)t * kTileKeys * kD, keys - t * kTileKeys, from,
-               wave);
+      dma_tile(kbuf[(t - t0) & 1], kp + (int64_t)key_tile(t) * kD, keys - key_tile(t), from, wave);
   };
   auto load_v = [&](int t) {
     if (t < t1)
-      dma_tile(vbuf[(t - t0) & 1], vp + (int64_t)t * kTileKeys * kD, keys - t * kTileKeys, from,
-               wave);
+      dma_tile(vbuf[(t - t0) & 1], vp + (int64_t)key_tile(t) * kD, keys - key_tile(t), from, wave);
   };
   load_k(t0);
   load_v(t0);
@@ -179,6 +133,18 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kern
         for (int i = 0; i < 16; ++i)
           if (key0 + key_of(x, i, lane) >= limit) S[x][i] = -INFINITY;
     }
+    if constexpr (kWin) {
+      if (key0 < full && key0 + kTileKeys > sink) {
+        const int lo = limit - a.window;
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int key = key0 + key_of(x, i, lane);
+            if (key < lo && key >= sink) S[x][i] = -INFINITY;
+          }
+      }
+    }
   };
   begin();
   f16v S[2], next[2];
@@ -191,7 +157,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kern
     load_k(t + 2);
     load_v(t + 1);
     if (busy) {
-      mask(S, t * kTileKeys);
+      mask(S, key_tile(t));
       float c = a.qmult;
       const float ref = take_scores(rs, S, c);
       rs.l += Tl::template values<true, false>(vbuf[par], S, c, ref, lane, rs.O, kbuf[par ^ 1], q,
@@ -203,7 +169,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kern
     __syncthreads();
   }
   if (busy && t0 < t1) {
-    mask(S, (t1 - 1) * kTileKeys);
+    mask(S, key_tile(t1 - 1));
     float c = a.qmult;
     const float ref = take_scores(rs, S, c);
     rs.l += Tl::template values<false, false>(vbuf[(t1 - 1 - t0) & 1], S, c, ref, lane, rs.O,
@@ -214,18 +180,18 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kern
   // of both signs.  Where a row's result is no number the workgroup starts again, takes such
   // values out of the tiles and adds them in the rows that see their key: slowly, but it
   // costs the other calls one look at the result.
-  if (sizeof(T) == 2 || block_all < seen) {
+  if (sizeof(T) == 2 || kWin || block_all < seen) {
     if (__syncthreads_or(live && rs.odd())) {  // (also: the tiles' last reads are done)
       begin();
 #pragma unroll 1
       for (int t = t0; t < t1; ++t) {
-        const int key0 = t * kTileKeys;
+        const int key0 = key_tile(t);
         if (tid == 0) odd_keys = 0;
         dma_tile(kbuf[0], kp + (int64_t)key0 * kD, keys - key0, from, wave);
         dma_tile(vbuf[0], vp + (int64_t)key0 * kD, keys - key0, from, wave);
         dma_wait();
         __syncthreads();
-        const uint64_t mine = take_nonfinite<T>(vbuf[0], tid);
+        const uint64_t mine = take_nonfinite<T, 256>(vbuf[0], tid);
         if (mine) atomicOr((unsigned long long*)&odd_keys, (unsigned long long)mine);
         __syncthreads();
         Tl::template scores<false>(kbuf[0], q, lane, S);
@@ -239,7 +205,14 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kern
 #pragma unroll
             for (int i = 0; i < 16; ++i)
               S[x][i] = __builtin_amdgcn_exp2f(fmaf(S[x][i], c, -ref));
-          add_nonfinite(odd, vp, key0, limit, S, lane, rs.O);
+          const int lo = limit - a.window;
+          add_nonfinite(
+              odd, [&](int key, int d) { return (float)vp[(int64_t)(key0 + key) * kD + d]; },
+              [&](int key) {
+                key += key0;
+                return key < limit && (!kWin || key >= lo || key < sink);
+              },
+              S, lane, rs.O);
         }
         __syncthreads();
       }
@@ -266,12 +239,18 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kern
     }
 }
 
-hipError_t launch_attend_dense(const AttendLaunch& a) {
-  if (a.dtype == SWAN_F32)
-    hipLaunchKernelGGL(attend_dense_kernel<float>, dim3(a.units), dim3(256), 0, a.stream, a);
+template <typename T>
+static hipError_t launch_dense_t(const AttendLaunch& a) {
+  const dim3 grid(a.units), block(256);
+  if (a.window > 0)
+    hipLaunchKernelGGL((attend_dense_kernel<T, true>), grid, block, 0, a.stream, a);
   else
-    hipLaunchKernelGGL(attend_dense_kernel<_Float16>, dim3(a.units), dim3(256), 0, a.stream, a);
+    hipLaunchKernelGGL((attend_dense_kernel<T, false>), grid, block, 0, a.stream, a);
   return hipGetLastError();
+}
+
+hipError_t launch_attend_dense(const AttendLaunch& a) {
+  return a.dtype == SWAN_F32 ? launch_dense_t<float>(a) : launch_dense_t<_Float16>(a);
 }
 
 }  // namespace swan

@@ -134,8 +134,49 @@ __device__ __forceinline__ float row_queries(const float* qr, bool live, int lan
   return c;
 }
 
+// The least / largest v of a wave
+template <bool kMax>
+__device__ __forceinline__ int wave_pick(int v) {
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) {
+    const int o = __shfl_xor(v, d, 64);
+    v = kMax ? max(v, o) : min(v, o);
+  }
+  return __builtin_amdgcn_readfirstlane(v);
+}
+
+// With a sliding window: the tiles of a source that some row of a row tile sees.
+struct Seen {
+  int skip, sink_tiles, nt;  // page tiles before the window; of these with first keys; tiles
+  // tok_a .. tok_b: the row tile's tokens.  L tokens are cached, in np pages (S of them) and
+  // ring tiles.
+  __device__ __forceinline__ void find(const AttendLaunch& a, const Tokens& tokens, int j, int tok_a,
+                                  int tok_b, int L, int S, int np, int ring_tiles, int lane) {
+    // lane l has list entry l: the first key of its first row in the tile, and its first keys
+    const int next = __shfl_down(tokens.tok0, 1, 64);  // (by every lane: each is read from)
+    const int end = lane + 1 >= a.first[j + 1] ? a.toks[j] : next;
+    const bool mine = lane >= a.first[j] && lane < a.first[j + 1] && tokens.tok0 <= tok_b &&
+                      end > tok_a;
+    const int lo = wave_pick<false>(mine ? a.lo[lane] + max(0, tok_a - tokens.tok0) : INT32_MAX);
+    const int sink = wave_pick<true>(mine ? (int)a.sink[lane] : 0);
+    skip = lo >= S ? np : max(0, lo) / kTileKeys;
+    sink_tiles = min((min(sink, S) + kTileKeys - 1) / kTileKeys, skip);
+    nt = np - skip + sink_tiles + (lo < L || sink > S ? ring_tiles : 0);
+  }
+  // the page or ring tile that the t-th of these is
+  __device__ __forceinline__ int tile(int t) const { return t < sink_tiles ? t : t - sink_tiles + skip; }
+};
+
+// The tokens of a tile: `count` keys (more: all), key `at` being token key0 + at, from at =
+// turn on `wrap` less.
+struct Span {
+  int count, key0, turn, wrap;
+  __device__ __forceinline__ int token(int at) const { return key0 + at - (at >= turn ? wrap : 0); }
+  __device__ __forceinline__ int least() const { return wrap ? key0 + turn - wrap : key0; }
+};
+
 // A wave's 32 query rows, and their products with a tile
-template <typename E, int W>
+template <typename E, int W, bool kWin>
 struct QueryRows {
   using Tl = Tile<E>;
   int64_t row;
@@ -143,6 +184,8 @@ struct QueryRows {
   float c;
   typename Tl::template Q<true> q;
   RowState<E> rs;
+  int lo, sink;        // with a window: this lane's row sees no key from `sink` to `lo`
+  int full, all_sink;  // the largest lo, the least sink of the wave's rows
 
   __device__ __forceinline__ QueryRows(const AttendLaunch& a, const Unit& un, const Tokens& tokens,
                                       int wave, int lane) {
@@ -151,29 +194,64 @@ struct QueryRows {
     const int tok = (int)a.by_g.of(r), g = (int)(r - (uint32_t)tok * (uint32_t)G);
     live = tok < toks;
     busy = (int)a.by_g.of(un.tile * (32 * W) + 32 * wave) < toks;
-    int b, i;
-    tokens.at(a, un.j, live ? tok : 0, b, i);
+    int e, b, i;
+    tokens.at(a, un.j, live ? tok : 0, e, b, i);
     row = ((int64_t)b * a.Hq + un.h * G + g) * a.n + i;
     c = row_queries<E>((const float*)a.q + row * kD, live, lane, q);
     rs.clear();
+    if constexpr (kWin) {
+      lo = a.lo[e] + i;
+      sink = a.sink[e];
+      full = wave_pick<true>(live ? lo : INT32_MIN);
+      all_sink = wave_pick<false>(live ? sink : INT32_MAX);
+    }
   }
-  // one tile, of `count` keys (more: all); kOdd: with infinite values, as in Tile::values
-  template <bool kOdd>
-  __device__ __forceinline__ void tile(const char* kb, const char* vb, int count, int lane) {
-    f16v S[2];
+  // scores of a tile
+  __device__ __forceinline__ void scores(const char* kb, const Span& sp, int lane, f16v (&S)[2]) {
     // (products first, where the other workgroup's wave has exponentials to do)
     if constexpr (W == 4) __builtin_amdgcn_s_setprio(1);
     Tl::template scores<true>(kb, q, lane, S);
     if constexpr (W == 4) __builtin_amdgcn_s_setprio(0);
-    if (count < kTileKeys) {
+    if (sp.count < kTileKeys) {
 #pragma unroll
       for (int x = 0; x < 2; ++x)
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          if (key_of(x, e, lane) >= count) S[x][e] = -INFINITY;
+          if (key_of(x, e, lane) >= sp.count) S[x][e] = -INFINITY;
+    }
+    if constexpr (kWin) {
+      if (sp.least() < full && (sp.wrap || sp.key0 + kTileKeys > all_sink)) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (!sees(sp.token(key_of(x, e, lane)))) S[x][e] = -INFINITY;
+      }
     }
     rs.raise(tile_max(S) * c);
+  }
+  __device__ __forceinline__ bool sees(int token) const { return token >= lo || token < sink; }
+  // one tile; kOdd: with infinite values, as in Tile::values
+  template <bool kOdd>
+  __device__ __forceinline__ void tile(const char* kb, const char* vb, const Span& sp, int lane) {
+    f16v S[2];
+    scores(kb, sp, lane, S);
     rs.l += Tl::template values<false, kOdd>(vb, S, c, rs.safe_ref(), lane, rs.O, kb, q, S);
+  }
+  // one tile without the values that are no numbers of the tokens odd; those: value(key, dim)
+  template <typename V>
+  __device__ __forceinline__ void apart(const char* kb, const char* vb, const Span& sp,
+                                        uint64_t odd, int lane, V value) {
+    f16v S[2], P[2];
+    scores(kb, sp, lane, S);
+    const float ref = rs.safe_ref();
+    rs.l += Tl::template values<false, false>(vb, S, c, ref, lane, rs.O, kb, q, P);
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) P[x][e] = __builtin_amdgcn_exp2f(fmaf(S[x][e], c, -ref));
+    add_nonfinite(
+        odd, value, [&](int key) { return key < sp.count && sees(sp.token(key)); }, P, lane, rs.O);
   }
 };
 
@@ -196,7 +274,9 @@ struct QueryRows {
 // 44 % and 31 %.  Few rows: 32 tokens over 32768 keys 55 us, 1.9 TB/s of pages, MFMA 26 %; 4
 // tokens of 32 heads over 4095 keys 20 us, where workgroups start and load for longer than
 // they multiply.
-template <typename T, int NU, int W>
+//
+// kWin: with a sliding window, over the tiles that some row of the row tile sees (Seen).
+template <typename T, int NU, int W, bool kWin>
 __global__ __launch_bounds__(64 * W, sizeof(typename Fmt<T>::Elem) == 2 ? 2 : 1) void
 attend_pages_kernel(AttendLaunch a) {
   using E = typename Fmt<T>::Elem;
@@ -206,6 +286,7 @@ attend_pages_kernel(AttendLaunch a) {
   __shared__ struct alignas(1024) {
     char buf[2 * N][R::kTile];  // keys and values of N tiles
     int odd;                    // some row's sum is no number
+    uint64_t odd_keys;          // keys of a tile with values that are no numbers
   } sh;
   auto& buf = sh.buf;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -214,7 +295,18 @@ attend_pages_kernel(AttendLaunch a) {
   const Unit un = unit_at(a, blockIdx.x);
   const int j = un.j, h = un.h, L = a.keys[j], cs = a.cseq[j];
   const int S = L > a.bb ? L - a.bb : 0, np = pages_for(S), nb = L < a.bb ? L : a.bb;
-  const int nt = np + (nb + kTileKeys - 1) / kTileKeys;
+  const int ring_tiles = (nb + kTileKeys - 1) / kTileKeys;
+  Seen seen;
+  if constexpr (kWin) {
+    const uint32_t r0 = (uint32_t)un.tile * (32 * W);
+    seen.find(a, tokens, j, (int)a.by_g.of(r0),
+              min(a.toks[j] - 1, (int)a.by_g.of(r0 + 32 * W - 1)), L, S, np, ring_tiles, lane);
+  } else {
+    seen.nt = np + ring_tiles;
+  }
+  const int nt = seen.nt;
+  // the page or ring tile that the t-th one is
+  auto tile_at = [&](int t) { return kWin ? seen.tile(t) : t; };
   const int t0 = split_first(nt, un.split, un.nsplit);
   const int t1 = split_first(nt, un.split + 1, un.nsplit);
   const int nk = kpad_of(a.kact[0][j]) / 8, nv = kpad_of(a.kact[1][j]) / 8;
@@ -227,16 +319,18 @@ attend_pages_kernel(AttendLaunch a) {
   const DmaFrom<E> from = dma_from<E>(wave & 3, lane);
   PageStage<T, NU, W> st;
   // stage: the loads of tile t, where it is a page
-  auto stage = [&](int t) {
-    const bool page = t < t1 && t < np;
+  auto stage = [&](int x) {
+    const int t = tile_at(x);
+    const bool page = x < t1 && t < np;
     st.load(page ? kpages + t * kbytes : nullptr, page ? vpages + t * vbytes : nullptr, nk, nv, wave,
             lane);
   };
   // clear: zeros where tile t is a page, the ring's rows (true: to be waited for) where not
-  auto clear = [&](int t, int at) {
+  auto clear = [&](int x, int at) {
     char* kb = buf[at];
     char* vb = buf[N + at];
-    if (t >= t1) return false;
+    if (x >= t1) return false;
+    const int t = tile_at(x);
     if (t < np) {
       const u32x4 zero = {0u, 0u, 0u, 0u};
 #pragma unroll
@@ -257,13 +351,22 @@ attend_pages_kernel(AttendLaunch a) {
     return kAsync;
   };
   // scatter: what stage(t) loaded
-  auto scatter = [&](int t, int at) {
-    st.scatter(buf[at], buf[N + at], nk, nv, wave, lane, t < t1 && t * kPage + lane < S);
+  auto scatter = [&](int x, int at) {
+    st.scatter(buf[at], buf[N + at], nk, nv, wave, lane, x < t1 && tile_at(x) * kPage + lane < S);
   };
-  auto count = [&](int t) { return t < np ? S - t * kPage : nb - (t - np) * kTileKeys; };
+  QueryRows<E, W, kWin> rows(a, un, tokens, wave, lane);
+  // the tokens of the t-th tile; a ring's slot s is token L - L % bb + s, from slot L % bb on
+  // bb less (L <= bb: token s)
+  const int turn = kWin && L > a.bb && a.bb > 0 ? L % a.bb : 0;
+  auto span = [&](int x) {
+    const int t = tile_at(x), slot0 = (t - np) * kTileKeys;
+    const bool ring = t >= np, wrapped = ring && L > a.bb;
+    return Span{ring ? nb - slot0 : S - t * kPage,
+                !ring ? t * kPage : wrapped ? L - turn + slot0 : slot0,
+                wrapped ? turn - slot0 : kTileKeys, wrapped ? a.bb : 0};
+  };
   stage(t0);
 
-  QueryRows<E, W> rows(a, un, tokens, wave, lane);
   if (tid == 0) sh.odd = 0;
   // all tiles, of which the first is staged
   auto attend = [&](auto odd) {
@@ -282,7 +385,7 @@ attend_pages_kernel(AttendLaunch a) {
         __syncthreads();
         scatter(t + 1, par ^ 1);
         stage(t + 2);
-        if (rows.busy) rows.template tile<kOdd>(buf[par], buf[N + par], count(t), lane);
+        if (rows.busy) rows.template tile<kOdd>(buf[par], buf[N + par], span(t), lane);
         if (ring_tile) dma_wait();
         __syncthreads();
       }
@@ -297,7 +400,7 @@ attend_pages_kernel(AttendLaunch a) {
       };
       for (int t = t0; t < t1; ++t) {
         if (!late) prepare(t);
-        if (rows.busy) rows.template tile<kOdd>(buf[x0], buf[N + x0], count(t), lane);
+        if (rows.busy) rows.template tile<kOdd>(buf[x0], buf[N + x0], span(t), lane);
         if (late) prepare(t);
         __syncthreads();
         const int x = x0;
@@ -308,7 +411,39 @@ attend_pages_kernel(AttendLaunch a) {
     }
   };
   attend(std::false_type());
-  if constexpr (sizeof(E) == 2) {
+  if constexpr (kWin) {
+    // A value that is no number, of a token that only some rows see, makes NaNs of the other
+    // rows (0 times it), and an infinite one may of any row (its products with the parts of
+    // p): once more, one tile at a time, with such values out of the tile and added in the
+    // rows that see their token.
+    if (rows.live && rows.rs.odd()) sh.odd = 1;
+    __syncthreads();
+    if (sh.odd) {
+      rows.rs.clear();
+#pragma unroll 1
+      for (int t = t0; t < t1; ++t) {
+        if (tid == 0) sh.odd_keys = 0;
+        stage(t);
+        const bool ring_tile = clear(t, 0);
+        __syncthreads();
+        scatter(t, 0);
+        if (ring_tile) dma_wait();
+        __syncthreads();
+        const u32x4* from = (const u32x4*)buf[N];
+        for (int x = tid; x < R::kTile / 16; x += 64 * W) ((u32x4*)buf[N + 1])[x] = from[x];
+        __syncthreads();
+        const uint64_t mine = take_nonfinite<E, 64 * W>(buf[N], tid);
+        if (mine) atomicOr((unsigned long long*)&sh.odd_keys, (unsigned long long)mine);
+        __syncthreads();
+        const SWAN_LDS char* raw = (const SWAN_LDS char*)(SWAN_LDS char*)buf[N + 1];
+        if (rows.busy)
+          rows.apart(buf[0], buf[N], span(t), sh.odd_keys, lane, [&](int key, int d) {
+            return (float)*(const SWAN_LDS E*)(raw + R::at(key, d));
+          });
+        __syncthreads();
+      }
+    }
+  } else if constexpr (sizeof(E) == 2) {
     // An infinite value's products with the parts of p may have made NaNs: once more, with
     // care.  (The barrier is also behind the tiles' last reads.)
     if (rows.live && rows.rs.odd()) sh.odd = 1;
@@ -322,7 +457,7 @@ attend_pages_kernel(AttendLaunch a) {
   write_partial(a, rows.rs, rows.row, un.split, rows.live, lane);
 }
 
-template <typename T>
+template <typename T, bool kWin>
 static hipError_t launch_pages_t(const AttendLaunch& a) {
   // registers for the groups that a wave has in flight: those of up to 128 components in both
   // roles, or of 256 (4 tokens of 32 heads over 4095 keys, k = 48: 35.7 us with room for 128
@@ -336,22 +471,27 @@ static hipError_t launch_pages_t(const AttendLaunch& a) {
   if (a.tile_rows > kTileRows) {
     if constexpr (sizeof(typename Fmt<T>::Elem) == 2) {
       if (most <= 16)
-        hipLaunchKernelGGL((attend_pages_kernel<T, 2, 8>), grid, eight, 0, a.stream, a);
+        hipLaunchKernelGGL((attend_pages_kernel<T, 2, 8, kWin>), grid, eight, 0, a.stream, a);
       else
-        hipLaunchKernelGGL((attend_pages_kernel<T, 4, 8>), grid, eight, 0, a.stream, a);
+        hipLaunchKernelGGL((attend_pages_kernel<T, 4, 8, kWin>), grid, eight, 0, a.stream, a);
     }
   } else if (most <= 16) {
-    hipLaunchKernelGGL((attend_pages_kernel<T, 4, 4>), grid, four, 0, a.stream, a);
+    hipLaunchKernelGGL((attend_pages_kernel<T, 4, 4, kWin>), grid, four, 0, a.stream, a);
   } else {
-    hipLaunchKernelGGL((attend_pages_kernel<T, 8, 4>), grid, four, 0, a.stream, a);
+    hipLaunchKernelGGL((attend_pages_kernel<T, 8, 4, kWin>), grid, four, 0, a.stream, a);
   }
   return hipGetLastError();
 }
 
+template <bool kWin>
+static hipError_t launch_pages_w(const AttendLaunch& a) {
+  if (a.dtype == SWAN_F32) return launch_pages_t<float, kWin>(a);
+  if (a.dtype == SWAN_F16_E4M3) return launch_pages_t<E4M3V, kWin>(a);
+  return launch_pages_t<_Float16, kWin>(a);
+}
+
 hipError_t launch_attend_pages(const AttendLaunch& a) {
-  if (a.dtype == SWAN_F32) return launch_pages_t<float>(a);
-  if (a.dtype == SWAN_F16_E4M3) return launch_pages_t<E4M3V>(a);
-  return launch_pages_t<_Float16>(a);
+  return a.window > 0 ? launch_pages_w<true>(a) : launch_pages_w<false>(a);
 }
 
 }  // namespace swan

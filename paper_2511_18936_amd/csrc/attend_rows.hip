@@ -266,7 +266,7 @@ __global__ __launch_bounds__(256) void join_rows_kernel(JoinLaunch a) {
 template <typename T>
 static hipError_t launch_join_t(const JoinLaunch& a) {
   const int64_t rows = (int64_t)a.B * a.H * a.n;
-  if (a.own)
+  if (a.decode)
     hipLaunchKernelGGL(join_decode_kernel<T>, dim3((unsigned)rows), dim3(kJoinThreads), 0, a.stream,
                        a);
   else

@@ -13,7 +13,7 @@
 // have a row and 4 pairs each, and the sines are shared by the heads; 3 x 517 positions of
 // 12 + 2 x 4 float32 heads 9.6 us.  Single tokens (4 x 48 heads) 3 us, the chain of pow and
 // sincos.
-#include "swan_cache_ops.h"
+#include "rotary.h"
 #include "swan_layer_ops.h"
 
 namespace swan {
@@ -97,24 +97,37 @@ __device__ __forceinline__ double row_sum(double v) {
 
 constexpr int kTilePos = 4;  // positions of a workgroup
 
+// the weights of a lane's pairs: of the first elements, then of the second
+template <typename T, int kForm>
+__device__ __forceinline__ void pair_weights(const QkvRowsLaunch& a, int role, int64_t head,
+                                             int at0, int at1, double (&w)[8]) {
+  weights_at<T>(a, role, head + at0, *(double(*)[4])w);
+  weights_at<T>(a, role, head + at1, *(double(*)[4])(w + 4));
+  to_pairs<kForm, 4>(*(double(*)[4])w, *(double(*)[4])(w + 4));
+}
+
 template <typename T>
 struct alignas(4 * sizeof(T)) Four {
   T v[4];
 };
 
-// One row's 4 + 4 elements of a lane (of 16): norm with weights w (NULL: none), rotation
-template <typename T>
-__device__ __forceinline__ void turn_row(Four<T>& lo, Four<T>& hi, const double* w, double eps,
-                                         const double (&c)[4], const double (&s)[4]) {
+// One row's 4 + 4 elements of a lane (of 16): norm with weights w, rotation (unless the lane's
+// pairs are left as they are: !turn)
+template <typename T, int kForm>
+__device__ __forceinline__ void turn_row(Four<T>& lo, Four<T>& hi, bool norm,
+                                         const double (&w)[8], double eps, const double (&c)[4],
+                                         const double (&s)[4], bool turn) {
   double x0[4], x1[4];
   bool nan = false;
+  const Four<T> was0 = lo, was1 = hi;
+  to_pairs<kForm, 4>(lo.v, hi.v);
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     x0[e] = (double)(float)lo.v[e];
     x1[e] = (double)(float)hi.v[e];
     nan |= __builtin_isunordered((float)lo.v[e], (float)hi.v[e]);
   }
-  if (w) {
+  if (norm) {
     double ss = 0.0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) ss += x0[e] * x0[e] + x1[e] * x1[e];
@@ -128,8 +141,9 @@ __device__ __forceinline__ void turn_row(Four<T>& lo, Four<T>& hi, const double*
   }
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    lo.v[e] = stored<T>(x0[e] * c[e] - x1[e] * s[e]);
-    hi.v[e] = stored<T>(x1[e] * c[e] + x0[e] * s[e]);
+    const double y0 = x0[e] * c[e] - x1[e] * s[e], y1 = x1[e] * c[e] + x0[e] * s[e];
+    lo.v[e] = stored<T>(kForm == 0 || turn ? y0 : x0[e]);
+    hi.v[e] = stored<T>(kForm == 0 || turn ? y1 : x1[e]);
   }
   if (nan)
 #pragma unroll
@@ -137,28 +151,36 @@ __device__ __forceinline__ void turn_row(Four<T>& lo, Four<T>& hi, const double*
       one_nan_of(lo.v[e]);
       one_nan_of(hi.v[e]);
     }
+  from_pairs<kForm, 4>(lo.v, hi.v);
+  if (kForm != 0 && !turn && !norm) {
+    lo = was0;
+    hi = was1;
+  }
 }
 
 // A workgroup takes 4 positions at a time and `heads` of their heads (grid: positions,
 // chunks of heads): its 256 threads compute the 4 x 64 sines and cosines once for all of
 // them, then a quarter wave (16 lanes of 4 pairs, 8-byte accesses for binary16) has a head's
 // row of one position, wave w every fourth head, two at a time.
-template <typename T>
-__global__ __launch_bounds__(256) void qkv_rows_kernel(QkvRowsLaunch a, int heads) {
+template <typename T, int kForm>
+__global__ __launch_bounds__(256) void qkv_rows_kernel(QkvRowsLaunch a, int heads,
+                                                       FormArg<kForm> f) {
   __shared__ f64x2 cs[kTilePos][kD / 2];
   using Vec = Four<T>;
   const int t = threadIdx.x, wave = t >> 6, p = (t >> 4) & 3, l = t & 15;
   const int h0 = blockIdx.y * heads, h1 = min(a.Hq + 2 * a.Hkv, h0 + heads);
   const uint32_t n = (uint32_t)a.n, positions = (uint32_t)a.B * n;  // below 2^31
   const uint32_t tiles = (positions + kTilePos - 1) / kTilePos;
-  const double freq = pow(a.base, -(2.0 * (t & 63)) / kD);
+  const double freq = pair_freq<kForm>(f, a.base, t & 63);
+  const bool turn = turned<kForm>(f, 4 * l);
+  const int at0 = place<kForm, 4>(f, 4 * l, false), at1 = place<kForm, 4>(f, 4 * l, true);
   for (uint32_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
     {
       const uint32_t at = tile * kTilePos + wave;
       if (at < positions) {
         const uint32_t b = at / n;
         double s, c;
-        sincos(((double)a.pos0[b] + (double)(at - b * n)) * freq, &s, &c);
+        pair_turn<kForm>(f, ((double)a.pos0[b] + (double)(at - b * n)) * freq, s, c);
         cs[wave][t & 63] = f64x2{c, s};
       }
     }
@@ -166,7 +188,7 @@ __global__ __launch_bounds__(256) void qkv_rows_kernel(QkvRowsLaunch a, int head
     const uint32_t at = tile * kTilePos + p;
     if (at < positions) {
       const int b = (int)(at / n), i = (int)(at - b * n);
-      const T* row = (const T*)a.x + b * a.seq + i * a.row + 4 * l;
+      const T* row = (const T*)a.x + b * a.seq + i * a.row;
       double c[4], s[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -178,37 +200,35 @@ __global__ __launch_bounds__(256) void qkv_rows_kernel(QkvRowsLaunch a, int head
 #pragma unroll
       for (int role = 0; role < 3; ++role) {
         const int count = role == 0 ? a.Hq : a.Hkv, last = min(first + count, h1);
-        T* out = (T*)a.out[role] + (((int64_t)b * count - first) * a.n + i) * kD + 4 * l;
+        T* out = (T*)a.out[role] + (((int64_t)b * count - first) * a.n + i) * kD;
         const bool norm = role < 2 && a.w[role] != nullptr;
-        double w[8];
+        double w[8] = {};
         if (norm && a.wstep == 0) {
-          weights_at<T>(a, role, 4 * l, *(double(*)[4])w);
-          weights_at<T>(a, role, 4 * l + kD / 2, *(double(*)[4])(w + 4));
+          pair_weights<T, kForm>(a, role, 0, at0, at1, w);
         }
         // the first of this wave's heads that is the chunk's and this role's
         for (int h = max(first, h0) + wave; h < last; h += 8) {
           const bool two = h + 4 < last;
           Vec lo[2], hi[2];
-          lo[0] = *(const Vec*)(row + h * kD);
-          hi[0] = *(const Vec*)(row + h * kD + kD / 2);
+          lo[0] = *(const Vec*)(row + h * kD + at0);
+          hi[0] = *(const Vec*)(row + h * kD + at1);
           if (two) {
-            lo[1] = *(const Vec*)(row + (h + 4) * kD);
-            hi[1] = *(const Vec*)(row + (h + 4) * kD + kD / 2);
+            lo[1] = *(const Vec*)(row + (h + 4) * kD + at0);
+            hi[1] = *(const Vec*)(row + (h + 4) * kD + at1);
           }
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
             if (x == 1 && !two) break;
             if (role < 2) {
               if (norm && a.wstep) {
-                const int64_t at = (int64_t)(h + 4 * x - first) * a.wstep + 4 * l;
-                weights_at<T>(a, role, at, *(double(*)[4])w);
-                weights_at<T>(a, role, at + kD / 2, *(double(*)[4])(w + 4));
+                pair_weights<T, kForm>(a, role, (int64_t)(h + 4 * x - first) * a.wstep, at0, at1,
+                                       w);
               }
-              turn_row<T>(lo[x], hi[x], norm ? w : nullptr, a.eps, c, s);
+              turn_row<T, kForm>(lo[x], hi[x], norm, w, a.eps, c, s, turn);
             }
             T* to = out + (int64_t)(h + 4 * x) * a.n * kD;
-            *(Vec*)to = lo[x];
-            *(Vec*)(to + kD / 2) = hi[x];
+            *(Vec*)(to + at0) = lo[x];
+            *(Vec*)(to + at1) = hi[x];
           }
         }
         first += count;
@@ -220,47 +240,51 @@ __global__ __launch_bounds__(256) void qkv_rows_kernel(QkvRowsLaunch a, int head
 
 // Few rows: a wave per (position, head), lane l the pair (l, l + 64); the row and its
 // weights are loaded before the chain of pow and sincos, which bounds it.
-template <typename T>
-__global__ __launch_bounds__(64) void qkv_rows_few_kernel(QkvRowsLaunch a) {
+template <typename T, int kForm>
+__global__ __launch_bounds__(64) void qkv_rows_few_kernel(QkvRowsLaunch a, FormArg<kForm> f) {
   const int l = threadIdx.x, i = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
-  const T* row = (const T*)a.x + b * a.seq + i * a.row + (int64_t)h * kD + l;
-  const T lo = row[0], hi = row[kD / 2];
+  const bool turn = turned<kForm>(f, l);
+  const int at0 = place<kForm, 1>(f, l, false), gap = place<kForm, 1>(f, l, true) - at0;
+  const T* row = (const T*)a.x + b * a.seq + i * a.row + (int64_t)h * kD + at0;
+  const T lo = row[0], hi = row[gap];
   const int role = h < a.Hq ? 0 : h < a.Hq + a.Hkv ? 1 : 2;
   const int hr = role == 0 ? h : role == 1 ? h - a.Hq : h - a.Hq - a.Hkv;
-  T* to = (T*)a.out[role] + (((int64_t)b * (role == 0 ? a.Hq : a.Hkv) + hr) * a.n + i) * kD + l;
-  if (role == 2) {
+  T* to = (T*)a.out[role] + (((int64_t)b * (role == 0 ? a.Hq : a.Hkv) + hr) * a.n + i) * kD + at0;
+  if (role == 2 || (kForm != 0 && !turn && !a.w[role])) {
     to[0] = lo;
-    to[kD / 2] = hi;
+    to[gap] = hi;
     return;
   }
   double x0 = (double)(float)lo, x1 = (double)(float)hi;
   bool nan = x0 != x0 || x1 != x1;
   if (a.w[role]) {
     double w0[1], w1[1];
-    weights_at<T>(a, role, (int64_t)hr * a.wstep + l, w0);
-    weights_at<T>(a, role, (int64_t)hr * a.wstep + l + kD / 2, w1);
+    weights_at<T>(a, role, (int64_t)hr * a.wstep + at0, w0);
+    weights_at<T>(a, role, (int64_t)hr * a.wstep + at0 + gap, w1);
     const double r = inv_root<T>(row_sum<64>(x0 * x0 + x1 * x1) * (1.0 / kD) + a.eps);
     x0 *= r * w0[0];
     x1 *= r * w1[0];
     nan |= !(r - r == 0.0);
   }
   double s, c;
-  sincos(((double)a.pos0[b] + (double)i) * pow(a.base, -(2.0 * l) / kD), &s, &c);
-  T y = stored<T>(x0 * c - x1 * s), z = stored<T>(x1 * c + x0 * s);
+  pair_turn<kForm>(f, ((double)a.pos0[b] + (double)i) * pair_freq<kForm>(f, a.base, l), s, c);
+  const double y0 = x0 * c - x1 * s, y1 = x1 * c + x0 * s;
+  T y = stored<T>(kForm == 0 || turn ? y0 : x0), z = stored<T>(kForm == 0 || turn ? y1 : x1);
   if (nan) {
     one_nan_of(y);
     one_nan_of(z);
   }
   to[0] = y;
-  to[kD / 2] = z;
+  to[gap] = z;
 }
 
-template <typename T>
-static hipError_t launch_qkv_rows_t(const QkvRowsLaunch& a) {
+template <typename T, int kForm>
+static hipError_t launch_qkv_rows_t(const QkvRowsLaunch& a, const FormArg<kForm>& f) {
   const int64_t positions = (int64_t)a.B * a.n;
   const int H = a.Hq + 2 * a.Hkv;
   if (positions * H <= 4096 && H <= 65535) {
-    hipLaunchKernelGGL(qkv_rows_few_kernel<T>, dim3(a.n, H, a.B), dim3(64), 0, a.stream, a);
+    hipLaunchKernelGGL((qkv_rows_few_kernel<T, kForm>), dim3(a.n, H, a.B), dim3(64), 0, a.stream, a,
+                       f);
     return hipGetLastError();
   }
   // Few positions split their heads, 4 at least to each, over 768 workgroups: fewer leave
@@ -273,12 +297,19 @@ static hipError_t launch_qkv_rows_t(const QkvRowsLaunch& a) {
   chunks = chunks < 1 ? 1 : chunks > (H + 3) / 4 ? (H + 3) / 4 : chunks;
   const int heads = (int)(((H + chunks - 1) / chunks + 3) / 4 * 4);
   const dim3 grid((unsigned)(tiles < 2048 ? tiles : 2048), (unsigned)((H + heads - 1) / heads));
-  hipLaunchKernelGGL(qkv_rows_kernel<T>, grid, dim3(256), 0, a.stream, a, heads);
+  hipLaunchKernelGGL((qkv_rows_kernel<T, kForm>), grid, dim3(256), 0, a.stream, a, heads, f);
   return hipGetLastError();
 }
 
-hipError_t launch_qkv_rows(const QkvRowsLaunch& a) {
-  return a.dtype == SWAN_F32 ? launch_qkv_rows_t<float>(a) : launch_qkv_rows_t<_Float16>(a);
+template <typename T>
+static hipError_t launch_qkv_rows_form(const QkvRowsLaunch& a, const RotaryForm* f) {
+  if (!f) return launch_qkv_rows_t<T, 0>(a, WholeHead());
+  return f->interleaved ? launch_qkv_rows_t<T, 2>(a, *f) : launch_qkv_rows_t<T, 1>(a, *f);
+}
+
+hipError_t launch_qkv_rows(const QkvRowsLaunch& a, const RotaryForm* form) {
+  return a.dtype == SWAN_F32 ? launch_qkv_rows_form<float>(a, form)
+                             : launch_qkv_rows_form<_Float16>(a, form);
 }
 
 }  // namespace swan

@@ -11,9 +11,7 @@
 #include <string>
 
 #include "swan.h"
-#include "swan_cache_ops.h"
-#include "swan_layer.h"
-#include "swan_layer_ops.h"
+#include "swan_host.h"
 
 // ---------------------------------------------------------------------------
 // Scratch of swan_decode_attention_noalloc: the decode workspace (q_hat, then
@@ -25,8 +23,9 @@
 constexpr size_t kScratchBytes = SWAN_NOALLOC_SCRATCH_BYTES;
 static __device__ __align__(256) char scratch[kScratchBytes];
 
-namespace {
+namespace swan_host {
 
+namespace {
 thread_local std::string g_last_error;
 thread_local hipEvent_t g_prof_start = nullptr;
 thread_local hipEvent_t g_prof_stop = nullptr;
@@ -42,6 +41,7 @@ struct Tuning {
   int side_streams = swan::kSideStreams;
 };
 thread_local Tuning g_tuning;
+}  // namespace
 
 swan_status fail(swan_status st, const char* fmt, ...) {
   char buf[512];
@@ -105,11 +105,6 @@ swan_status check_k(const swan_cache* c, const int32_t* k_active_host,
       return fail(SWAN_ERR_INVALID_ARG, "k_value[%d] = %d outside 1..%d", b, kv, c->head_dim);
   }
   return SWAN_OK;
-}
-
-// k of role r (0 keys, 1 values) of sequence b
-inline int k_of(const int32_t* k_active_host, const int32_t* k_value_host, int r, int b) {
-  return (r == 1 && k_value_host) ? k_value_host[b] : k_active_host[b];
 }
 
 swan_status check_cache_ptrs(const swan_cache* c) {
@@ -575,8 +570,11 @@ int key_tiles(const swan_cache* c, int L) {
 // Groups and splits of a source: one group per cache sequence with tokens and query rows.
 // Every split has a tile; used[b] = splits of query
 // sequence b's group (0: none).  Returns the largest.
+// before[b], pos[b]: with a window, the position of the source's first token, and of query
+// sequence b's first row.
 int plan_pages(const swan_prefix* s, int32_t batch, int32_t n, const int32_t* n_host,
-               swan::AttendLaunch& a, int16_t* used) {
+               const Window& w, const int32_t* before, const int32_t* pos, swan::AttendLaunch& a,
+               int16_t* used) {
   const swan_cache* c = s->cache;
   const int G = c->n_q_heads / c->n_kv_heads;
   swan::SeqTab tab;
@@ -595,6 +593,10 @@ int plan_pages(const swan_prefix* s, int32_t batch, int32_t n, const int32_t* n_
       if (s->of_host[b] != p || nb == 0) continue;
       a.seq[entries] = (uint8_t)b;
       a.tok0[entries] = (int32_t)toks;
+      if (w.window > 0) {
+        a.lo[entries] = pos[b] - before[b] - w.window + 1;
+        a.sink[entries] = (uint16_t)(w.sinks > before[b] ? w.sinks - before[b] : 0);
+      }
       ++entries;
       toks += nb;
     }
@@ -610,12 +612,24 @@ int plan_pages(const swan_prefix* s, int32_t batch, int32_t n, const int32_t* n_
     many |= c->dtype != SWAN_F32 && toks * G > swan::kTileRows;
     ++a.groups;
   }
-  a.first[a.groups] = entries;
   int tiles[SWAN_MAX_BATCH];
   int64_t base[SWAN_MAX_BATCH], wide[SWAN_MAX_BATCH], rows = 0;  // row tiles x kv heads
+  a.first[a.groups] = entries;
   for (int j = 0; j < a.groups; ++j) {
     const int64_t r = (int64_t)a.toks[j] * G;
     tiles[j] = key_tiles(c, a.keys[j]);
+    if (w.window > 0) {  // (the most that a row tile has: Seen::find of all rows)
+      const int L = a.keys[j], S = L > c->buffer_tokens ? L - c->buffer_tokens : 0;
+      int lo = INT32_MAX, sink = 0;
+      for (int e = a.first[j]; e < a.first[j + 1]; ++e) {
+        lo = a.lo[e] < lo ? a.lo[e] : lo;
+        sink = a.sink[e] > sink ? a.sink[e] : sink;
+      }
+      const int skip = lo >= S ? swan::pages_for(S) : (lo > 0 ? lo : 0) / swan::kPage;
+      const int sink_tiles = swan::pages_for(sink < S ? sink : S);
+      tiles[j] -= skip - (sink_tiles < skip ? sink_tiles : skip);
+      if (tiles[j] < 1) tiles[j] = 1;
+    }
     base[j] = (r + swan::kTileRows - 1) / swan::kTileRows * c->n_kv_heads;
     wide[j] = (r + swan::kManyRows - 1) / swan::kManyRows * c->n_kv_heads;
     rows += (int64_t)a.toks[j] * c->n_q_heads;
@@ -662,18 +676,19 @@ int plan_pages(const swan_prefix* s, int32_t batch, int32_t n, const int32_t* n_
   a.out = nullptr;
   a.qmult = 0.f;
   a.m = a.causal = 0;
+  a.window = w.window;
   return most;
 }
 
-struct AttendPlan {
-  swan::AttendLaunch a[2];
-  int16_t used[2][SWAN_MAX_BATCH];
-  int base[2], slots;
-  size_t qhat, bytes;  // bytes of q_hat; of the workspace
-};
+swan_status check_window(int32_t window, int32_t sinks) {
+  if (window < 1) return fail(SWAN_ERR_INVALID_ARG, "window %d < 1", window);
+  if (sinks < 0 || sinks > swan::kMaxSinks)
+    return fail(SWAN_ERR_INVALID_ARG, "sinks %d outside 0..%d", sinks, swan::kMaxSinks);
+  return SWAN_OK;
+}
 
 swan_status attend_prep(const swan_prefix* sources, int32_t n_sources, int32_t batch, int32_t n,
-                        const int32_t* n_host, bool need_ptrs, AttendPlan& pl) {
+                        const int32_t* n_host, bool need_ptrs, AttendPlan& pl, const Window& w) {
   if (!sources || n_sources < 1 || n_sources > 2)
     return fail(SWAN_ERR_INVALID_ARG, "sources is NULL, or n_sources %d outside 1..2", n_sources);
   if (batch < 1 || batch > SWAN_MAX_BATCH)
@@ -692,11 +707,24 @@ swan_status attend_prep(const swan_prefix* sources, int32_t n_sources, int32_t b
   if ((int64_t)batch * c->n_q_heads * n > INT32_MAX)
     return fail(SWAN_ERR_UNSUPPORTED, "%d sequences x %d heads x %d rows: above 2^31 - 1", batch,
                 c->n_q_heads, n);
+  // positions: the first source's tokens, the second's, the rows
+  int32_t before[2][SWAN_MAX_BATCH] = {}, pos[SWAN_MAX_BATCH] = {};
+  for (int b = 0; w.window > 0 && b < batch; ++b) {
+    int64_t at = 0;
+    for (int s = 0; s < n_sources; ++s) {
+      before[s][b] = (int32_t)at;
+      if (sources[s].of_host[b] >= 0) at += sources[s].seq_len_host[sources[s].of_host[b]];
+    }
+    if (at + n > INT32_MAX)
+      return fail(SWAN_ERR_UNSUPPORTED, "sequence %d: %lld cached tokens and %d rows: above 2^31 - 1",
+                  b, (long long)at, n);
+    pos[b] = w.pos ? w.pos[b] : (int32_t)at;
+  }
   pl.slots = 0;
   for (int s = 0; s < 2; ++s) {
     pl.base[s] = pl.slots;
     if (s < n_sources) {
-      pl.slots += plan_pages(&sources[s], batch, n, n_host, pl.a[s], pl.used[s]);
+      pl.slots += plan_pages(&sources[s], batch, n, n_host, w, before[s], pos, pl.a[s], pl.used[s]);
       if (pl.a[s].units < 0) return fail(SWAN_ERR_UNSUPPORTED, "too many rows for one call");
     } else {
       pl.a[s].groups = 0;
@@ -709,16 +737,9 @@ swan_status attend_prep(const swan_prefix* sources, int32_t n_sources, int32_t b
   return SWAN_OK;
 }
 
-// plan of swan_prompt_attention
-struct PromptPlan {
-  swan::AttendLaunch a;
-  int16_t used[SWAN_MAX_BATCH];
-  size_t bytes;
-};
-
-swan_status prompt_prep(int32_t dtype, int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t n, int32_t m,
-                        int32_t head_dim, const int32_t* n_host, const int32_t* m_host,
-                        int32_t causal, PromptPlan& pl) {
+swan_status prompt_prep(int32_t dtype, int32_t batch, int32_t n_q_heads, int32_t n_kv_heads,
+                        int32_t n, int32_t m, int32_t head_dim, const int32_t* n_host, const int32_t* m_host,
+                        int32_t causal, PromptPlan& pl, int32_t window, const int32_t* sinks_host) {
   if (!dtype_ok(dtype)) return fail(SWAN_ERR_UNSUPPORTED, "dtype %d not supported", dtype);
   if (batch < 1 || batch > SWAN_MAX_BATCH)
     return fail(SWAN_ERR_INVALID_ARG, "batch %d outside 1..%d", batch, SWAN_MAX_BATCH);
@@ -732,6 +753,8 @@ swan_status prompt_prep(int32_t dtype, int32_t batch, int32_t n_q_heads, int32_t
   if (st != SWAN_OK) return st;
   if ((st = check_rows("m", m_host, batch, m)) != SWAN_OK) return st;
   if (causal != 0 && causal != 1) return fail(SWAN_ERR_INVALID_ARG, "causal %d", causal);
+  for (int b = 0; window > 0 && sinks_host && b < batch; ++b)
+    if ((st = check_window(window, sinks_host[b])) != SWAN_OK) return st;
   if ((int64_t)batch * n_q_heads * n > INT32_MAX)
     return fail(SWAN_ERR_UNSUPPORTED, "%d sequences x %d heads x %d rows: above 2^31 - 1", batch,
                 n_q_heads, n);
@@ -751,7 +774,7 @@ swan_status prompt_prep(int32_t dtype, int32_t batch, int32_t n_q_heads, int32_t
     order[at] = b;
   }
   int tiles[SWAN_MAX_BATCH];
-  int64_t base[SWAN_MAX_BATCH], rows = 0;
+  int64_t base[SWAN_MAX_BATCH], rows = 0, all = 0, seen = 0;
   for (int j = 0; j < count; ++j) {
     const int b = order[j];
     a.first[j] = j;
@@ -761,14 +784,23 @@ swan_status prompt_prep(int32_t dtype, int32_t batch, int32_t n_q_heads, int32_t
     a.toks[j] = n_host ? n_host[b] : n;
     a.keys[j] = m_host ? m_host[b] : m;
     tiles[j] = (a.keys[j] + swan::kTileKeys - 1) / swan::kTileKeys;
+    all += tiles[j];
+    if (window > 0) {  // the tiles that a row tile's windows and the first keys take at most
+      a.sink[j] = (uint16_t)(sinks_host ? sinks_host[b] : 0);
+      const int64_t most = ((int64_t)window + swan::kTileRows / G) / swan::kTileKeys + 2 +
+                           (a.sink[j] + swan::kTileKeys - 1) / swan::kTileKeys;
+      if (most < tiles[j]) tiles[j] = (int)most;
+    }
+    seen += tiles[j];
     base[j] = ((int64_t)a.toks[j] * G + swan::kTileRows - 1) / swan::kTileRows * n_kv_heads;
     rows += (int64_t)a.toks[j] * n_q_heads;
   }
   a.first[count] = count;
   a.groups = count;
   double cost;
-  const int per = plan_tiles(attend_cost(dtype, false), count, base, tiles, rows, causal != 0, false,
-                             cost);
+  // (windows that leave out half of a prompt's tiles make its row tiles alike)
+  const int per = plan_tiles(attend_cost(dtype, false), count, base, tiles, rows,
+                             causal != 0 && 2 * seen > all, false, cost);
   int64_t units = 0;
   int most = 1;
   for (int j = 0; j < count; ++j) {
@@ -790,6 +822,7 @@ swan_status prompt_prep(int32_t dtype, int32_t batch, int32_t n_q_heads, int32_t
   a.n = n;
   a.m = m;
   a.causal = causal;
+  a.window = window;
   a.slots = most;
   a.slot0 = 0;
   a.k_ring = a.v_ring = nullptr;
@@ -854,6 +887,7 @@ hipError_t launch_decode_prefix(swan::DecodeLaunch& da, AttendPlan& pl, void* wo
   j.n = 1;
   j.slots = pl.slots;
   j.dtype = da.dtype;
+  j.decode = 1;
   j.own_slots = da.n_splits;
   j.own = da.part;
   j.own_bb = da.bb;
@@ -868,7 +902,274 @@ hipError_t launch_decode_prefix(swan::DecodeLaunch& da, AttendPlan& pl, void* wo
   return swan::launch_join(j);
 }
 
-}  // namespace
+swan_status attend_run(const swan_prefix* sources, int32_t n_sources, int32_t batch, int32_t n,
+                       const int32_t* n_host, const Window& w, const void* q, const float* P_qk,
+                        const float* P_vo, float scale, float* o, float* lse, void* workspace,
+                        size_t workspace_bytes, void* stream) {
+  AttendPlan pl;
+  swan_status st = attend_prep(sources, n_sources, batch, n, n_host, true, pl, w);
+  if (st != SWAN_OK) return st;
+  if ((st = check_scale(scale)) != SWAN_OK) return st;
+  int32_t rows[SWAN_MAX_BATCH] = {};
+  bool any = false;
+  for (int b = 0; b < batch; ++b) {
+    rows[b] = n_host ? n_host[b] : n;
+    any |= rows[b] > 0;
+  }
+  if (!any) return ok();
+  if (!q || !P_qk || !o || !lse) return fail(SWAN_ERR_INVALID_ARG, "q / P_qk / o / lse is NULL");
+  if ((((uintptr_t)q | (uintptr_t)P_qk | (uintptr_t)P_vo | (uintptr_t)o) & 15) != 0)
+    return fail(SWAN_ERR_INVALID_ARG, "q / P_qk / P_vo / o must be 16-byte aligned");
+  if (!workspace || workspace_bytes < pl.bytes)
+    return fail(SWAN_ERR_WORKSPACE, "workspace of %zu bytes, need %zu", workspace_bytes, pl.bytes);
+  if (((uintptr_t)workspace & 255) != 0)
+    return fail(SWAN_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+  const swan_cache* c = sources[0].cache;
+  const int64_t n_rows = (int64_t)batch * c->n_q_heads * n;
+  if (overlap(o, n_rows * SWAN_HEAD_DIM * 4, lse, n_rows * 4))
+    return fail(SWAN_ERR_INVALID_ARG, "o and lse overlap");
+  float* qhat = (float*)workspace;
+  float* part = (float*)((char*)workspace + pl.qhat);
+  swan::RotateLaunch r;
+  r.x = q;
+  r.P = P_qk;
+  r.y = qhat;
+  r.mult = scale_or_default(scale) * 1.4426950408889634f;
+  r.x_dtype = c->dtype == SWAN_F32 ? SWAN_F32 : SWAN_F16;
+  r.transposed = 0;
+  r.B = batch;
+  r.H = c->n_q_heads;
+  r.Hkv = c->n_kv_heads;
+  r.n = n;
+  for (int b = 0; b < SWAN_MAX_BATCH; ++b) r.rows[b] = b < batch ? rows[b] : 0;
+  r.stream = (hipStream_t)stream;
+  hipError_t e = swan::launch_rotate_rows(r);
+  if (e != hipSuccess) return hip_status(e, "rotate launch");
+  for (int s = 0; s < n_sources; ++s) {
+    swan::AttendLaunch& a = pl.a[s];
+    if (a.units == 0) continue;
+    a.q = qhat;
+    a.part = part;
+    a.slots = pl.slots;
+    a.slot0 = pl.base[s];
+    a.stream = (hipStream_t)stream;
+    if ((e = swan::launch_attend_pages(a)) != hipSuccess) return hip_status(e, "attend launch");
+  }
+  swan::JoinLaunch j;
+  j.part = part;
+  j.o0 = j.lse0 = nullptr;
+  j.P_vo = nullptr;
+  j.out = nullptr;
+  j.o = P_vo ? qhat : o;  // q_hat's place is free by now
+  j.lse = lse;
+  j.B = batch;
+  j.H = c->n_q_heads;
+  j.Hkv = c->n_kv_heads;
+  j.n = n;
+  j.slots = pl.slots;
+  j.dtype = c->dtype;
+  j.decode = 0;
+  j.own_slots = 0;
+  j.own = nullptr;
+  j.own_bb = 0;
+  for (int b = 0; b < SWAN_MAX_BATCH; ++b) {
+    for (int s = 0; s < 2; ++s) j.used[s][b] = b < batch ? pl.used[s][b] : 0;
+    j.rows[b] = b < batch ? rows[b] : 0;
+  }
+  j.base[0] = pl.base[0];
+  j.base[1] = pl.base[1];
+  j.stream = (hipStream_t)stream;
+  if ((e = swan::launch_join(j)) != hipSuccess) return hip_status(e, "join launch");
+  if (!P_vo) return ok();
+  r.x = qhat;
+  r.P = P_vo;
+  r.y = o;
+  r.mult = 1.f;
+  r.x_dtype = SWAN_F32;
+  r.transposed = 1;
+  return hip_status(swan::launch_rotate_rows(r), "rotate launch");
+}
+
+swan_status prompt_run(const void* q, const void* k, const void* v, int32_t dtype,
+                       int32_t batch, int32_t n_q_heads, int32_t n_kv_heads,
+                       int32_t n, int32_t m, int32_t head_dim, const int32_t* n_host,
+                       const int32_t* m_host, int32_t causal, int32_t window,
+                       const int32_t* sinks_host, float scale,
+                       const float* o0, const float* lse0, void* out,
+                       void* workspace, size_t workspace_bytes, void* stream) {
+  PromptPlan pl;
+  swan_status st = prompt_prep(dtype, batch, n_q_heads, n_kv_heads, n, m, head_dim, n_host, m_host,
+                               causal, pl, window, sinks_host);
+  if (st != SWAN_OK) return st;
+  if ((st = check_scale(scale)) != SWAN_OK) return st;
+  if ((o0 == nullptr) != (lse0 == nullptr))
+    return fail(SWAN_ERR_INVALID_ARG, "pass both parts of the state or neither");
+  if (pl.a.groups == 0) return ok();
+  bool any_key = false;
+  for (int j = 0; j < pl.a.groups; ++j) any_key |= pl.a.keys[j] > 0;
+  if (!q || !out || (any_key && (!k || !v)))
+    return fail(SWAN_ERR_INVALID_ARG, "q / k / v / out is NULL");
+  const void* ptrs[5] = {q, k, v, o0, out};
+  for (const void* p : ptrs)
+    if (((uintptr_t)p & 15) != 0)
+      return fail(SWAN_ERR_INVALID_ARG, "q / k / v / o0 / out must be 16-byte aligned");
+  if (pl.bytes > 0) {
+    if (!workspace || workspace_bytes < pl.bytes)
+      return fail(SWAN_ERR_WORKSPACE, "workspace of %zu bytes, need %zu", workspace_bytes,
+                  pl.bytes);
+    if (((uintptr_t)workspace & 255) != 0)
+      return fail(SWAN_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+  }
+  const int64_t es = elem_bytes(dtype), row = (int64_t)batch * SWAN_HEAD_DIM;
+  const int64_t q_bytes = row * n_q_heads * n * es, kv_bytes = row * n_kv_heads * m * es;
+  if (overlap(out, q_bytes, q, q_bytes) || overlap(out, q_bytes, k, kv_bytes) ||
+      overlap(out, q_bytes, v, kv_bytes) || overlap(out, q_bytes, o0, row * n_q_heads * n * 4) ||
+      overlap(out, q_bytes, lse0, (int64_t)batch * n_q_heads * n * 4))
+    return fail(SWAN_ERR_INVALID_ARG, "out overlaps q, k, v or the state");
+  swan::AttendLaunch& a = pl.a;
+  a.q = q;
+  a.o0 = o0;
+  a.lse0 = lse0;
+  a.out = out;
+  a.part = pl.bytes > 0 ? (float*)workspace : nullptr;
+  a.k = k;
+  a.v = v;
+  a.qmult = scale_or_default(scale) * 1.4426950408889634f;
+  a.dtype = dtype == SWAN_F32 ? SWAN_F32 : SWAN_F16;
+  a.stream = (hipStream_t)stream;
+  hipError_t e = swan::launch_attend_dense(a);
+  if (e != hipSuccess || !a.part) return hip_status(e, "prompt attention launch");
+  swan::JoinLaunch j;
+  j.part = a.part;
+  j.o0 = o0;
+  j.lse0 = lse0;
+  j.P_vo = nullptr;
+  j.out = out;
+  j.o = j.lse = nullptr;
+  j.B = batch;
+  j.H = n_q_heads;
+  j.Hkv = n_kv_heads;
+  j.n = n;
+  j.slots = a.slots;
+  j.dtype = a.dtype;
+  j.decode = 0;
+  j.own_slots = 0;
+  j.own = nullptr;
+  j.own_bb = 0;
+  for (int b = 0; b < SWAN_MAX_BATCH; ++b) {
+    j.used[0][b] = b < batch ? pl.used[b] : 0;
+    j.used[1][b] = 0;
+    j.rows[b] = b < batch ? (n_host ? n_host[b] : n) : 0;
+  }
+  j.base[0] = j.base[1] = 0;
+  j.stream = a.stream;
+  return hip_status(swan::launch_join(j), "join launch");
+}
+
+swan_status rope_prep(const void* x, void* y, int32_t dtype, int32_t batch, int32_t n_heads,
+                      int32_t n, int32_t head_dim, const int32_t* pos0_host, double base,
+                      void* stream, swan::RopeLaunch& a) {
+  if (!dtype_ok(dtype)) return fail(SWAN_ERR_UNSUPPORTED, "dtype %d not supported", dtype);
+  if (head_dim != SWAN_HEAD_DIM)
+    return fail(SWAN_ERR_UNSUPPORTED, "head_dim %d: the GPU path supports %d only", head_dim,
+                SWAN_HEAD_DIM);
+  if (batch < 1 || batch > SWAN_MAX_BATCH || n_heads < 1 || n < 0)
+    return fail(SWAN_ERR_INVALID_ARG, "batch %d, n_heads %d, n %d", batch, n_heads, n);
+  if (!(base > 1.0) || isinf(base)) return fail(SWAN_ERR_INVALID_ARG, "base must be > 1");
+  if (!pos0_host) return fail(SWAN_ERR_INVALID_ARG, "pos0_host is NULL");
+  if (n == 0) return SWAN_OK;
+  if (!x || !y) return fail(SWAN_ERR_INVALID_ARG, "x / y is NULL");
+  if ((((uintptr_t)x | (uintptr_t)y) & 15) != 0)
+    return fail(SWAN_ERR_INVALID_ARG, "x / y must be 16-byte aligned");
+  a.x = x;
+  a.y = y;
+  a.B = batch;
+  a.H = n_heads;
+  a.n = n;
+  a.dtype = dtype;
+  for (int b = 0; b < SWAN_MAX_BATCH; ++b) {
+    if (b < batch && (pos0_host[b] < 0 || (int64_t)pos0_host[b] + n > INT32_MAX))
+      return fail(SWAN_ERR_INVALID_ARG, "pos0[%d] = %d out of range", b, pos0_host[b]);
+    a.pos0[b] = b < batch ? pos0_host[b] : 0;
+  }
+  a.base = base;
+  a.stream = (hipStream_t)stream;
+  return SWAN_OK;
+}
+
+swan_status qkv_rows_prep(const void* qkv, int64_t seq_stride, int64_t row_stride, int32_t dtype,
+                          int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t n,
+                          int32_t head_dim, const int32_t* pos0_host, double base,
+                          const void* q_weight, const void* k_weight, int32_t weights_per_head,
+                          int32_t weights_f32, double eps, void* q, void* k, void* v,
+                          void* stream, swan::QkvRowsLaunch& a) {
+  if (!dtype_ok(dtype)) return fail(SWAN_ERR_UNSUPPORTED, "dtype %d not supported", dtype);
+  if (head_dim != SWAN_HEAD_DIM)
+    return fail(SWAN_ERR_UNSUPPORTED, "head_dim %d: the GPU path supports %d only", head_dim,
+                SWAN_HEAD_DIM);
+  if (batch < 1 || batch > SWAN_MAX_BATCH || n < 0)
+    return fail(SWAN_ERR_INVALID_ARG, "batch %d, n %d", batch, n);
+  if (n_q_heads < 0 || n_kv_heads < 0 || n_q_heads + (int64_t)n_kv_heads < 1 ||
+      n_q_heads + 2 * (int64_t)n_kv_heads > 65535)
+    return fail(SWAN_ERR_INVALID_ARG, "n_q_heads %d, n_kv_heads %d", n_q_heads, n_kv_heads);
+  if ((int64_t)batch * n > INT32_MAX)
+    return fail(SWAN_ERR_INVALID_ARG, "batch %d x n %d: above 2^31 - 1 rows", batch, n);
+  if (!(base > 1.0) || isinf(base)) return fail(SWAN_ERR_INVALID_ARG, "base must be > 1");
+  if (!(eps >= 0.0) || isinf(eps)) return fail(SWAN_ERR_INVALID_ARG, "eps must be finite, >= 0");
+  if ((weights_per_head != 0 && weights_per_head != 1) || (weights_f32 != 0 && weights_f32 != 1))
+    return fail(SWAN_ERR_INVALID_ARG, "weights_per_head %d, weights_f32 %d: 0 or 1",
+                weights_per_head, weights_f32);
+  if (!pos0_host) return fail(SWAN_ERR_INVALID_ARG, "pos0_host is NULL");
+  if (n == 0) return SWAN_OK;
+  const int64_t width = (n_q_heads + 2 * (int64_t)n_kv_heads) * SWAN_HEAD_DIM;
+  if (row_stride < width || row_stride % 8 != 0 || seq_stride < 0 || seq_stride % 8 != 0)
+    return fail(SWAN_ERR_INVALID_ARG,
+                "strides %lld (sequence) and %lld (row of %lld): multiples of 8, a row at least",
+                (long long)seq_stride, (long long)row_stride, (long long)width);
+  if (!qkv || (n_q_heads && !q) || (n_kv_heads && (!k || !v)))
+    return fail(SWAN_ERR_INVALID_ARG, "qkv / q / k / v is NULL");
+  const void* ptrs[6] = {qkv, q, k, v, q_weight, k_weight};
+  for (const void* p : ptrs)
+    if (((uintptr_t)p & 15) != 0)
+      return fail(SWAN_ERR_INVALID_ARG, "pointers must be 16-byte aligned");
+  a.x = qkv;
+  a.seq = seq_stride;
+  a.row = row_stride;
+  a.out[0] = q;
+  a.out[1] = k;
+  a.out[2] = v;
+  a.w[0] = q_weight;
+  a.w[1] = k_weight;
+  a.wstep = weights_per_head ? SWAN_HEAD_DIM : 0;
+  a.w32 = weights_f32;
+  a.B = batch;
+  a.Hq = n_q_heads;
+  a.Hkv = n_kv_heads;
+  a.n = n;
+  a.dtype = dtype;
+  a.eps = eps;
+  a.base = base;
+  for (int b = 0; b < SWAN_MAX_BATCH; ++b) {
+    if (b < batch && (pos0_host[b] < 0 || (int64_t)pos0_host[b] + n > INT32_MAX))
+      return fail(SWAN_ERR_INVALID_ARG, "pos0[%d] = %d out of range", b, pos0_host[b]);
+    a.pos0[b] = b < batch ? pos0_host[b] : 0;
+  }
+  // the outputs and the rows read share no byte
+  const int64_t es = elem_bytes(dtype), each = (int64_t)batch * n * SWAN_HEAD_DIM * es;
+  const void* lo[4] = {qkv, q, k, v};
+  const int64_t size[4] = {((batch - 1) * seq_stride + (n - 1) * row_stride + width) * es,
+                           each * n_q_heads, each * n_kv_heads, each * n_kv_heads};
+  for (int x = 0; x < 4; ++x)
+    for (int y = x + 1; y < 4; ++y)
+      if (overlap(lo[x], size[x], lo[y], size[y]))
+        return fail(SWAN_ERR_INVALID_ARG, "qkv, q, k and v overlap");
+  a.stream = (hipStream_t)stream;
+  return SWAN_OK;
+}
+
+}  // namespace swan_host
+
+using namespace swan_host;
 
 extern "C" {
 
@@ -1103,33 +1404,10 @@ swan_status swan_change_k(const swan_cache* src, const int32_t* k_active_src,
 swan_status swan_rope(const void* x, void* y, int32_t dtype, int32_t batch, int32_t n_heads,
                       int32_t n, int32_t head_dim, const int32_t* pos0_host, double base,
                       void* stream) {
-  if (!dtype_ok(dtype)) return fail(SWAN_ERR_UNSUPPORTED, "dtype %d not supported", dtype);
-  if (head_dim != SWAN_HEAD_DIM)
-    return fail(SWAN_ERR_UNSUPPORTED, "head_dim %d: the GPU path supports %d only", head_dim,
-                SWAN_HEAD_DIM);
-  if (batch < 1 || batch > SWAN_MAX_BATCH || n_heads < 1 || n < 0)
-    return fail(SWAN_ERR_INVALID_ARG, "batch %d, n_heads %d, n %d", batch, n_heads, n);
-  if (!(base > 1.0) || isinf(base)) return fail(SWAN_ERR_INVALID_ARG, "base must be > 1");
-  if (!pos0_host) return fail(SWAN_ERR_INVALID_ARG, "pos0_host is NULL");
-  if (n == 0) return ok();
-  if (!x || !y) return fail(SWAN_ERR_INVALID_ARG, "x / y is NULL");
-  if ((((uintptr_t)x | (uintptr_t)y) & 15) != 0)
-    return fail(SWAN_ERR_INVALID_ARG, "x / y must be 16-byte aligned");
   swan::RopeLaunch a;
-  a.x = x;
-  a.y = y;
-  a.B = batch;
-  a.H = n_heads;
-  a.n = n;
-  a.dtype = dtype;
-  for (int b = 0; b < SWAN_MAX_BATCH; ++b) {
-    if (b < batch && (pos0_host[b] < 0 || (int64_t)pos0_host[b] + n > INT32_MAX))
-      return fail(SWAN_ERR_INVALID_ARG, "pos0[%d] = %d out of range", b, pos0_host[b]);
-    a.pos0[b] = b < batch ? pos0_host[b] : 0;
-  }
-  a.base = base;
-  a.stream = (hipStream_t)stream;
-  return hip_status(swan::launch_rope(a), "rope launch");
+  const swan_status st = rope_prep(x, y, dtype, batch, n_heads, n, head_dim, pos0_host, base, stream, a);
+  if (st != SWAN_OK) return st;
+  return n == 0 ? ok() : hip_status(swan::launch_rope(a), "rope launch");
 }
 
 swan_status swan_qkv_rows(const void* qkv, int64_t seq_stride, int64_t row_stride, int32_t dtype,
@@ -1138,69 +1416,12 @@ swan_status swan_qkv_rows(const void* qkv, int64_t seq_stride, int64_t row_strid
                           const void* q_weight, const void* k_weight, int32_t weights_per_head,
                           int32_t weights_f32, double eps, void* q, void* k, void* v,
                           void* stream) {
-  if (!dtype_ok(dtype)) return fail(SWAN_ERR_UNSUPPORTED, "dtype %d not supported", dtype);
-  if (head_dim != SWAN_HEAD_DIM)
-    return fail(SWAN_ERR_UNSUPPORTED, "head_dim %d: the GPU path supports %d only", head_dim,
-                SWAN_HEAD_DIM);
-  if (batch < 1 || batch > SWAN_MAX_BATCH || n < 0)
-    return fail(SWAN_ERR_INVALID_ARG, "batch %d, n %d", batch, n);
-  if (n_q_heads < 0 || n_kv_heads < 0 || n_q_heads + (int64_t)n_kv_heads < 1 ||
-      n_q_heads + 2 * (int64_t)n_kv_heads > 65535)
-    return fail(SWAN_ERR_INVALID_ARG, "n_q_heads %d, n_kv_heads %d", n_q_heads, n_kv_heads);
-  if ((int64_t)batch * n > INT32_MAX)
-    return fail(SWAN_ERR_INVALID_ARG, "batch %d x n %d: above 2^31 - 1 rows", batch, n);
-  if (!(base > 1.0) || isinf(base)) return fail(SWAN_ERR_INVALID_ARG, "base must be > 1");
-  if (!(eps >= 0.0) || isinf(eps)) return fail(SWAN_ERR_INVALID_ARG, "eps must be finite, >= 0");
-  if ((weights_per_head != 0 && weights_per_head != 1) || (weights_f32 != 0 && weights_f32 != 1))
-    return fail(SWAN_ERR_INVALID_ARG, "weights_per_head %d, weights_f32 %d: 0 or 1",
-                weights_per_head, weights_f32);
-  if (!pos0_host) return fail(SWAN_ERR_INVALID_ARG, "pos0_host is NULL");
-  if (n == 0) return ok();
-  const int64_t width = (n_q_heads + 2 * (int64_t)n_kv_heads) * SWAN_HEAD_DIM;
-  if (row_stride < width || row_stride % 8 != 0 || seq_stride < 0 || seq_stride % 8 != 0)
-    return fail(SWAN_ERR_INVALID_ARG,
-                "strides %lld (sequence) and %lld (row of %lld): multiples of 8, a row at least",
-                (long long)seq_stride, (long long)row_stride, (long long)width);
-  if (!qkv || (n_q_heads && !q) || (n_kv_heads && (!k || !v)))
-    return fail(SWAN_ERR_INVALID_ARG, "qkv / q / k / v is NULL");
-  const void* ptrs[6] = {qkv, q, k, v, q_weight, k_weight};
-  for (const void* p : ptrs)
-    if (((uintptr_t)p & 15) != 0)
-      return fail(SWAN_ERR_INVALID_ARG, "pointers must be 16-byte aligned");
   swan::QkvRowsLaunch a;
-  a.x = qkv;
-  a.seq = seq_stride;
-  a.row = row_stride;
-  a.out[0] = q;
-  a.out[1] = k;
-  a.out[2] = v;
-  a.w[0] = q_weight;
-  a.w[1] = k_weight;
-  a.wstep = weights_per_head ? SWAN_HEAD_DIM : 0;
-  a.w32 = weights_f32;
-  a.B = batch;
-  a.Hq = n_q_heads;
-  a.Hkv = n_kv_heads;
-  a.n = n;
-  a.dtype = dtype;
-  a.eps = eps;
-  a.base = base;
-  for (int b = 0; b < SWAN_MAX_BATCH; ++b) {
-    if (b < batch && (pos0_host[b] < 0 || (int64_t)pos0_host[b] + n > INT32_MAX))
-      return fail(SWAN_ERR_INVALID_ARG, "pos0[%d] = %d out of range", b, pos0_host[b]);
-    a.pos0[b] = b < batch ? pos0_host[b] : 0;
-  }
-  // the outputs and the rows read share no byte
-  const int64_t es = elem_bytes(dtype), each = (int64_t)batch * n * SWAN_HEAD_DIM * es;
-  const void* lo[4] = {qkv, q, k, v};
-  const int64_t size[4] = {((batch - 1) * seq_stride + (n - 1) * row_stride + width) * es,
-                           each * n_q_heads, each * n_kv_heads, each * n_kv_heads};
-  for (int x = 0; x < 4; ++x)
-    for (int y = x + 1; y < 4; ++y)
-      if (overlap(lo[x], size[x], lo[y], size[y]))
-        return fail(SWAN_ERR_INVALID_ARG, "qkv, q, k and v overlap");
-  a.stream = (hipStream_t)stream;
-  return hip_status(swan::launch_qkv_rows(a), "qkv_rows launch");
+  const swan_status st = qkv_rows_prep(qkv, seq_stride, row_stride, dtype, batch, n_q_heads,
+                                       n_kv_heads, n, head_dim, pos0_host, base, q_weight, k_weight,
+                                       weights_per_head, weights_f32, eps, q, k, v, stream, a);
+  if (st != SWAN_OK) return st;
+  return n == 0 ? ok() : hip_status(swan::launch_qkv_rows(a), "qkv_rows launch");
 }
 
 swan_status swan_attend_workspace_bytes(const swan_prefix* sources, int32_t n_sources,
@@ -1218,87 +1439,8 @@ swan_status swan_attend(const swan_prefix* sources, int32_t n_sources, int32_t b
                         const int32_t* n_host, const void* q, const float* P_qk,
                         const float* P_vo, float scale, float* o, float* lse, void* workspace,
                         size_t workspace_bytes, void* stream) {
-  AttendPlan pl;
-  swan_status st = attend_prep(sources, n_sources, batch, n, n_host, true, pl);
-  if (st != SWAN_OK) return st;
-  if ((st = check_scale(scale)) != SWAN_OK) return st;
-  int32_t rows[SWAN_MAX_BATCH] = {};
-  bool any = false;
-  for (int b = 0; b < batch; ++b) {
-    rows[b] = n_host ? n_host[b] : n;
-    any |= rows[b] > 0;
-  }
-  if (!any) return ok();
-  if (!q || !P_qk || !o || !lse) return fail(SWAN_ERR_INVALID_ARG, "q / P_qk / o / lse is NULL");
-  if ((((uintptr_t)q | (uintptr_t)P_qk | (uintptr_t)P_vo | (uintptr_t)o) & 15) != 0)
-    return fail(SWAN_ERR_INVALID_ARG, "q / P_qk / P_vo / o must be 16-byte aligned");
-  if (!workspace || workspace_bytes < pl.bytes)
-    return fail(SWAN_ERR_WORKSPACE, "workspace of %zu bytes, need %zu", workspace_bytes, pl.bytes);
-  if (((uintptr_t)workspace & 255) != 0)
-    return fail(SWAN_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
-  const swan_cache* c = sources[0].cache;
-  const int64_t n_rows = (int64_t)batch * c->n_q_heads * n;
-  if (overlap(o, n_rows * SWAN_HEAD_DIM * 4, lse, n_rows * 4))
-    return fail(SWAN_ERR_INVALID_ARG, "o and lse overlap");
-  float* qhat = (float*)workspace;
-  float* part = (float*)((char*)workspace + pl.qhat);
-  swan::RotateLaunch r;
-  r.x = q;
-  r.P = P_qk;
-  r.y = qhat;
-  r.mult = scale_or_default(scale) * 1.4426950408889634f;
-  r.x_dtype = c->dtype == SWAN_F32 ? SWAN_F32 : SWAN_F16;
-  r.transposed = 0;
-  r.B = batch;
-  r.H = c->n_q_heads;
-  r.Hkv = c->n_kv_heads;
-  r.n = n;
-  for (int b = 0; b < SWAN_MAX_BATCH; ++b) r.rows[b] = b < batch ? rows[b] : 0;
-  r.stream = (hipStream_t)stream;
-  hipError_t e = swan::launch_rotate_rows(r);
-  if (e != hipSuccess) return hip_status(e, "rotate launch");
-  for (int s = 0; s < n_sources; ++s) {
-    swan::AttendLaunch& a = pl.a[s];
-    if (a.units == 0) continue;
-    a.q = qhat;
-    a.part = part;
-    a.slots = pl.slots;
-    a.slot0 = pl.base[s];
-    a.stream = (hipStream_t)stream;
-    if ((e = swan::launch_attend_pages(a)) != hipSuccess) return hip_status(e, "attend launch");
-  }
-  swan::JoinLaunch j;
-  j.part = part;
-  j.o0 = j.lse0 = nullptr;
-  j.P_vo = nullptr;
-  j.out = nullptr;
-  j.o = P_vo ? qhat : o;  // q_hat's place is free by now
-  j.lse = lse;
-  j.B = batch;
-  j.H = c->n_q_heads;
-  j.Hkv = c->n_kv_heads;
-  j.n = n;
-  j.slots = pl.slots;
-  j.dtype = c->dtype;
-  j.own_slots = 0;
-  j.own = nullptr;
-  j.own_bb = 0;
-  for (int b = 0; b < SWAN_MAX_BATCH; ++b) {
-    for (int s = 0; s < 2; ++s) j.used[s][b] = b < batch ? pl.used[s][b] : 0;
-    j.rows[b] = b < batch ? rows[b] : 0;
-  }
-  j.base[0] = pl.base[0];
-  j.base[1] = pl.base[1];
-  j.stream = (hipStream_t)stream;
-  if ((e = swan::launch_join(j)) != hipSuccess) return hip_status(e, "join launch");
-  if (!P_vo) return ok();
-  r.x = qhat;
-  r.P = P_vo;
-  r.y = o;
-  r.mult = 1.f;
-  r.x_dtype = SWAN_F32;
-  r.transposed = 1;
-  return hip_status(swan::launch_rotate_rows(r), "rotate launch");
+  return attend_run(sources, n_sources, batch, n, n_host, Window(), q, P_qk, P_vo, scale, o, lse,
+                    workspace, workspace_bytes, stream);
 }
 
 swan_status swan_prompt_workspace_bytes(int32_t dtype, int32_t batch, int32_t n_q_heads, int32_t n_kv_heads,
@@ -1320,72 +1462,8 @@ swan_status swan_prompt_attention(const void* q, const void* k, const void* v, i
                                   const int32_t* m_host, int32_t causal, float scale,
                                   const float* o0, const float* lse0, void* out,
                                   void* workspace, size_t workspace_bytes, void* stream) {
-  PromptPlan pl;
-  swan_status st = prompt_prep(dtype, batch, n_q_heads, n_kv_heads, n, m, head_dim, n_host, m_host,
-                               causal, pl);
-  if (st != SWAN_OK) return st;
-  if ((st = check_scale(scale)) != SWAN_OK) return st;
-  if ((o0 == nullptr) != (lse0 == nullptr))
-    return fail(SWAN_ERR_INVALID_ARG, "pass both parts of the state or neither");
-  if (pl.a.groups == 0) return ok();
-  bool any_key = false;
-  for (int j = 0; j < pl.a.groups; ++j) any_key |= pl.a.keys[j] > 0;
-  if (!q || !out || (any_key && (!k || !v)))
-    return fail(SWAN_ERR_INVALID_ARG, "q / k / v / out is NULL");
-  const void* ptrs[5] = {q, k, v, o0, out};
-  for (const void* p : ptrs)
-    if (((uintptr_t)p & 15) != 0)
-      return fail(SWAN_ERR_INVALID_ARG, "q / k / v / o0 / out must be 16-byte aligned");
-  if (pl.bytes > 0) {
-    if (!workspace || workspace_bytes < pl.bytes)
-      return fail(SWAN_ERR_WORKSPACE, "workspace of %zu bytes, need %zu", workspace_bytes,
-                  pl.bytes);
-    if (((uintptr_t)workspace & 255) != 0)
-      return fail(SWAN_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
-  }
-  const int64_t es = elem_bytes(dtype), row = (int64_t)batch * SWAN_HEAD_DIM;
-  const int64_t q_bytes = row * n_q_heads * n * es, kv_bytes = row * n_kv_heads * m * es;
-  if (overlap(out, q_bytes, q, q_bytes) || overlap(out, q_bytes, k, kv_bytes) ||
-      overlap(out, q_bytes, v, kv_bytes) || overlap(out, q_bytes, o0, row * n_q_heads * n * 4) ||
-      overlap(out, q_bytes, lse0, (int64_t)batch * n_q_heads * n * 4))
-    return fail(SWAN_ERR_INVALID_ARG, "out overlaps q, k, v or the state");
-  swan::AttendLaunch& a = pl.a;
-  a.q = q;
-  a.o0 = o0;
-  a.lse0 = lse0;
-  a.out = out;
-  a.part = pl.bytes > 0 ? (float*)workspace : nullptr;
-  a.k = k;
-  a.v = v;
-  a.qmult = scale_or_default(scale) * 1.4426950408889634f;
-  a.dtype = dtype == SWAN_F32 ? SWAN_F32 : SWAN_F16;
-  a.stream = (hipStream_t)stream;
-  hipError_t e = swan::launch_attend_dense(a);
-  if (e != hipSuccess || !a.part) return hip_status(e, "prompt attention launch");
-  swan::JoinLaunch j;
-  j.part = a.part;
-  j.o0 = o0;
-  j.lse0 = lse0;
-  j.P_vo = nullptr;
-  j.out = out;
-  j.o = j.lse = nullptr;
-  j.B = batch;
-  j.H = n_q_heads;
-  j.Hkv = n_kv_heads;
-  j.n = n;
-  j.slots = a.slots;
-  j.dtype = a.dtype;
-  j.own_slots = 0;
-  j.own = nullptr;
-  j.own_bb = 0;
-  for (int b = 0; b < SWAN_MAX_BATCH; ++b) {
-    j.used[0][b] = b < batch ? pl.used[b] : 0;
-    j.used[1][b] = 0;
-    j.rows[b] = b < batch ? (n_host ? n_host[b] : n) : 0;
-  }
-  j.base[0] = j.base[1] = 0;
-  j.stream = a.stream;
-  return hip_status(swan::launch_join(j), "join launch");
+  return prompt_run(q, k, v, dtype, batch, n_q_heads, n_kv_heads, n, m, head_dim, n_host, m_host,
+                    causal, 0, nullptr, scale, o0, lse0, out, workspace, workspace_bytes, stream);
 }
 
 swan_status swan_prefix_workspace_bytes(const swan_prefix* prefix, const swan_cache* c,

@@ -76,7 +76,13 @@ struct RopeLaunch {
   double base;
   hipStream_t stream;
 };
-hipError_t launch_rope(const RopeLaunch& a);
+// other forms (rotary.h): the frequencies of half pairs, then zeros
+struct RotaryForm {
+  double magnitude;
+  int half, interleaved;
+  double freq[kD / 2];
+};
+hipError_t launch_rope(const RopeLaunch& a, const RotaryForm* form = nullptr);
 
 constexpr int kMaxCalib = 64;  // problems per launch
 struct CalibLaunch {

@@ -2,6 +2,7 @@
 // attention of several rows per sequence (over cached tokens, over a prompt).
 #pragma once
 
+#include "swan_cache_ops.h"
 #include "swan_device.h"
 #include "swan_internal.h"
 #include "swan_layer.h"
@@ -21,7 +22,7 @@ struct QkvRowsLaunch {
   int32_t pos0[SWAN_MAX_BATCH];
   hipStream_t stream;
 };
-hipError_t launch_qkv_rows(const QkvRowsLaunch& a);
+hipError_t launch_qkv_rows(const QkvRowsLaunch& a, const RotaryForm* form = nullptr);
 
 // ---------------------------------------------------------------------------
 // attention of several rows per sequence (attend.h): rows of q over one of
@@ -84,8 +85,15 @@ struct AttendLaunch {
   int32_t cseq[SWAN_MAX_BATCH];       // pages: cache sequence of a group; dense: its sequence
   int32_t kact[2][SWAN_MAX_BATCH];    // pages: k of the group's keys / values
   uint8_t seq[SWAN_MAX_BATCH];        // sequence of a list entry
+  // With a sliding window a row sees the keys from its first one on (to its causal limit,
+  // where there is one), and those below `sink`, both numbered from the source's first key.
+  // dense: the first one is the limit - window; pages: lo + i for row i of a list entry.
+  int window;                         // 0: none
+  int32_t lo[SWAN_MAX_BATCH];
+  uint16_t sink[SWAN_MAX_BATCH];      // of a list entry (dense: group)
   hipStream_t stream;
 };
+constexpr int kMaxSinks = 65535;
 static_assert(sizeof(AttendLaunch) <= 4096, "passed to the kernels by value");
 hipError_t launch_attend_pages(const AttendLaunch& a);
 hipError_t launch_attend_dense(const AttendLaunch& a);
@@ -105,17 +113,18 @@ struct RotateLaunch {
 };
 hipError_t launch_rotate_rows(const RotateLaunch& a);
 
-// The partials of a row to one result: of up to two sources and a state, or (decode, with
-// `own`) of one source and a decode step's own cache.
+// The partials of a row to one result: of up to two sources and a state, or (decode) of up to
+// two sources and, with `own`, a decode step's own cache.
 struct JoinLaunch {
   const float* part;   // [B H n][slots][kPartFloats]
   const float* o0;     // a state to continue from, or NULL
   const float* lse0;
-  const float* P_vo;   // with `own`: rotates the result back, or NULL
+  const float* P_vo;   // decode: rotates the result back, or NULL
   void* out;           // storage type, or NULL
   float* o;            // float32 state, or NULL (unless `out`)
   float* lse;
   int B, H, Hkv, n, slots, dtype;
+  int decode;          // rows are single tokens, rotated back with P_vo
   int own_slots;       // decode: the partials of swan_decode_attention, own_slots + 1 per row
   const float* own;
   int own_bb;
@@ -127,5 +136,68 @@ struct JoinLaunch {
 };
 static_assert(sizeof(JoinLaunch) <= 4096, "passed to the kernels by value");
 hipError_t launch_join(const JoinLaunch& a);
+
+// ---------------------------------------------------------------------------
+// decode with a sliding window (window_decode.h): the partials of one token per sequence over
+// the tokens of its cache from lo on, and those below sink.  Sequence b's parts are its
+// nsplit[b] splits of the pages that hold such tokens, then one for each 64 slots of its ring.
+// ---------------------------------------------------------------------------
+struct WindowLaunch {
+  const void* q;       // [B][Hq][128] of the storage type
+  const float* P_qk;
+  float* qhat;         // [B][Hq][128]: rotated, x qmult
+  float* part;         // [B][Hq][slots][kPartFloats]
+  const void* k_pages;
+  const void* v_pages;
+  const void* k_ring;
+  const void* v_ring;
+  float qmult;
+  int B, Hq, Hkv, bb, npc, slots, dtype;
+  int qhat_ready;      // qhat is there already (decode steps)
+  int32_t len[SWAN_MAX_BATCH], lo[SWAN_MAX_BATCH], sink[SWAN_MAX_BATCH];
+  int32_t nsplit[SWAN_MAX_BATCH];  // 0: no such page
+  int32_t kact[2][SWAN_MAX_BATCH];
+  int64_t off[2][SWAN_MAX_BATCH];
+  hipStream_t stream;
+};
+hipError_t launch_window(const WindowLaunch& a);
+// the sequences of one launch, whose k_pad is 8 kp8 at most
+hipError_t launch_window_gqa(const WindowLaunch& a, const SeqGroup& g, int kp8);
+
+// The pages of a sequence that hold tokens from lo on or below sink: the first `sinks`, then
+// those from `skip` on.
+struct WindowPages {
+  int S, sinks, skip, count;  // pruned tokens; ... ; the pages in all
+  __host__ __device__ WindowPages(int L, int bb, int lo, int sink) {
+    S = L > bb ? L - bb : 0;
+    const int np = pages_for(S);
+    skip = lo >= S ? np : (lo > 0 ? lo : 0) / kPage;
+    sinks = pages_for(sink < S ? sink : S);
+    if (sinks > skip) sinks = skip;
+    count = sinks + np - skip;
+  }
+  __host__ __device__ int page(int x) const { return x < sinks ? x : x - sinks + skip; }
+};
+
+// ---------------------------------------------------------------------------
+// sequences of a cache to places of another (copy_sequences.hip)
+// ---------------------------------------------------------------------------
+struct CopyLaunch {
+  const void* src[4];  // key pages, value pages, key ring, value ring
+  void* dst[4];
+  int Hkv, bb, npc_src, npc_dst, dtype, n;
+  int max_pages;                   // of a destination sequence
+  int32_t from[SWAN_MAX_BATCH];    // list entry: source sequence
+  int32_t to[SWAN_MAX_BATCH];      // destination sequence
+  int32_t len[SWAN_MAX_BATCH];     // tokens of the source
+  int32_t first[SWAN_MAX_BATCH];   // tokens first .. first + drop - 1 are left out
+  int32_t drop[SWAN_MAX_BATCH];
+  int32_t k[2][SWAN_MAX_BATCH];
+  int64_t off_src[2][SWAN_MAX_BATCH];
+  int64_t off_dst[2][SWAN_MAX_BATCH];
+  hipStream_t stream;
+};
+static_assert(sizeof(CopyLaunch) <= 4096, "passed to the kernel by value");
+hipError_t launch_copy(const CopyLaunch& a);
 
 }  // namespace swan

@@ -18,6 +18,9 @@ A prompt call fills the cache; with attend=True it also returns the rows' attent
 dense, causal kind over the rows themselves (swan_prompt_attention), continued from
 swan_attend over what is cached before them (pruned tokens as they are stored).  Sequences
 can stand behind a prefix that another layer's cache holds once for all of them (fork).
+With a sliding window all of these see the last `window` tokens and the first `sinks` alone
+(swan_long.h), and compact() gives back the memory of those that no row sees any more; the
+positions count on.  select() makes a layer of copies of some sequences.
 The SWAN steps run in libswan's kernels.
 Weights are [in][out] row-major, x . W.
 """
@@ -118,18 +121,26 @@ def _no_project(self, x):
 
 class SwanAttentionLayer:
     def __init__(self, W_q, W_k, W_v, W_o, P_qk, P_vo, n_heads: int, n_kv_heads: int,
-                 rope_base: float, batch: int, buffer_tokens: int, capacity: int,
+                 rope_base, batch: int, buffer_tokens: int, capacity: int,
                  k_active: Sequence[int], k_value: Optional[Sequence[int]] = None,
-                 sparse_values: str = "same", q_norm=None, k_norm=None, norm_eps: float = 1e-6):
+                 sparse_values: str = "same", q_norm=None, k_norm=None, norm_eps: float = 1e-6,
+                 window: Optional[int] = None, sinks: int = 0):
         """W_q [hidden][n_heads*128], W_k and W_v [hidden][n_kv*128], W_o
         [n_heads*128][hidden] (float16 or float32, cuda); P_qk, P_vo [n_kv][128][128]
         float32 (swan_calibrate_rotation of post-RoPE keys and of values).  q_norm, k_norm:
-        weights of the heads' norms before RoPE ([128], or [heads][128]; None: no norm)."""
+        weights of the heads' norms before RoPE ([128], or [heads][128]; None: no norm).
+        rope_base: a number, or a swan.Rotary.  window: a row sees the last `window` tokens up
+        to itself and the first `sinks` (None: all)."""
         import torch
+
+        swan._window(window, sinks)
+        if window is not None and (window < 1 or sinks < 0):
+            raise ValueError(f"window {window} < 1 or sinks {sinks} < 0")
+        self.window, self.sinks = window, sinks
 
         d = HEAD_DIM
         self.n_heads, self.n_kv_heads = n_heads, n_kv_heads
-        self.rope_base = float(rope_base)
+        self.rope_base = rope_base if isinstance(rope_base, swan.Rotary) else float(rope_base)
         self.dtype = W_q.dtype
         self.P_qk = P_qk.contiguous()
         G = n_heads // n_kv_heads
@@ -153,6 +164,10 @@ class SwanAttentionLayer:
 
     prefix: Optional[swan.Prefix] = None
     _prefix_len: Optional[Sequence[int]] = None  # of the prefix's cache, at the fork
+    _prefix_dropped: Optional[Sequence[int]] = None  # tokens that compact() had left out of it
+    _dropped: Optional[Sequence[int]] = None  # tokens that compact() left out, per sequence
+    window: Optional[int] = None
+    sinks = 0
     q_norm = k_norm = None
     norm_eps = 1e-6
 
@@ -176,23 +191,80 @@ class SwanAttentionLayer:
                                    sparse_values=sparse_values, k_value=k_value)
         new.prefix = swan.Prefix(self.cache, of)
         new._prefix_len = list(self.cache.seq_len)
+        new._prefix_dropped, new._dropped = self._dropped, None
+        self._hand_project(new)
+        return new
+
+    def _hand_project(self, new) -> None:
         own = vars(self).get("project")
         if own is not None:
             mine = getattr(own, "__self__", None) is self
             new.project = types.MethodType(own.__func__ if mine else _no_project, new)
+
+    def select(self, of: Sequence[int], capacity: Optional[int] = None) -> "SwanAttentionLayer":
+        """A layer with the same weights for len(of) sequences, sequence b a copy of this
+        layer's sequence of[b] (the hypotheses of a search in a new order, a batch without the
+        finished ones), with cache arrays of its own; a prefix stays shared.  A project()
+        replaced on this object goes over as in fork."""
+        of = [int(p) for p in of]
+        if any(not 0 <= p < self.cache.batch for p in of):
+            raise ValueError(f"of must be sequences of this layer, 0..{self.cache.batch - 1}")
+        self.positions()  # (refuses a prefix that has grown)
+        new = copy.copy(self)
+        new.cache = self.cache.select(of, sparse_capacity=capacity)
+        if self._dropped is not None:
+            new._dropped = [self._dropped[p] for p in of]
+        if self.prefix is not None:
+            new.prefix = swan.Prefix(self.prefix.cache, [self._prefix_of()[p] for p in of])
+        self._hand_project(new)
         return new
+
+    def compact(self, capacity: Optional[int] = None):
+        """Leaves out of the cache the pruned tokens that no later row sees through the window,
+        with room for `capacity` pruned tokens from now on (None: as before).  The tokens kept
+        are copied as they are, so later results stay the same.  Returns how many were left out
+        of each sequence."""
+        if self.window is None:
+            raise ValueError("a layer without a window sees every token")
+        first = self._own_sinks(0)
+        drop = self.cache.outside(self.window, first)
+        cache = self.cache.select(range(self.cache.batch), first, drop, sparse_capacity=capacity)
+        self._dropped = [a + b for a, b in zip(self._dropped or [0] * len(drop), drop)]
+        self.cache = cache
+        return drop
+
+    def _prefix_of(self):
+        return self.prefix.of or [0] * self.cache.batch
+
+    def _cached_before(self):
+        """Tokens held before each sequence's own."""
+        if self.prefix is None:
+            return [0] * self.cache.batch
+        lens = self.prefix.cache.seq_len
+        return [lens[p] if p >= 0 else 0 for p in self._prefix_of()]
+
+    def _own_sinks(self, own_tokens):
+        """What the prefix and `own_tokens` (a number, or one per sequence) leave of the first
+        tokens that stay visible."""
+        before = self._cached_before()
+        own = [own_tokens] * len(before) if isinstance(own_tokens, int) else own_tokens
+        return [max(0, self.sinks - b - L) for b, L in zip(before, own)]
 
     def positions(self):
         """The position of each sequence's next token."""
+        own = self.cache.seq_len
+        if self._dropped is not None:
+            own = [L + d for L, d in zip(own, self._dropped)]
         if self.prefix is None:
-            return self.cache.seq_len
-        before = self.prefix.cache.seq_len
-        of = self.prefix.of or [0] * self.cache.batch
+            return own
+        before, of = self.prefix.cache.seq_len, self._prefix_of()
         if self._prefix_len is not None and any(p >= 0 and before[p] != self._prefix_len[p]
                                                 for p in of):
             raise ValueError(f"the layer that this one was forked from has grown: its lengths "
                              f"were {self._prefix_len}, are {before}")
-        return [L + (before[p] if p >= 0 else 0) for L, p in zip(self.cache.seq_len, of)]
+        if self._prefix_dropped is not None:
+            before = [L + d for L, d in zip(before, self._prefix_dropped)]
+        return [L + (before[p] if p >= 0 else 0) for L, p in zip(own, of)]
 
     def project(self, x):
         """Post-RoPE q [B][H_q][n][128], k and v_hat [B][H_kv][n][128] of new rows x
@@ -209,6 +281,9 @@ class SwanAttentionLayer:
         kv = x @ self.W_qkv[:, self.n_heads * HEAD_DIM:]
         return swan.qkv_rows(kv, 0, self.n_kv_heads, self.positions(), self.rope_base, None,
                              self.k_norm, self.norm_eps)[1:]
+
+    def _seen(self):
+        return {} if self.window is None else dict(window=self.window, sinks=self.sinks)
 
     def __call__(self, x, attend: bool = False):
         """x [B][n][hidden]: append the n rows of every sequence to the cache; for a
@@ -227,12 +302,14 @@ class SwanAttentionLayer:
         if n != 1:
             state = None
             if self.prefix is not None or any(self.cache.seq_len):
-                state = self.cache.attend(q, self.P_qk, None, prefix=self.prefix)
-            o_hat = swan.prompt_attention(q, k, v, state=state)
+                state = self.cache.attend(q, self.P_qk, None, prefix=self.prefix, **self._seen())
+            first = {} if self.window is None else dict(
+                window=self.window, sinks=self._own_sinks(self.cache.seq_len))
+            o_hat = swan.prompt_attention(q, k, v, state=state, **first)
             self.cache.append(k, v, self.P_qk, None)
             return o_hat.transpose(1, 2).reshape(B, n, self.n_heads * HEAD_DIM) @ self.W_o_hat
         o_hat = self.cache.step(k, v, q[:, :, 0].contiguous(), self.P_qk, None,
-                                prefix=self.prefix)
+                                prefix=self.prefix, **self._seen())
         return o_hat.view(B, self.n_heads * HEAD_DIM) @ self.W_o_hat
 
 

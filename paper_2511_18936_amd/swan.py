@@ -1,5 +1,5 @@
-"""ctypes binding of libswan (include/swan.h, include/swan_layer.h), plus a small cache
-holder.
+"""ctypes binding of libswan (include/swan.h, include/swan_layer.h, include/swan_long.h), plus
+a small cache holder.
 
 Argument marshalling only: every step of the path runs in the library's HIP
 kernels.  PyTorch provides device memory and the current stream.  If the
@@ -7,7 +7,9 @@ library is missing the import fails loudly; there is no fallback.
 """
 from __future__ import annotations
 
+import copy
 import ctypes
+import math
 import os
 from typing import Optional, Sequence
 
@@ -82,6 +84,16 @@ class PrefixDesc(ctypes.Structure):
     ]
 
 
+class RotaryDesc(ctypes.Structure):
+    """swan_rotary: dims turned, pairs of neighbours or not, magnitude, frequencies."""
+    _fields_ = [
+        ("dims", ctypes.c_int32),
+        ("interleaved", ctypes.c_int32),
+        ("magnitude", ctypes.c_double),
+        ("freq_host", ctypes.POINTER(ctypes.c_double)),
+    ]
+
+
 def _load() -> ctypes.CDLL:
     # torch first: its HIP runtime (soname libamdhip64.so.7) then also serves
     # libswan, so the process holds a single runtime and a single device context
@@ -94,7 +106,7 @@ def _load() -> ctypes.CDLL:
     lib = ctypes.CDLL(LIB_PATH)
     i32, i64, sz, vp = ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.c_void_p
     pi32, psz, pdesc = ctypes.POINTER(i32), ctypes.POINTER(sz), ctypes.POINTER(CacheDesc)
-    pprefix = ctypes.POINTER(PrefixDesc)
+    pprefix, protary = ctypes.POINTER(PrefixDesc), ctypes.POINTER(RotaryDesc)
     lib.swan_last_error.restype = ctypes.c_char_p
     lib.swan_last_error.argtypes = []
     lib.swan_version.restype = i32
@@ -128,6 +140,22 @@ def _load() -> ctypes.CDLL:
                                          ctypes.c_float, vp, vp, sz, vp],
         "swan_decode_step_prefix": [pprefix, pdesc, pi32, pi32, pi32, vp, vp, vp, vp, vp,
                                     ctypes.c_float, vp, vp, sz, vp],
+        "swan_rope_rotary": [vp, vp, i32, i32, i32, i32, i32, pi32, protary, vp],
+        "swan_qkv_rows_rotary": [vp, i64, i64, i32, i32, i32, i32, i32, i32, pi32, protary, vp, vp,
+                                 i32, i32, ctypes.c_double, vp, vp, vp, vp],
+        "swan_prompt_window_workspace_bytes": [i32, i32, i32, i32, i32, i32, i32, pi32, pi32, i32,
+                                               pi32, psz],
+        "swan_prompt_attention_window": [vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, pi32, pi32,
+                                         i32, pi32, ctypes.c_float, vp, vp, vp, vp, sz, vp],
+        "swan_attend_window_workspace_bytes": [pprefix, i32, i32, i32, pi32, i32, i32, psz],
+        "swan_attend_window": [pprefix, i32, i32, i32, pi32, i32, i32, vp, vp, vp, ctypes.c_float,
+                               vp, vp, vp, sz, vp],
+        "swan_decode_window_workspace_bytes": [pprefix, pdesc, pi32, pi32, pi32, i32, i32, psz],
+        "swan_decode_attention_window": [pprefix, pdesc, pi32, pi32, pi32, i32, i32, vp, vp, vp,
+                                         ctypes.c_float, vp, vp, sz, vp],
+        "swan_decode_step_window": [pprefix, pdesc, pi32, pi32, pi32, i32, i32, vp, vp, vp, vp, vp,
+                                    ctypes.c_float, vp, vp, sz, vp],
+        "swan_copy_sequences": [pdesc, pi32, pi32, pi32, pdesc, pi32, pi32, pi32, pi32, pi32, vp],
         "swan_set_decode_tuning": [ctypes.POINTER(DecodeTuning)],
         "swan_set_profile_events": [vp, vp],
     }
@@ -383,11 +411,73 @@ def change_k(src: CacheDesc, k_active_src: Sequence[int], k_value_src: Optional[
                               _i32_array(seq_len), _stream(stream)))
 
 
-def rope(x, pos0: Sequence[int], base: float, out=None, stream=None):
+class Rotary:
+    """How rows are turned to their positions: of a head's first `dims` dims (a multiple of 8)
+    dims j and j + dims/2 are pair j, or with interleaved=True dims 2j and 2j + 1; a pair turns
+    by pos * freqs[j] (None: base^(-2j/dims)) and is multiplied by `magnitude`.  The other dims
+    stay as they are.  Taken by rope, qkv_rows and the layer in the place of a base."""
+
+    def __init__(self, base: float = 10000.0, dims: int = HEAD_DIM, interleaved: bool = False,
+                 freqs: Optional[Sequence[float]] = None, magnitude: float = 1.0):
+        self.dims, self.interleaved = int(dims), bool(interleaved)
+        self.magnitude = float(magnitude)
+        if self.dims < 8 or self.dims > HEAD_DIM or self.dims % 8:
+            raise SwanError(SWAN_ERR_INVALID_ARG,
+                            f"dims {dims}: a multiple of 8 within 8..{HEAD_DIM}")
+        if not self.magnitude > 0 or math.isinf(self.magnitude):
+            raise SwanError(SWAN_ERR_INVALID_ARG, f"magnitude {magnitude}")
+        half = self.dims // 2
+        if freqs is None:
+            if not base > 1 or math.isinf(base):
+                raise SwanError(SWAN_ERR_INVALID_ARG, f"base {base} must be > 1")
+            freqs = [float(base) ** (-j / half) for j in range(half)]
+        freqs = [float(f) for f in freqs]
+        if len(freqs) != half or not all(math.isfinite(f) for f in freqs):
+            raise SwanError(SWAN_ERR_INVALID_ARG, f"freqs must be {half} finite numbers")
+        self.freqs = tuple(freqs)
+        self._freqs = (ctypes.c_double * half)(*freqs)
+        self._desc = RotaryDesc(self.dims, int(self.interleaved), self.magnitude, self._freqs)
+
+    def stretched(self, factor: float) -> "Rotary":
+        """Positions interpolated: every frequency divided by `factor`."""
+        self._check_factor(factor)
+        return self._with([f / factor for f in self.freqs], self.magnitude)
+
+    def by_parts(self, factor: float, original: int, low: float = 1.0, high: float = 32.0,
+                 magnitude: Optional[float] = None) -> "Rotary":
+        """Stretched to `factor` times the `original` context by parts: frequencies that turn
+        fewer than `low` times in it are divided by `factor`, those that turn more than `high`
+        times stay, those between are mixed linearly in their turns.  magnitude: what the
+        present one is multiplied by (None: 0.1 ln(factor) + 1)."""
+        self._check_factor(factor)
+        if not 0 < low < high:
+            raise SwanError(SWAN_ERR_INVALID_ARG, f"low {low} and high {high}: 0 < low < high")
+        if magnitude is None:
+            magnitude = 0.1 * math.log(factor) + 1.0 if factor > 1 else 1.0
+        freqs = []
+        for f in self.freqs:
+            keep = min(1.0, max(0.0, (original * f / (2 * math.pi) - low) / (high - low)))
+            freqs.append(keep * f + (1 - keep) * f / factor)
+        return self._with(freqs, self.magnitude * magnitude)
+
+    @staticmethod
+    def _check_factor(factor: float) -> None:
+        if not factor > 0 or math.isinf(factor):
+            raise SwanError(SWAN_ERR_INVALID_ARG, f"factor {factor} must be finite, > 0")
+
+    def _with(self, freqs, magnitude: float) -> "Rotary":
+        return Rotary(dims=self.dims, interleaved=self.interleaved, freqs=freqs,
+                      magnitude=magnitude)
+
+
+def rope(x, pos0: Sequence[int], base, out=None, stream=None):
     """RoPE of rows x [B][H][n][128] (float16 or float32, cuda) at positions pos0[b] + i;
-    out=None writes a new tensor, out=x works in place."""
+    out=None writes a new tensor, out=x works in place.  base: a number (dims j and j + 64 of
+    the whole head, base^(-2j/128)), or a Rotary."""
     import torch
 
+    if isinstance(base, Rotary):
+        return _rope_rotary(x, pos0, base, out, stream)
     if out is None:
         out = torch.empty_like(x) if stream is None else _result_like(x, x.shape, stream)
     B, H, n, d = x.shape
@@ -395,6 +485,31 @@ def rope(x, pos0: Sequence[int], base: float, out=None, stream=None):
     _check(_lib.swan_rope(_ptr(x), _ptr(out), code, B, H, n, d, _i32_array(pos0), float(base),
                           _stream(stream)))
     return out
+
+
+def _rope_rotary(x, pos0: Sequence[int], rotary: Rotary, out, stream):
+    if x.dim() != 4:
+        raise SwanError(SWAN_ERR_INVALID_ARG, "x must be [B][H][n][128]")
+    code = _storage_code(x.dtype)
+    B, H, n, d = x.shape
+    _tensor(x, "x", x.dtype, (B, H, n, HEAD_DIM))
+    _on_gpu(x=x)
+    if out is None:
+        out = _result_like(x, x.shape, stream)
+    _tensor(out, "out", x.dtype, (B, H, n, HEAD_DIM))
+    if out is not x and out.data_ptr() != x.data_ptr() and _share(x, out):
+        raise SwanError(SWAN_ERR_INVALID_ARG, "out overlaps x without being it")
+    with _CallsOn(_same_gpu(x=x, out=out), stream) as s:
+        _check(_lib.swan_rope_rotary(_ptr(x), _ptr(out), code, B, H, n, d,
+                                     _per_sequence(pos0, B, "pos0"), ctypes.byref(rotary._desc),
+                                     s))
+    return out
+
+
+def _share(a, b) -> bool:
+    """Whether two contiguous tensors share a byte."""
+    a0, b0 = a.data_ptr(), b.data_ptr()
+    return (a0 < b0 + b.numel() * b.element_size() and b0 < a0 + a.numel() * a.element_size())
 
 
 def _same_gpu(**tensors):
@@ -488,13 +603,13 @@ def _result_like(t, shape, stream):
     return t.new_empty(shape) if stream is None else _result("empty", shape, t.dtype, t.device, stream)
 
 
-def qkv_rows(qkv, n_q_heads: int, n_kv_heads: int, pos0: Sequence[int], base: float,
+def qkv_rows(qkv, n_q_heads: int, n_kv_heads: int, pos0: Sequence[int], base,
              q_weight=None, k_weight=None, eps: float = 1e-6, out=None, stream=None):
     """A layer's projections qkv [B][n][(n_q + 2 n_kv) * 128] (float16 or float32, cuda; rows
     may be strided) as q [B][n_q][n][128], k and v [B][n_kv][n][128]: q and k divided by
     their root mean square and weighted (q_weight / k_weight: [128], or [heads][128], of
     qkv's type or float32; None: no norm), then rotated to positions pos0[b] + i as by
-    rope(); v as it is.  out = (q, k, v) writes existing tensors; n_q_heads = 0 gives
+    rope() (base: a number or a Rotary); v as it is.  out = (q, k, v) writes existing tensors; n_q_heads = 0 gives
     (None, k, v)."""
     if qkv.dim() != 3:
         raise SwanError(SWAN_ERR_INVALID_ARG, "qkv must be [B][n][(n_q + 2 n_kv) * 128]")
@@ -528,11 +643,12 @@ def qkv_rows(qkv, n_q_heads: int, n_kv_heads: int, pos0: Sequence[int], base: fl
         device = _same_gpu(qkv=qkv, q=q, k=k, v=v, q_weight=q_weight, k_weight=k_weight)
     # (a dimension of one element has no stride of its own)
     with _CallsOn(device, stream) as s:
-        _check(_lib.swan_qkv_rows(_ptr(qkv), seq if B > 1 else 0, row if n > 1 else width, code, B,
-                                  n_q_heads, n_kv_heads, n, HEAD_DIM,
-                                  _per_sequence(pos0, B, "pos0"), base, _ptr(q_weight),
-                                  _ptr(k_weight), per_head, w32, eps, _ptr(q), _ptr(k), _ptr(v),
-                                  s))
+        call, how = _lib.swan_qkv_rows, base
+        if isinstance(base, Rotary):
+            call, how = _lib.swan_qkv_rows_rotary, ctypes.byref(base._desc)
+        _check(call(_ptr(qkv), seq if B > 1 else 0, row if n > 1 else width, code, B, n_q_heads,
+                    n_kv_heads, n, HEAD_DIM, _per_sequence(pos0, B, "pos0"), how, _ptr(q_weight),
+                    _ptr(k_weight), per_head, w32, eps, _ptr(q), _ptr(k), _ptr(v), s))
     return q, k, v
 
 
@@ -557,13 +673,18 @@ def _norm_weights(dtype, n_q_heads: int, n_kv_heads: int, q_weight, k_weight):
 
 def prompt_attention(q, k, v, causal: bool = True, n: Optional[Sequence[int]] = None,
                      m: Optional[Sequence[int]] = None, scale: float = 0.0, state=None, out=None,
-                     workspace=None, stream=None):
+                     workspace=None, stream=None, window: Optional[int] = None, sinks=0):
     """Dense attention of rows q [B][H_q][n][128] over k, v [B][H_kv][m][128] (float16 or
     float32, cuda): a prompt's (causal: row i sees keys j <= i + m_b - n_b) or rows over
     another sequence's keys and values (causal=False).  n / m: the rows used of each
     sequence (None: all); the others are not read, and out's rows past n_b not written
     (zeros where out is None).  state: what SwanCache.attend or attend returned for these
-    rows, to continue from."""
+    rows, to continue from.  window (causal only): a row sees the last `window` keys up to
+    itself, and the first `sinks` (a number, or one per sequence; behind cached tokens what
+    those leave of them: max(0, sinks - cached tokens))."""
+    _window(window, sinks)
+    if window is not None and not causal:
+        raise SwanError(SWAN_ERR_INVALID_ARG, "a window needs causal=True")
     if q.dim() != 4 or k.dim() != 4:
         raise SwanError(SWAN_ERR_INVALID_ARG, "q, k and v must be [B][heads][rows][128]")
     code = _storage_code(q.dtype)
@@ -580,17 +701,34 @@ def prompt_attention(q, k, v, causal: bool = True, n: Optional[Sequence[int]] = 
     device = _same_gpu(q=q, k=k, v=v, out=out, o=o0, lse=lse0)
     ns, ms = _per_sequence(n, B, "n"), _per_sequence(m, B, "m")
     need = ctypes.c_size_t()
-    _check(_lib.swan_prompt_workspace_bytes(code, B, hq, hkv, nq, nk, d, ns, ms, int(causal),
-                                            ctypes.byref(need)))
+    bytes_of, call, how = _lib.swan_prompt_workspace_bytes, _lib.swan_prompt_attention, ()
+    if window is None:
+        how = (int(causal),)
+    else:
+        bytes_of = _lib.swan_prompt_window_workspace_bytes
+        call = _lib.swan_prompt_attention_window
+        first = [sinks] * B if isinstance(sinks, int) else sinks
+        how = (window, _per_sequence(first, B, "sinks"))
+    _check(bytes_of(code, B, hq, hkv, nq, nk, d, ns, ms, *how, ctypes.byref(need)))
     ws = None
     if need.value:
         ws = _workspace(workspace, need.value, device, stream)
     with _CallsOn(device, stream) as s:
-        _check(_lib.swan_prompt_attention(
-            _ptr(q), _ptr(k), _ptr(v), code, B, hq, hkv, nq, nk, d, ns, ms, int(causal),
-            float(scale), _ptr(o0), _ptr(lse0), _ptr(out), _ptr(ws),
-            0 if ws is None else ws.numel() * ws.element_size(), s))
+        _check(call(_ptr(q), _ptr(k), _ptr(v), code, B, hq, hkv, nq, nk, d, ns, ms, *how,
+                    float(scale), _ptr(o0), _ptr(lse0), _ptr(out), _ptr(ws),
+                    0 if ws is None else ws.numel() * ws.element_size(), s))
     return out
+
+
+def _window(window, sinks) -> None:
+    if window is None and (not isinstance(sinks, int) or sinks != 0):
+        raise SwanError(SWAN_ERR_INVALID_ARG, "sinks without a window")
+    for x in (window, sinks):
+        if isinstance(x, (bool, float)):
+            raise SwanError(SWAN_ERR_INVALID_ARG, f"window and sinks are whole numbers, not {x}")
+    # (ctypes would take such a number's low 32 bits)
+    if window is not None and window > 2**31 - 1 or isinstance(sinks, int) and sinks > 2**31 - 1:
+        raise SwanError(SWAN_ERR_INVALID_ARG, f"window {window} or sinks {sinks} too large")
 
 
 def _state(state, B: int, heads: int, n: int):
@@ -624,12 +762,15 @@ class Prefix:
 
 
 def attend(sources, q, P_qk, P_vo, n: Optional[Sequence[int]] = None, scale: float = 0.0,
-           out=None, workspace=None, stream=None):
+           out=None, workspace=None, stream=None, window: Optional[int] = None, sinks: int = 0):
     """Rows q [B][H_q][n][128] over all cached tokens of one or two sources (Prefix objects:
     a shared prefix, the sequences' own caches), none masked: the state (o [B][H_q][n][128],
     lse [B][H_q][n]) in float32 that prompt_attention continues from.  n: the rows used of
     each sequence (None: all); the others are not read, and not written (zeros where out
-    is None).  P_vo None leaves o rotated."""
+    is None).  P_vo None leaves o rotated.  window: row i, standing i positions behind the
+    cached tokens, sees those of the last `window` positions up to itself, and the first
+    `sinks`."""
+    _window(window, sinks)
     sources = list(sources)
     if not sources:
         raise SwanError(SWAN_ERR_INVALID_ARG, "no sources")
@@ -651,12 +792,15 @@ def attend(sources, q, P_qk, P_vo, n: Optional[Sequence[int]] = None, scale: flo
     descs = (PrefixDesc * len(sources))(*[s._desc(B) for s in sources])
     ns = _per_sequence(n, B, "n")
     need = ctypes.c_size_t()
-    _check(_lib.swan_attend_workspace_bytes(descs, len(sources), B, nq, ns, ctypes.byref(need)))
+    bytes_of, call, how = _lib.swan_attend_workspace_bytes, _lib.swan_attend, ()
+    if window is not None:
+        bytes_of, call = _lib.swan_attend_window_workspace_bytes, _lib.swan_attend_window
+        how = (window, sinks)
+    _check(bytes_of(descs, len(sources), B, nq, ns, *how, ctypes.byref(need)))
     ws = _workspace(workspace, need.value, device, stream)
     with _CallsOn(device, stream) as s:
-        _check(_lib.swan_attend(descs, len(sources), B, nq, ns, _ptr(q), _ptr(P_qk), _ptr(P_vo),
-                                float(scale), _ptr(o), _ptr(lse), _ptr(ws),
-                                ws.numel() * ws.element_size(), s))
+        _check(call(descs, len(sources), B, nq, ns, *how, _ptr(q), _ptr(P_qk), _ptr(P_vo),
+                    float(scale), _ptr(o), _ptr(lse), _ptr(ws), ws.numel() * ws.element_size(), s))
     return o, lse
 
 
@@ -714,6 +858,71 @@ def prefix_workspace_bytes(prefix: Prefix, desc: CacheDesc, seq_len: Sequence[in
     return out.value
 
 
+def decode_window_workspace_bytes(desc: CacheDesc, seq_len: Sequence[int],
+                                  k_active: Sequence[int], window: int, sinks: int = 0,
+                                  k_value: Optional[Sequence[int]] = None,
+                                  prefix: Optional[Prefix] = None) -> int:
+    _window(window, sinks)
+    out = ctypes.c_size_t()
+    p = None if prefix is None else ctypes.byref(prefix._desc(desc.batch))
+    _check(_lib.swan_decode_window_workspace_bytes(
+        p, ctypes.byref(desc), _per_sequence(seq_len, desc.batch, "seq_len"),
+        _per_sequence(k_active, desc.batch, "k_active"),
+        _per_sequence(k_value, desc.batch, "k_value"), window, sinks, ctypes.byref(out)))
+    return out.value
+
+
+def decode_window(desc: CacheDesc, seq_len: Sequence[int], k_active: Sequence[int], q, P_qk, P_vo,
+                  out, workspace, window: int, sinks: int = 0, scale: float = 0.0, stream=None,
+                  k_value: Optional[Sequence[int]] = None, prefix: Optional[Prefix] = None,
+                  new=None) -> None:
+    """swan_decode_attention_window, or with new = (k_new, v_new) swan_decode_step_window
+    (seq_len: lengths before it), behind a prefix where one is given."""
+    _window(window, sinks)
+    if window is None:
+        raise SwanError(SWAN_ERR_INVALID_ARG, "window is None")
+    _decode_tensors(desc, q, P_qk, P_vo, out)
+    k_new, v_new = new or (None, None)
+    if new is not None:
+        et = _elem_torch_dtype(desc.dtype)
+        shape = (desc.batch, desc.n_kv_heads, 1, desc.head_dim)
+        _tensor(k_new, "k_new", et, shape)
+        _tensor(v_new, "v_new", et, shape)
+    if workspace is None or not workspace.is_cuda or not workspace.is_contiguous():
+        raise SwanError(SWAN_ERR_WORKSPACE, "workspace must be a contiguous GPU tensor")
+    device = _same_gpu(q=q, out=out, P_qk=P_qk, P_vo=P_vo, k_new=k_new, v_new=v_new,
+                       workspace=workspace,
+                       prefix=None if prefix is None else prefix.cache.k_pages)
+    p = None if prefix is None else ctypes.byref(prefix._desc(desc.batch))
+    B = desc.batch
+    head = (p, ctypes.byref(desc), _per_sequence(seq_len, B, "seq_len"),
+            _per_sequence(k_active, B, "k_active"), _per_sequence(k_value, B, "k_value"), window,
+            sinks)
+    tail = (_ptr(q), _ptr(P_qk), _ptr(P_vo), float(scale), _ptr(out), _ptr(workspace),
+            workspace.numel() * workspace.element_size())
+    with _CallsOn(device, stream) as s:
+        if new is None:
+            _check(_lib.swan_decode_attention_window(*head, *tail, s))
+        else:
+            _check(_lib.swan_decode_step_window(*head, _ptr(k_new), _ptr(v_new), *tail, s))
+
+
+def copy_sequences(src: CacheDesc, src_len: Sequence[int], k_active_src: Sequence[int],
+                   k_value_src: Optional[Sequence[int]], dst: CacheDesc,
+                   k_active_dst: Sequence[int], k_value_dst: Optional[Sequence[int]],
+                   of: Sequence[int], first: Optional[Sequence[int]] = None,
+                   drop: Optional[Sequence[int]] = None, stream=None) -> None:
+    """Sequences of src to places of dst (see swan_copy_sequences)."""
+    _check(_lib.swan_copy_sequences(
+        ctypes.byref(src), _per_sequence(src_len, src.batch, "src_len"),
+        _per_sequence(k_active_src, src.batch, "k_active_src"),
+        _per_sequence(k_value_src, src.batch, "k_value_src"), ctypes.byref(dst),
+        _per_sequence(k_active_dst, dst.batch, "k_active_dst"),
+        _per_sequence(k_value_dst, dst.batch, "k_value_dst"),
+        _per_sequence(of, dst.batch, "of"), _per_sequence(first, dst.batch, "first"),
+        _per_sequence(drop, dst.batch, "drop"), _stream(stream)))
+
+
 def set_decode_tuning(target_waves: int = 0, short_split_pages: int = 0, merge_pct: int = 0,
                       side_streams: int = 0) -> None:
     """Split plan and launch grouping of the decode calls on this thread
@@ -760,17 +969,22 @@ class SwanCache:
         self.desc = CacheDesc(batch, n_q_heads, n_kv_heads, head_dim, buffer_tokens,
                               sparse_capacity, dtype_code(dtype, sparse_values), 0, None, None,
                               None, None)
-        kb, vb, rb = cache_bytes(self.desc, self.k_active, self.k_value)
+        self._allocate(None)
+
+    def _allocate(self, stream) -> None:
+        """The arrays that desc describes, zeroed, for work on `stream`."""
+        d = self.desc
+        kb, vb, rb = cache_bytes(d, self.k_active, self.k_value)
         # torch's caching allocator returns 256-byte aligned blocks
-        self.k_pages = torch.zeros(max(kb, 16), dtype=torch.uint8, device=self.device)
-        self.v_pages = torch.zeros(max(vb, 16), dtype=torch.uint8, device=self.device)
-        shape = (batch, n_kv_heads, buffer_tokens, head_dim)
-        self.k_ring = torch.zeros(shape, dtype=dtype, device=self.device)
-        self.v_ring = torch.zeros(shape, dtype=dtype, device=self.device)
-        self.desc.k_pages = self.k_pages.data_ptr()
-        self.desc.v_pages = self.v_pages.data_ptr()
-        self.desc.k_ring = self.k_ring.data_ptr() if buffer_tokens > 0 else None
-        self.desc.v_ring = self.v_ring.data_ptr() if buffer_tokens > 0 else None
+        self.k_pages = _result("zeros", max(kb, 16), "uint8", self.device, stream)
+        self.v_pages = _result("zeros", max(vb, 16), "uint8", self.device, stream)
+        shape = (d.batch, d.n_kv_heads, d.buffer_tokens, d.head_dim)
+        self.k_ring = _result("zeros", shape, self.dtype, self.device, stream)
+        self.v_ring = _result("zeros", shape, self.dtype, self.device, stream)
+        d.k_pages = self.k_pages.data_ptr()
+        d.v_pages = self.v_pages.data_ptr()
+        d.k_ring = self.k_ring.data_ptr() if d.buffer_tokens > 0 else None
+        d.v_ring = self.v_ring.data_ptr() if d.buffer_tokens > 0 else None
 
     @property
     def batch(self) -> int:
@@ -809,14 +1023,64 @@ class SwanCache:
         self.desc, self.k_pages, self.v_pages = dst, k_pages, v_pages
         self.k_active, self.k_value = k_active, k_value
 
+    def outside(self, window: int, sinks=0):
+        """Per sequence, how many pruned tokens after the first `sinks` (a number, or one per
+        sequence) no later row with this window sees: the `drop` that copy_from and select can
+        leave out from first=sinks on."""
+        if window < 1:
+            raise SwanError(SWAN_ERR_INVALID_ARG, f"window {window} < 1")
+        b = self.desc.buffer_tokens
+        first = [sinks] * self.batch if isinstance(sinks, int) else list(sinks)
+        return [max(0, min(L - window + 1, L - b) - f) for L, f in zip(self.seq_len, first)]
+
+    def copy_from(self, src: "SwanCache", of: Sequence[int], first=0,
+                  drop: Optional[Sequence[int]] = None, stream=None) -> None:
+        """Sequence b becomes sequence of[b] of another cache `src` (-1: it stays as it is; one
+        may be taken several times), without its tokens first .. first + drop[b] - 1 (pruned
+        ones; first: a number, or one per sequence).  The tokens behind move up: keys keep the
+        positions they were turned to, so a caller that counts positions adds drop[b]."""
+        of = [int(p) for p in of]
+        first = [first] * self.batch if isinstance(first, int) else list(first)
+        device = _same_gpu(src=src.k_pages, dst=self.k_pages)
+        with _CallsOn(device, stream):
+            copy_sequences(src.desc, src.seq_len, src.k_active, src.k_value, self.desc,
+                           self.k_active, self.k_value, of, first, drop,
+                           stream)
+        for b, p in enumerate(of):
+            if p >= 0:
+                self.seq_len[b] = src.seq_len[p] - (0 if drop is None else int(drop[b]))
+
+    def select(self, of: Sequence[int], first=0, drop: Optional[Sequence[int]] = None,
+               sparse_capacity: Optional[int] = None, stream=None) -> "SwanCache":
+        """A new cache of len(of) sequences, sequence b a copy of sequence of[b] (-1: empty):
+        forks, a new order, without finished sequences, with another capacity, or (first, drop
+        as in copy_from) without tokens that are not needed any more."""
+        of = [int(p) for p in of]
+        if any(not -1 <= p < self.batch for p in of):
+            raise ValueError(f"of must be sequences of this cache, -1..{self.batch - 1}")
+        new = copy.copy(self)
+        new.k_active = [self.k_active[max(p, 0)] for p in of]
+        new.k_value = None if self.k_value is None else [self.k_value[max(p, 0)] for p in of]
+        new.seq_len = [0] * len(of)
+        d = self.desc
+        new.desc = CacheDesc(len(of), d.n_q_heads, d.n_kv_heads, d.head_dim, d.buffer_tokens,
+                             d.sparse_capacity if sparse_capacity is None else sparse_capacity,
+                             d.dtype, 0, None, None, None, None)
+        new._allocate(stream)
+        new.copy_from(self, of, first, drop, stream)
+        return new
+
     def workspace(self, seq_len: Optional[Sequence[int]] = None, prefix: Optional[Prefix] = None,
-                  stream=None):
+                  stream=None, window: Optional[int] = None, sinks: int = 0):
         """A decode workspace for these lengths (default: the present ones), of the caching
         allocator's memory for `stream` (or, captured, for its graph).  decode() and step()
         take one for each call, so calls on several streams, and graphs that are replayed
         beside them, share none."""
         lens = self.seq_len if seq_len is None else seq_len
-        if prefix is None:
+        if window is not None:
+            need = decode_window_workspace_bytes(self.desc, lens, self.k_active, window, sinks,
+                                                 self.k_value, prefix)
+        elif prefix is None:
             need = decode_workspace_bytes(self.desc, lens, self.k_active, self.k_value)
         else:
             need = prefix_workspace_bytes(prefix, self.desc, lens, self.k_active, self.k_value)
@@ -824,19 +1088,27 @@ class SwanCache:
 
     def attend(self, q, P_qk, P_vo, of: Optional[Sequence[int]] = None,
                n: Optional[Sequence[int]] = None, scale: float = 0.0,
-               prefix: Optional[Prefix] = None, out=None, workspace=None, stream=None):
+               prefix: Optional[Prefix] = None, out=None, workspace=None, stream=None,
+               window: Optional[int] = None, sinks: int = 0):
         """Rows q [B][H_q][n][128] over all tokens of this cache, of sequence of[b] for query
-        sequence b (-1: none; None: its own, b), and of a prefix: see attend()."""
+        sequence b (-1: none; None: its own, b), and of a prefix, or over those that a window
+        shows: see attend()."""
         own = Prefix(self, range(self.batch) if of is None else of)
         return attend([own] if prefix is None else [prefix, own], q, P_qk, P_vo, n, scale, out,
-                      workspace, stream)
+                      workspace, stream, window, sinks)
 
     def decode(self, q, P_qk, P_vo, out=None, scale: float = 0.0, stream=None,
-               prefix: Optional[Prefix] = None):
-        """Attention of q ([B][H_q][d]) over the cache, behind a prefix where one is given."""
+               prefix: Optional[Prefix] = None, window: Optional[int] = None, sinks: int = 0):
+        """Attention of q ([B][H_q][d]) over the cache, behind a prefix where one is given.
+        window: over the last `window` tokens and the first `sinks` alone."""
+        _window(window, sinks)
         if out is None:
             out = _result_like(q, q.shape, stream)
-        if prefix is None:
+        if window is not None:
+            decode_window(self.desc, self.seq_len, self.k_active, q, P_qk, P_vo, out,
+                          self.workspace(None, prefix, stream, window, sinks), window, sinks,
+                          scale, stream, self.k_value, prefix)
+        elif prefix is None:
             decode_attention(self.desc, self.seq_len, self.k_active, q, P_qk, P_vo, out,
                              self.workspace(None, None, stream), scale, stream, self.k_value)
         else:
@@ -846,15 +1118,19 @@ class SwanCache:
         return out
 
     def step(self, k_new, v_new, q, P_qk, P_vo, out=None, scale: float = 0.0, stream=None,
-             prefix: Optional[Prefix] = None):
+             prefix: Optional[Prefix] = None, window: Optional[int] = None, sinks: int = 0):
         """One decode step (swan_decode_step): append k_new / v_new ([B][H_kv][1][d]),
         advance the lengths, and return the attention of q ([B][H_q][d]) over the cache,
-        behind a prefix where one is given."""
+        behind a prefix where one is given; window, sinks as in decode()."""
+        _window(window, sinks)
         if out is None:
             out = _result_like(q, q.shape, stream)
         after = [L + 1 for L in self.seq_len]
-        ws = self.workspace(after, prefix, stream)
-        if prefix is None:
+        ws = self.workspace(after, prefix, stream, window, sinks)
+        if window is not None:
+            decode_window(self.desc, self.seq_len, self.k_active, q, P_qk, P_vo, out, ws, window,
+                          sinks, scale, stream, self.k_value, prefix, (k_new, v_new))
+        elif prefix is None:
             decode_step(self.desc, self.seq_len, self.k_active, k_new, v_new, q, P_qk, P_vo, out,
                         ws, scale, stream, self.k_value)
         else:
