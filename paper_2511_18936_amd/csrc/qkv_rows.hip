@@ -14,7 +14,7 @@
 // 12 + 2 x 4 float32 heads 9.6 us.  Single tokens (4 x 48 heads) 3 us, the chain of pow and
 // sincos.
 #include "rotary.h"
-#include "swan_layer_ops.h"
+#include "swan_cache_ops.h"
 
 namespace swan {
 
@@ -169,6 +169,7 @@ __global__ __launch_bounds__(256) void qkv_rows_kernel(QkvRowsLaunch a, int head
   using Vec = Four<T>;
   const int t = threadIdx.x, wave = t >> 6, p = (t >> 4) & 3, l = t & 15;
   const int h0 = blockIdx.y * heads, h1 = min(a.Hq + 2 * a.Hkv, h0 + heads);
+  const int64_t step = kForm == 0 ? kD : a.head;
   const uint32_t n = (uint32_t)a.n, positions = (uint32_t)a.B * n;  // below 2^31
   const uint32_t tiles = (positions + kTilePos - 1) / kTilePos;
   const double freq = pair_freq<kForm>(f, a.base, t & 63);
@@ -210,11 +211,11 @@ __global__ __launch_bounds__(256) void qkv_rows_kernel(QkvRowsLaunch a, int head
         for (int h = max(first, h0) + wave; h < last; h += 8) {
           const bool two = h + 4 < last;
           Vec lo[2], hi[2];
-          lo[0] = *(const Vec*)(row + h * kD + at0);
-          hi[0] = *(const Vec*)(row + h * kD + at1);
+          lo[0] = *(const Vec*)(row + h * step + at0);
+          hi[0] = *(const Vec*)(row + h * step + at1);
           if (two) {
-            lo[1] = *(const Vec*)(row + (h + 4) * kD + at0);
-            hi[1] = *(const Vec*)(row + (h + 4) * kD + at1);
+            lo[1] = *(const Vec*)(row + (h + 4) * step + at0);
+            hi[1] = *(const Vec*)(row + (h + 4) * step + at1);
           }
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
@@ -245,7 +246,7 @@ __global__ __launch_bounds__(64) void qkv_rows_few_kernel(QkvRowsLaunch a, FormA
   const int l = threadIdx.x, i = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
   const bool turn = turned<kForm>(f, l);
   const int at0 = place<kForm, 1>(f, l, false), gap = place<kForm, 1>(f, l, true) - at0;
-  const T* row = (const T*)a.x + b * a.seq + i * a.row + (int64_t)h * kD + at0;
+  const T* row = (const T*)a.x + b * a.seq + i * a.row + h * (kForm == 0 ? kD : a.head) + at0;
   const T lo = row[0], hi = row[gap];
   const int role = h < a.Hq ? 0 : h < a.Hq + a.Hkv ? 1 : 2;
   const int hr = role == 0 ? h : role == 1 ? h - a.Hq : h - a.Hq - a.Hkv;

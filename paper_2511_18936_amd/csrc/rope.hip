@@ -5,7 +5,8 @@
 // the angle pos * base^(-2j/128) ("rotate half" pairing), computed in float64
 // and rounded once to the storage type, so the rows are what the cache's exact
 // rotation then sees.
-#include "rotary.h"
+#include "swan_cache_ops.h"
+#include "swan_device.h"
 
 namespace swan {
 
@@ -28,9 +29,8 @@ __device__ __forceinline__ void one_nan_of(T& y) {
 //
 // What bounds it: memory.  32 heads x 1999 positions, binary16: 46 us with pow and
 // sincos for every row, 14.8 us now; 16 x 32 heads x 8192: 2.45, 0.62 ms.
-template <typename T, int kForm>
-__global__ __launch_bounds__(256) void rope_kernel(RopeLaunch a, int heads, int chunks,
-                                                   FormArg<kForm> f) {
+template <typename T>
+__global__ __launch_bounds__(256) void rope_kernel(RopeLaunch a, int heads, int chunks) {
   constexpr int E = 2;
   const int lane = threadIdx.x & 63;
   const int l = lane & 31, first = lane >> 5;
@@ -39,9 +39,7 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeLaunch a, int heads, int 
   const int64_t items = (int64_t)a.B * a.n * chunks;
   double freq[E];
 #pragma unroll
-  for (int e = 0; e < E; ++e) freq[e] = pair_freq<kForm>(f, a.base, E * l + e);
-  const bool turn = turned<kForm>(f, E * l);
-  const int at0 = place<kForm, E>(f, E * l, false), at1 = place<kForm, E>(f, E * l, true);
+  for (int e = 0; e < E; ++e) freq[e] = pow(a.base, -(2.0 * (E * l + e)) / kD);
   for (int64_t w = (int64_t)blockIdx.x * wpb + (threadIdx.x >> 6); w < items; w += waves) {
     const int chunk = (int)(w % chunks);
     const int64_t at = w / chunks;
@@ -49,22 +47,16 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeLaunch a, int heads, int 
     const double pos = (double)a.pos0[b] + (double)i;
     double s[E], c[E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) pair_turn<kForm>(f, pos * freq[e], s[e], c[e]);
+    for (int e = 0; e < E; ++e) sincos(pos * freq[e], &s[e], &c[e]);
     const int h1 = min(a.H, (chunk + 1) * heads);
 #pragma unroll 4
     for (int h = chunk * heads + first; h < h1; h += E) {
-      const int64_t off = (((int64_t)b * a.H + h) * a.n + i) * kD;
+      const int64_t off = (((int64_t)b * a.H + h) * a.n + i) * kD + E * l;
       struct alignas(E * sizeof(T)) Vec {
         T v[E];
       };
-      Vec lo = *(const Vec*)((const T*)a.x + off + at0);
-      Vec hi = *(const Vec*)((const T*)a.x + off + at1);
-      if (kForm != 0 && !turn) {
-        *(Vec*)((T*)a.y + off + at0) = lo;
-        *(Vec*)((T*)a.y + off + at1) = hi;
-        continue;
-      }
-      to_pairs<kForm, E>(lo.v, hi.v);
+      const Vec lo = *(const Vec*)((const T*)a.x + off);
+      const Vec hi = *(const Vec*)((const T*)a.x + off + kD / 2);
       Vec p, q;
       bool nan = false;
 #pragma unroll
@@ -80,9 +72,8 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeLaunch a, int heads, int 
           one_nan_of(p.v[e]);
           one_nan_of(q.v[e]);
         }
-      from_pairs<kForm, E>(p.v, q.v);
-      *(Vec*)((T*)a.y + off + at0) = p;
-      *(Vec*)((T*)a.y + off + at1) = q;
+      *(Vec*)((T*)a.y + off) = p;
+      *(Vec*)((T*)a.y + off + kD / 2) = q;
     }
   }
 }
@@ -95,38 +86,35 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeLaunch a, int heads, int 
 // 64-bit divisions for that and the loads after the chain, float32 rows took 3.3 us
 // for 8 heads x 1 position and 5.9 for 32 x 100, now 2.7 and 4.3; 8 x 1999, binary16,
 // 8.2 and 6.1 (13.4 with pow and sincos for every row).
-template <typename T, int kForm>
-__global__ __launch_bounds__(64) void rope_few_kernel(RopeLaunch a, int heads, FormArg<kForm> f) {
+template <typename T>
+__global__ __launch_bounds__(64) void rope_few_kernel(RopeLaunch a, int heads) {
   const int l = threadIdx.x, i = blockIdx.x, b = blockIdx.z;
   const int h0 = blockIdx.y * heads, h1 = min(a.H, h0 + heads);
-  const bool turn = turned<kForm>(f, l);
-  const int at0 = place<kForm, 1>(f, l, false), gap = place<kForm, 1>(f, l, true) - at0;
-  int64_t off = (((int64_t)b * a.H + h0) * a.n + i) * kD + at0;
-  T lo = ((const T*)a.x)[off], hi = ((const T*)a.x)[off + gap];
+  int64_t off = (((int64_t)b * a.H + h0) * a.n + i) * kD + l;
+  T lo = ((const T*)a.x)[off], hi = ((const T*)a.x)[off + kD / 2];
   double s, c;
-  pair_turn<kForm>(f, ((double)a.pos0[b] + (double)i) * pair_freq<kForm>(f, a.base, l), s, c);
+  sincos(((double)a.pos0[b] + (double)i) * pow(a.base, -(2.0 * l) / kD), &s, &c);
 #pragma unroll 1
   for (int h = h0; h < h1; ++h) {
     const int64_t next = off + (h + 1 < h1 ? (int64_t)a.n * kD : 0);
-    const T was0 = lo, was1 = hi;
     const double x0 = (double)(float)lo, x1 = (double)(float)hi;
     if (h + 1 < h1) {
       lo = ((const T*)a.x)[next];
-      hi = ((const T*)a.x)[next + gap];
+      hi = ((const T*)a.x)[next + kD / 2];
     }
     T p = rounded<T>(x0 * c - x1 * s), q = rounded<T>(x1 * c + x0 * s);
     if (x0 != x0 || x1 != x1) {
       one_nan_of(p);
       one_nan_of(q);
     }
-    ((T*)a.y)[off] = kForm == 0 || turn ? p : was0;
-    ((T*)a.y)[off + gap] = kForm == 0 || turn ? q : was1;
+    ((T*)a.y)[off] = p;
+    ((T*)a.y)[off + kD / 2] = q;
     off = next;
   }
 }
 
-template <typename T, int kForm>
-static hipError_t launch_rope_t(const RopeLaunch& a, const FormArg<kForm>& f) {
+template <typename T>
+static hipError_t launch_rope_t(const RopeLaunch& a) {
   // Up to 4096 waves (4 per SIMD), so that pow and sincos are shared by as many
   // rows as the GPU's size allows.  Few rows (a decode step, or a few thousand
   // positions of few heads): the shorter chain, one wave per workgroup; more
@@ -135,8 +123,8 @@ static hipError_t launch_rope_t(const RopeLaunch& a, const FormArg<kForm>& f) {
   if (rows * a.H <= 4 * 4096) {
     const int heads = (int)((rows * a.H + 4095) / 4096);  // 1 to 4
     const int chunks = (a.H + heads - 1) / heads;
-    hipLaunchKernelGGL((rope_few_kernel<T, kForm>), dim3(a.n, chunks, a.B), dim3(64), 0, a.stream,
-                       a, heads, f);
+    hipLaunchKernelGGL(rope_few_kernel<T>, dim3(a.n, chunks, a.B), dim3(64), 0, a.stream, a,
+                       heads);
     return hipGetLastError();
   }
   const int64_t most = (a.H + 1) / 2;
@@ -146,18 +134,12 @@ static hipError_t launch_rope_t(const RopeLaunch& a, const FormArg<kForm>& f) {
   const int chunks = (a.H + heads - 1) / heads;
   const int64_t items = rows * chunks;
   const dim3 grid((unsigned)((items < 4096 ? items + 3 : 4096) / 4));
-  hipLaunchKernelGGL((rope_kernel<T, kForm>), grid, dim3(256), 0, a.stream, a, heads, chunks, f);
+  hipLaunchKernelGGL(rope_kernel<T>, grid, dim3(256), 0, a.stream, a, heads, chunks);
   return hipGetLastError();
 }
 
-template <typename T>
-static hipError_t launch_rope_form(const RopeLaunch& a, const RotaryForm* f) {
-  if (!f) return launch_rope_t<T, 0>(a, WholeHead());
-  return f->interleaved ? launch_rope_t<T, 2>(a, *f) : launch_rope_t<T, 1>(a, *f);
-}
-
-hipError_t launch_rope(const RopeLaunch& a, const RotaryForm* form) {
-  return a.dtype == SWAN_F32 ? launch_rope_form<float>(a, form) : launch_rope_form<_Float16>(a, form);
+hipError_t launch_rope(const RopeLaunch& a) {
+  return a.dtype == SWAN_F32 ? launch_rope_t<float>(a) : launch_rope_t<_Float16>(a);
 }
 
 }  // namespace swan

@@ -9,7 +9,7 @@
 
 #include <type_traits>
 
-#include "swan_cache_ops.h"
+#include "swan_layer_ops.h"
 
 namespace swan {
 

@@ -1135,6 +1135,7 @@ swan_status qkv_rows_prep(const void* qkv, int64_t seq_stride, int64_t row_strid
   a.x = qkv;
   a.seq = seq_stride;
   a.row = row_stride;
+  a.head = SWAN_HEAD_DIM;
   a.out[0] = q;
   a.out[1] = k;
   a.out[2] = v;

@@ -76,13 +76,7 @@ struct RopeLaunch {
   double base;
   hipStream_t stream;
 };
-// other forms (rotary.h): the frequencies of half pairs, then zeros
-struct RotaryForm {
-  double magnitude;
-  int half, interleaved;
-  double freq[kD / 2];
-};
-hipError_t launch_rope(const RopeLaunch& a, const RotaryForm* form = nullptr);
+hipError_t launch_rope(const RopeLaunch& a);
 
 constexpr int kMaxCalib = 64;  // problems per launch
 struct CalibLaunch {

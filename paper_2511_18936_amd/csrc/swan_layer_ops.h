@@ -2,17 +2,25 @@
 // attention of several rows per sequence (over cached tokens, over a prompt).
 #pragma once
 
-#include "swan_cache_ops.h"
 #include "swan_device.h"
 #include "swan_internal.h"
 #include "swan_layer.h"
 
 namespace swan {
 
-// [q | k | v] projections to heads (qkv_rows.hip)
+// other forms of RoPE (rotary.h): the frequencies of half pairs, then zeros
+struct RotaryForm {
+  double magnitude;
+  int half, interleaved;
+  double freq[kD / 2];
+};
+
+// [q | k | v] projections to heads (qkv_rows.hip); with a form also heads alone, whose rows
+// are anywhere (head), and which may be written in place
 struct QkvRowsLaunch {
   const void* x;        // rows of Hq q, Hkv k and Hkv v heads, 128 elements each
   int64_t seq, row;     // elements from a sequence (a row) to the next
+  int64_t head;         // with a form: from a head of a row to the next (else 128)
   void* out[3];         // q, k, v: [B][heads][n][128]
   const void* w[2];     // norm weights of q and k (NULL: no norm)
   int wstep;            // elements from a head's weights to the next's (0: shared)

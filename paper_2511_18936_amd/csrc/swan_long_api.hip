@@ -31,9 +31,54 @@ swan_status rotary_form(const swan_rotary* r, int32_t head_dim, swan::RotaryForm
   return SWAN_OK;
 }
 
-// Pages of a split: every one costs its chain of loads, so a launch of few pages takes one
-// each, one of many about two waves per wave slot of the GPU, as decode plans without a window
-constexpr int kWindowWaves = 256 * 4 * 2;
+// Pages per workgroup, so that the launch and the join of its partials are shortest: pages[j]
+// of sequence j, weighed by their entries, for each of its `units`.  LDS holds four workgroups
+// a CU, 1024 in all.  A plan's time is taken as that of its longest split, or of all pages
+// spread evenly, in one such round, or as rounds, or as spread evenly with half a workgroup's time
+// more; 2 us to start, and for a page (of `entries` in both roles) 1024 of them at 10 TB/s (8-bit
+// values no less: their LDS work is that of 16-bit ones).  Of eleven plans measured for each of
+// nine shapes (1 to 32 sequences, 8 to 64 heads) it takes the best or one within 3 %: 16 x 32
+// heads over 300 to 4096 tokens 84 us with 8 pages, 102 with 2, 100 with 22; 2 x 32 heads over
+// 1000 18 with 2, 24 with 1 (whose 1088 workgroups take two rounds) and with 8.
+int plan_window(int32_t dtype, int entries, int groups, const int* pages, int units, int heads) {
+  constexpr double kSlots = 1024, kStart = 2.0;
+  const double page = 64.0 * entries * (dtype == SWAN_F32 ? 5 : 3) * kSlots / 10e6;
+  int64_t total = 0;
+  int longest = 1;
+  for (int j = 0; j < groups; ++j) {
+    total += (int64_t)pages[j] * units;
+    longest = pages[j] > longest ? pages[j] : longest;
+  }
+  const double even = (double)total * page / kSlots;
+  int best = longest;
+  double least = 1e30;
+  // every plan of few pages, then steps of an eighth
+  for (int per = (longest + swan::kMaxSplits - 1) / swan::kMaxSplits; per <= longest;
+       per += per < 16 ? 1 : per / 8) {
+    int64_t splits = 0;
+    int most = 1;  // pages of a split
+    for (int j = 0; j < groups; ++j) {
+      const int ns = (pages[j] + per - 1) / per, each = (pages[j] + ns - 1) / ns;
+      splits += ns;
+      most = each > most ? each : most;
+    }
+    const double u = (double)splits * units, one = kStart + most * page;
+    double t;
+    if (u <= kSlots) {
+      const double run = most * page * (u <= 256 ? 0.7 : 1.0);
+      t = kStart + (run > even ? run : even);
+    } else {
+      const double rounds = ceil(u / kSlots) * one, spread = u * kStart / kSlots + even + 0.5 * one;
+      t = rounds < spread ? rounds : spread;
+    }
+    t += (double)splits * heads * (2.0 * 528 / 4e6);
+    if (t < least) {
+      least = t;
+      best = per;
+    }
+  }
+  return best;
+}
 
 struct WindowPlan {
   swan::WindowLaunch a;
@@ -100,26 +145,29 @@ swan_status window_prep(const swan_prefix* prefix, const swan_cache* c,
     }
   }
   const int hpw = swan::decode_heads_per_wave(c->dtype, c->n_q_heads, c->n_kv_heads);
+  // splits, a page being one of the most entries among the batch
   auto listed = [&](int b) {
     return swan::WindowPages(a.len[b], c->buffer_tokens, a.lo[b], a.sink[b]).count;
   };
-  auto weight = [&](int b) {
+  auto entries = [&](int b) {
     return swan::kpad_of(a.kact[0][b]) + swan::kpad_of(a.kact[1][b]);
   };
-  int64_t total = 0;
-  for (int b = 0; b < c->batch; ++b)
-    total += (int64_t)listed(b) * weight(b) * (c->n_q_heads / hpw);
-  int64_t per_wave = (total + kWindowWaves - 1) / kWindowWaves;
-  if (per_wave < 1) per_wave = 1;
+  int most = 0, groups = 0, pages[SWAN_MAX_BATCH], seq[SWAN_MAX_BATCH];
+  for (int b = 0; b < c->batch; ++b) most = entries(b) > most ? entries(b) : most;
+  for (int b = 0; b < c->batch; ++b) {
+    const int64_t n = listed(b);
+    if (n == 0) continue;
+    pages[groups] = (int)((n * entries(b) + most - 1) / most);
+    seq[groups++] = b;
+  }
+  for (int b = 0; b < SWAN_MAX_BATCH; ++b) a.nsplit[b] = 0;
+  const int per = groups == 0 ? 1 : plan_window(c->dtype, most, groups, pages, c->n_q_heads / hpw,
+                                                c->n_q_heads);
+  for (int j = 0; j < groups; ++j) a.nsplit[seq[j]] = (pages[j] + per - 1) / per;
   int slots = 0;
   for (int b = 0; b < SWAN_MAX_BATCH; ++b) {
-    a.nsplit[b] = 0;
     pl.used[b] = 0;
     if (b >= c->batch || a.len[b] == 0) continue;
-    const int64_t pages = listed(b);
-    int64_t ns = (pages * weight(b) + per_wave - 1) / per_wave;
-    ns = ns > pages ? pages : ns;
-    a.nsplit[b] = (int32_t)(ns > swan::kMaxSplits ? swan::kMaxSplits : ns);
     const int ring = a.len[b] < c->buffer_tokens ? a.len[b] : c->buffer_tokens;
     pl.used[b] = (int16_t)(a.nsplit[b] + swan::pages_for(ring));
     slots = pl.used[b] > slots ? pl.used[b] : slots;
@@ -227,7 +275,27 @@ swan_status swan_rope_rotary(const void* x, void* y, int32_t dtype, int32_t batc
   swan::RotaryForm f;
   if ((st = rotary_form(rotary, head_dim, f)) != SWAN_OK) return st;
   if (n == 0) return ok();
-  return hip_status(swan::launch_rope(a, &f), "rope launch");
+  if ((int64_t)batch * n > INT32_MAX)
+    return fail(SWAN_ERR_UNSUPPORTED, "batch %d x n %d: above 2^31 - 1 rows", batch, n);
+  // heads alone, without norms
+  swan::QkvRowsLaunch r;
+  r.x = x;
+  r.head = (int64_t)n * head_dim;
+  r.seq = r.head * n_heads;
+  r.row = head_dim;
+  r.out[0] = y;
+  r.out[1] = r.out[2] = nullptr;
+  r.w[0] = r.w[1] = nullptr;
+  r.wstep = r.w32 = 0;
+  r.B = batch;
+  r.Hq = n_heads;
+  r.Hkv = 0;
+  r.n = n;
+  r.dtype = dtype;
+  r.eps = r.base = 0.0;
+  for (int b = 0; b < SWAN_MAX_BATCH; ++b) r.pos0[b] = a.pos0[b];
+  r.stream = (hipStream_t)stream;
+  return hip_status(swan::launch_qkv_rows(r, &f), "rope launch");
 }
 
 swan_status swan_qkv_rows_rotary(const void* qkv, int64_t seq_stride, int64_t row_stride,

@@ -21,73 +21,89 @@ __device__ __forceinline__ int ring_token(int L, int bb, int s) {
   return L - at + s - (s >= at ? bb : 0);
 }
 
-// One wave: ring slots 64 piece .. + 63 of (sequence b, kv head h) for GH query heads from
-// hq0 on.  Lane t scores slot t, then lane l sums dims 2 l and 2 l + 1.  q: [kD][GH] floats of
-// scratch, p: [GH][64].
-template <typename E, int GH>
-__device__ void ring_wave(const WindowLaunch& a, int b, int h, int hq0, int piece, float* q,
+// One wave: ring slots 64 piece .. + 63 of (sequence b, kv head h) for query head hq.  Lane t
+// scores slot t; then a row of the values goes to 16 lanes (float32: 32), 16 bytes each, 4 (2)
+// rows at a time, and the lanes' sums of the same dims meet at the end.  What bounds it is the
+// latency of its loads, so 16 of them are in flight at a time, the first values' before the
+// scores.  One query head a wave, the rows of a group's others coming from L2: two need more
+// registers than the page waves, whose kernel it is.  q: kD floats of scratch, p: 64.
+template <typename E>
+__device__ void ring_wave(const WindowLaunch& a, int b, int h, int hq, int piece, float* q,
                           float* p, int lane) {
+  constexpr int N = 16 / (int)sizeof(E);  // elements of 16 bytes
+  constexpr int kLanes = kD / N, kAtOnce = 64 / kLanes, kLoads = 16;
+  struct alignas(16) Vec {
+    E v[N];
+  };
   const int L = a.len[b], nb = min(L, a.bb);
   const int64_t ring = (((int64_t)b * a.Hkv + h) * a.bb + 64 * piece) * kD;
-  const int count = min(64, nb - 64 * piece);
-  const float* qh = a.qhat + ((int64_t)b * a.Hq + hq0) * kD;
+  const int count = min(64, nb - 64 * piece), mine = min(lane, count - 1);
+  Vec k[kLoads], v[kLoads];
+  const E* row = (const E*)a.k_ring + ring + (int64_t)mine * kD;
+  const E* col = (const E*)a.v_ring + ring + N * (lane % kLanes);
+  const int first = lane / kLanes;  // row first + kAtOnce i is this lane's i-th
+  auto load_k = [&](int x0) {
 #pragma unroll
-  for (int x = 0; x < 2 * GH; ++x) q[(lane + 64 * (x & 1)) * GH + (x >> 1)] = qh[64 * x + lane];
+    for (int x = 0; x < kLoads; ++x) k[x] = *(const Vec*)(row + N * (x0 + x));
+  };
+  auto load_v = [&](int x0) {
+#pragma unroll
+    for (int x = 0; x < kLoads; ++x)
+      v[x] = *(const Vec*)(col + (int64_t)min(first + kAtOnce * (x0 + x), count - 1) * kD);
+  };
+  load_k(0);
+  load_v(0);
+  const float* qh = a.qhat + ((int64_t)b * a.Hq + hq) * kD;
+  q[lane] = qh[lane];
+  q[lane + 64] = qh[lane + 64];
   wave_lds_fence();
-  const int token = ring_token(L, a.bb, 64 * piece + min(lane, count - 1));
+  const int token = ring_token(L, a.bb, 64 * piece + mine);
   const bool seen = lane < count && (token >= a.lo[b] || token < a.sink[b]);
-  constexpr int N = 16 / (int)sizeof(E);
-  float s[GH];
+  float s0 = 0.f, s1 = 0.f;
 #pragma unroll
-  for (int g = 0; g < GH; ++g) s[g] = 0.f;
-  const E* row = (const E*)a.k_ring + ring + (int64_t)min(lane, count - 1) * kD;
-#pragma unroll 4
-  for (int c = 0; c < kD / N; ++c) {
-    struct alignas(16) {
-      E v[N];
-    } k = *(const decltype(k)*)(row + N * c);
+  for (int x0 = 0; x0 < kLanes; x0 += kLoads) {
+    if (x0 > 0) load_k(x0);
 #pragma unroll
-    for (int e = 0; e < N; ++e)
+    for (int x = 0; x < kLoads; ++x)
 #pragma unroll
-      for (int g = 0; g < GH; ++g) s[g] = fmaf(q[(N * c + e) * GH + g], (float)k.v[e], s[g]);
+      for (int e = 0; e < N; e += 2) {
+        s0 = fmaf(q[N * (x0 + x) + e], (float)k[x].v[e], s0);
+        s1 = fmaf(q[N * (x0 + x) + e + 1], (float)k[x].v[e + 1], s1);
+      }
   }
-  float* part = a.part + (((int64_t)b * a.Hq + hq0) * a.slots + a.nsplit[b] + piece) * kPartFloats;
-  const int64_t step = (int64_t)a.slots * kPartFloats;  // from a query head's part to the next's
-#pragma unroll
-  for (int g = 0; g < GH; ++g) {
-    const float m = wave_max(seen ? s[g] : -INFINITY);
-    const float w = seen ? exp2f(s[g] - m) : 0.f;
-    const float l = wave_sum(w);
-    p[g * 64 + lane] = w;
-    if (lane == 0) {
-      part[g * step] = m;
-      part[g * step + 1] = l;
-    }
+  float* part = a.part + (((int64_t)b * a.Hq + hq) * a.slots + a.nsplit[b] + piece) * kPartFloats;
+  const float s = seen ? s0 + s1 : -INFINITY, m = wave_max(s);
+  const float w = seen ? exp2f(s - m) : 0.f, l = wave_sum(w);
+  p[lane] = w;
+  if (lane == 0) {
+    part[0] = m;
+    part[1] = l;
   }
   wave_lds_fence();
-  const uint64_t mask = __ballot(seen);
-  float o[GH][2];
+  const uint64_t mask = __ballot(seen) >> first;
+  float o[N];
 #pragma unroll
-  for (int g = 0; g < GH; ++g) o[g][0] = o[g][1] = 0.f;
-  const E* col = (const E*)a.v_ring + ring + 2 * lane;
-#pragma unroll 8
-  for (int t = 0; t < count; ++t) {
-    struct alignas(2 * sizeof(E)) {
-      E v[2];
-    } v = *(const decltype(v)*)(col + t * kD);
-    const bool on = (mask >> t) & 1;  // (a hidden token's value may be no number)
-    const float v0 = on ? (float)v.v[0] : 0.f, v1 = on ? (float)v.v[1] : 0.f;
+  for (int e = 0; e < N; ++e) o[e] = 0.f;
 #pragma unroll
-    for (int g = 0; g < GH; ++g) {
-      const float w = p[g * 64 + t];
-      o[g][0] = fmaf(w, v0, o[g][0]);
-      o[g][1] = fmaf(w, v1, o[g][1]);
+  for (int x0 = 0; x0 < 64 / kAtOnce; x0 += kLoads) {
+    if (x0 > 0) load_v(x0);
+#pragma unroll
+    for (int x = 0; x < kLoads; ++x) {
+      const int t = kAtOnce * (x0 + x);
+      const bool on = (mask >> t) & 1;  // (a hidden token's value may be no number)
+      const float pt = p[t + first];
+#pragma unroll
+      for (int e = 0; e < N; ++e) o[e] = fmaf(pt, on ? (float)v[x].v[e] : 0.f, o[e]);
     }
   }
 #pragma unroll
-  for (int g = 0; g < GH; ++g) {
-    part[g * step + 4 + 2 * lane] = o[g][0];
-    part[g * step + 4 + 2 * lane + 1] = o[g][1];
+  for (int d = kLanes; d < 64; d *= 2)
+#pragma unroll
+    for (int e = 0; e < N; ++e) o[e] += __shfl_xor(o[e], d, 64);
+  if (lane < kLanes) {
+#pragma unroll
+    for (int e = 0; e < N; e += 4)
+      *(float4*)(part + 4 + N * lane + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
   }
 }
 

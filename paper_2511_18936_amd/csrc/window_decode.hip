@@ -31,22 +31,23 @@ __global__ __launch_bounds__(512) void window_rotate_kernel(WindowLaunch a) {
         ((part[0][j] + part[1][j]) + (part[2][j] + part[3][j])) * a.qmult;
 }
 
-// Grid: n * Hq * ring pieces, then n * Hq * g.n_splits waves over pages.
+// Grid: n * Hq * g.n_splits waves over pages, then n * Hq * ring pieces.
 template <typename T, int KP8>
 __global__ __launch_bounds__(64) void window_kernel(WindowLaunch a, SeqGroup g) {
   constexpr int kRows = kD + 1;  // and the spare row
   __shared__ __attribute__((aligned(16))) float qrep[kRows * kQRep];
   __shared__ __attribute__((aligned(16))) float acc[kRows * kAccCols];
   using E = typename Fmt<T>::Elem;
-  const int lane = threadIdx.x, U = g.n * a.Hq, pieces = pages_for(a.bb);
+  const int lane = threadIdx.x, U = g.n * a.Hq;
   int w = blockIdx.x;
   const int b = g.seq[w % U / a.Hq], hq = w % U % a.Hq, h = hq / (a.Hq / a.Hkv);
   w /= U;
-  if (w < pieces) {
-    if (64 * w < min(a.len[b], a.bb)) ring_wave<E, 1>(a, b, h, hq, w, qrep, acc, lane);
+  if (w >= g.n_splits) {
+    w -= g.n_splits;
+    if (64 * w < min(a.len[b], a.bb)) ring_wave<E>(a, b, h, hq, w, qrep, acc, lane);
     return;
   }
-  const int split = w - pieces, ns = a.nsplit[b];
+  const int split = w, ns = a.nsplit[b];
   if (split >= ns) return;
   const WindowPages list(a.len[b], a.bb, a.lo[b], a.sink[b]);
   const int x0 = split_begin(split, ns, list.count, true);

@@ -5,10 +5,11 @@
 
 namespace swan {
 
-// Grid: units * ceil(ring pieces / 2) ring blocks (a piece a wave), then units * g.n_splits
-// blocks over pages; a unit is GH query heads of one kv head of a sequence.
+// Grid: units * g.n_splits blocks over pages, then units * ring pieces * GH / 2, of a ring wave
+// per query head; a unit is GH query heads of one kv head of a sequence.  Two waves a SIMD, as
+// LDS allows four blocks a CU (the largest pages: one).
 template <typename T, int KP8, int GH>
-__global__ __launch_bounds__(128) void window_gqa_kernel(WindowLaunch a, SeqGroup g) {
+__global__ __launch_bounds__(128, KP8 <= 10 ? 2 : 1) void window_gqa_kernel(WindowLaunch a, SeqGroup g) {
   constexpr int R = qrep_replicas<GH>();
   __shared__ __attribute__((aligned(16))) GqaLds<GH, kD + 1> sh;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // 0: scores, 1: values
@@ -17,18 +18,14 @@ __global__ __launch_bounds__(128) void window_gqa_kernel(WindowLaunch a, SeqGrou
   const int ui = blockIdx.x % units, x = blockIdx.x / units;
   const int b = g.seq[ui / (a.Hkv * HC)], h = ui / HC % a.Hkv;
   const int hq0 = (h * HC + ui % HC) * GH;
-  const int rings = (pages_for(a.bb) + 1) / 2;
-  if (x < rings) {
-    static_assert(sizeof(sh.vt) >= 2 * 64 * GH * sizeof(float) &&
-                      sizeof(sh.qrep) >= 2 * kD * GH * sizeof(float),
-                  "scratch of two ring waves");
-    const int piece = 2 * x + wave;
+  if (x >= g.n_splits) {
+    const int piece = (x - g.n_splits) / (GH / 2), j = (x - g.n_splits) % (GH / 2) * 2 + wave;
     if (64 * piece < min(a.len[b], a.bb))
-      ring_wave<_Float16, GH>(a, b, h, hq0, piece, sh.qrep + wave * kD * GH,
-                              (float*)sh.vt + wave * 64 * GH, lane);
+      ring_wave<_Float16>(a, b, h, hq0 + j, piece, sh.qrep + wave * kD, (float*)sh.vt + wave * 64,
+                          lane);
     return;
   }
-  const int split = x - rings, ns = a.nsplit[b];
+  const int split = x, ns = a.nsplit[b];
   if (split >= ns) return;  // uniform over the block
   const WindowPages list(a.len[b], a.bb, a.lo[b], a.sink[b]);
   const int x0 = split_begin(split, ns, list.count, true);
@@ -116,7 +113,7 @@ __global__ __launch_bounds__(128) void window_gqa_kernel(WindowLaunch a, SeqGrou
 template <typename T, int KP8, int GH>
 static hipError_t launch_gqa_k(const WindowLaunch& a, const SeqGroup& g) {
   const int units = g.n * a.Hkv * (a.Hq / a.Hkv / GH);
-  const dim3 grid(units * ((pages_for(a.bb) + 1) / 2 + g.n_splits));
+  const dim3 grid(units * (g.n_splits + pages_for(a.bb) * (GH / 2)));
   hipLaunchKernelGGL((window_gqa_kernel<T, KP8, GH>), grid, dim3(128), 0, a.stream, a, g);
   return hipGetLastError();
 }
