@@ -35,13 +35,16 @@ swan_status rotary_form(const swan_rotary* r, int32_t head_dim, swan::RotaryForm
 // of sequence j, weighed by their entries, for each of its `units`.  LDS holds four workgroups
 // a CU, 1024 in all.  A plan's time is taken as that of its longest split, or of all pages
 // spread evenly, in one such round, or as rounds, or as spread evenly with half a workgroup's time
-// more; 2 us to start, and for a page (of `entries` in both roles) 1024 of them at 10 TB/s (8-bit
+// more; then `rings` workgroups of the ring, of 5, which find room beside a first round that
+// leaves some (32 sequences x 8 kv heads: 75 us with 848 workgroups, 92 with 1000 and with 1048).
+// 2 us to start, and for a page (of `entries` in both roles) 1024 of them at 10 TB/s (8-bit
 // values no less: their LDS work is that of 16-bit ones).  Of eleven plans measured for each of
 // nine shapes (1 to 32 sequences, 8 to 64 heads) it takes the best or one within 3 %: 16 x 32
 // heads over 300 to 4096 tokens 84 us with 8 pages, 102 with 2, 100 with 22; 2 x 32 heads over
 // 1000 18 with 2, 24 with 1 (whose 1088 workgroups take two rounds) and with 8.
-int plan_window(int32_t dtype, int entries, int groups, const int* pages, int units, int heads) {
-  constexpr double kSlots = 1024, kStart = 2.0;
+int plan_window(int32_t dtype, int entries, int groups, const int* pages, int units, int heads,
+                double rings) {
+  constexpr double kSlots = 1024, kStart = 2.0, kRing = 5.0;
   const double page = 64.0 * entries * (dtype == SWAN_F32 ? 5 : 3) * kSlots / 10e6;
   int64_t total = 0;
   int longest = 1;
@@ -67,9 +70,10 @@ int plan_window(int32_t dtype, int entries, int groups, const int* pages, int un
     if (u <= kSlots) {
       const double run = most * page * (u <= 256 ? 0.7 : 1.0);
       t = kStart + (run > even ? run : even);
+      if (rings > (kSlots - u) * t / kRing) t += kRing;
     } else {
       const double rounds = ceil(u / kSlots) * one, spread = u * kStart / kSlots + even + 0.5 * one;
-      t = rounds < spread ? rounds : spread;
+      t = (rounds < spread ? rounds : spread) + rings * kRing / kSlots;
     }
     t += (double)splits * heads * (2.0 * 528 / 4e6);
     if (t < least) {
@@ -161,8 +165,12 @@ swan_status window_prep(const swan_prefix* prefix, const swan_cache* c,
     seq[groups++] = b;
   }
   for (int b = 0; b < SWAN_MAX_BATCH; ++b) a.nsplit[b] = 0;
+  double rings = 0;
+  for (int b = 0; b < c->batch; ++b)
+    rings += swan::pages_for(a.len[b] < c->buffer_tokens ? a.len[b] : c->buffer_tokens);
+  rings *= hpw > 1 ? 0.5 * c->n_q_heads : c->n_q_heads;
   const int per = groups == 0 ? 1 : plan_window(c->dtype, most, groups, pages, c->n_q_heads / hpw,
-                                                c->n_q_heads);
+                                                c->n_q_heads, rings);
   for (int j = 0; j < groups; ++j) a.nsplit[seq[j]] = (pages[j] + per - 1) / per;
   int slots = 0;
   for (int b = 0; b < SWAN_MAX_BATCH; ++b) {
