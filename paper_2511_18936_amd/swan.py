@@ -858,17 +858,25 @@ def prefix_workspace_bytes(prefix: Prefix, desc: CacheDesc, seq_len: Sequence[in
     return out.value
 
 
+def _window_head(desc: CacheDesc, seq_len, k_active, k_value, prefix, window, sinks):
+    """The arguments that a windowed decode call and its workspace query share."""
+    _window(window, sinks)
+    if window is None or not isinstance(sinks, int):
+        raise SwanError(SWAN_ERR_INVALID_ARG, f"window {window}, sinks {sinks}")
+    B = desc.batch
+    return (None if prefix is None else ctypes.byref(prefix._desc(B)), ctypes.byref(desc),
+            _per_sequence(seq_len, B, "seq_len"), _per_sequence(k_active, B, "k_active"),
+            _per_sequence(k_value, B, "k_value"), window, sinks)
+
+
 def decode_window_workspace_bytes(desc: CacheDesc, seq_len: Sequence[int],
                                   k_active: Sequence[int], window: int, sinks: int = 0,
                                   k_value: Optional[Sequence[int]] = None,
                                   prefix: Optional[Prefix] = None) -> int:
-    _window(window, sinks)
     out = ctypes.c_size_t()
-    p = None if prefix is None else ctypes.byref(prefix._desc(desc.batch))
     _check(_lib.swan_decode_window_workspace_bytes(
-        p, ctypes.byref(desc), _per_sequence(seq_len, desc.batch, "seq_len"),
-        _per_sequence(k_active, desc.batch, "k_active"),
-        _per_sequence(k_value, desc.batch, "k_value"), window, sinks, ctypes.byref(out)))
+        *_window_head(desc, seq_len, k_active, k_value, prefix, window, sinks),
+        ctypes.byref(out)))
     return out.value
 
 
@@ -877,10 +885,9 @@ def decode_window(desc: CacheDesc, seq_len: Sequence[int], k_active: Sequence[in
                   k_value: Optional[Sequence[int]] = None, prefix: Optional[Prefix] = None,
                   new=None) -> None:
     """swan_decode_attention_window, or with new = (k_new, v_new) swan_decode_step_window
-    (seq_len: lengths before it), behind a prefix where one is given."""
-    _window(window, sinks)
-    if window is None:
-        raise SwanError(SWAN_ERR_INVALID_ARG, "window is None")
+    (seq_len: lengths before it), behind a prefix where one is given.  workspace None: the
+    caching allocator's memory for this call."""
+    head = _window_head(desc, seq_len, k_active, k_value, prefix, window, sinks)
     _decode_tensors(desc, q, P_qk, P_vo, out)
     k_new, v_new = new or (None, None)
     if new is not None:
@@ -888,17 +895,18 @@ def decode_window(desc: CacheDesc, seq_len: Sequence[int], k_active: Sequence[in
         shape = (desc.batch, desc.n_kv_heads, 1, desc.head_dim)
         _tensor(k_new, "k_new", et, shape)
         _tensor(v_new, "v_new", et, shape)
-    if workspace is None or not workspace.is_cuda or not workspace.is_contiguous():
-        raise SwanError(SWAN_ERR_WORKSPACE, "workspace must be a contiguous GPU tensor")
     device = _same_gpu(q=q, out=out, P_qk=P_qk, P_vo=P_vo, k_new=k_new, v_new=v_new,
-                       workspace=workspace,
                        prefix=None if prefix is None else prefix.cache.k_pages)
-    p = None if prefix is None else ctypes.byref(prefix._desc(desc.batch))
-    B = desc.batch
-    head = (p, ctypes.byref(desc), _per_sequence(seq_len, B, "seq_len"),
-            _per_sequence(k_active, B, "k_active"), _per_sequence(k_value, B, "k_value"), window,
-            sinks)
-    tail = (_ptr(q), _ptr(P_qk), _ptr(P_vo), float(scale), _ptr(out), _ptr(workspace),
+    if workspace is None:
+        need = ctypes.c_size_t()
+        ask = head
+        if new is not None:  # for the lengths after the step
+            ask = head[:2] + (_i32_array([L + 1 for L in seq_len]),) + head[3:]
+        _check(_lib.swan_decode_window_workspace_bytes(*ask, ctypes.byref(need)))
+        workspace = _made("empty", (need.value,), "uint8", device, stream)
+    else:
+        workspace = _workspace(workspace, 0, device, stream)
+    tail = (_ptr(q), _ptr(P_qk), _ptr(P_vo), scale, _ptr(out), workspace.data_ptr(),
             workspace.numel() * workspace.element_size())
     with _CallsOn(device, stream) as s:
         if new is None:
@@ -1101,13 +1109,11 @@ class SwanCache:
                prefix: Optional[Prefix] = None, window: Optional[int] = None, sinks: int = 0):
         """Attention of q ([B][H_q][d]) over the cache, behind a prefix where one is given.
         window: over the last `window` tokens and the first `sinks` alone."""
-        _window(window, sinks)
         if out is None:
             out = _result_like(q, q.shape, stream)
-        if window is not None:
-            decode_window(self.desc, self.seq_len, self.k_active, q, P_qk, P_vo, out,
-                          self.workspace(None, prefix, stream, window, sinks), window, sinks,
-                          scale, stream, self.k_value, prefix)
+        if window is not None or sinks:
+            decode_window(self.desc, self.seq_len, self.k_active, q, P_qk, P_vo, out, None, window,
+                          sinks, scale, stream, self.k_value, prefix)
         elif prefix is None:
             decode_attention(self.desc, self.seq_len, self.k_active, q, P_qk, P_vo, out,
                              self.workspace(None, None, stream), scale, stream, self.k_value)
@@ -1122,15 +1128,16 @@ class SwanCache:
         """One decode step (swan_decode_step): append k_new / v_new ([B][H_kv][1][d]),
         advance the lengths, and return the attention of q ([B][H_q][d]) over the cache,
         behind a prefix where one is given; window, sinks as in decode()."""
-        _window(window, sinks)
         if out is None:
             out = _result_like(q, q.shape, stream)
         after = [L + 1 for L in self.seq_len]
-        ws = self.workspace(after, prefix, stream, window, sinks)
-        if window is not None:
-            decode_window(self.desc, self.seq_len, self.k_active, q, P_qk, P_vo, out, ws, window,
+        if window is not None or sinks:
+            decode_window(self.desc, self.seq_len, self.k_active, q, P_qk, P_vo, out, None, window,
                           sinks, scale, stream, self.k_value, prefix, (k_new, v_new))
-        elif prefix is None:
+            self.seq_len = after
+            return out
+        ws = self.workspace(after, prefix, stream)
+        if prefix is None:
             decode_step(self.desc, self.seq_len, self.k_active, k_new, v_new, q, P_qk, P_vo, out,
                         ws, scale, stream, self.k_value)
         else:
