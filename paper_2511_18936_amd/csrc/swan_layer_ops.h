@@ -162,12 +162,14 @@ struct WindowLaunch {
   float qmult;
   int B, Hq, Hkv, bb, npc, slots, dtype;
   int qhat_ready;      // qhat is there already (decode steps)
+  int rotate_here;     // the attention's blocks rotate q themselves (grouped heads)
   int32_t len[SWAN_MAX_BATCH], lo[SWAN_MAX_BATCH], sink[SWAN_MAX_BATCH];
   int32_t nsplit[SWAN_MAX_BATCH];  // 0: no such page
   int32_t kact[2][SWAN_MAX_BATCH];
   int64_t off[2][SWAN_MAX_BATCH];
   hipStream_t stream;
 };
+constexpr int kRotateHeads = 4;  // the most heads a block for which rotate_here may be set
 hipError_t launch_window(const WindowLaunch& a);
 // the sequences of one launch, whose k_pad is 8 kp8 at most
 hipError_t launch_window_gqa(const WindowLaunch& a, const SeqGroup& g, int kp8);

@@ -180,6 +180,14 @@ swan_status window_prep(const swan_prefix* prefix, const swan_cache* c,
     pl.used[b] = (int16_t)(a.nsplit[b] + swan::pages_for(ring));
     slots = pl.used[b] > slots ? pl.used[b] : slots;
   }
+  double blocks = rings;
+  for (int b = 0; b < c->batch; ++b) blocks += (double)a.nsplit[b] * (c->n_q_heads / hpw);
+  // Few blocks rotate the queries of their heads themselves, each reading its P_qk from L2: a
+  // launch less (4 us of the host's time: 17 against 20.5 us a call for one sequence of 8 kv
+  // heads) at the same time on the GPU for 4 heads (15.1 us), for 2 at less (12.9 against 14.6).
+  // Not 8 heads (21.5 against 18.3), nor many blocks (16 sequences, 1024 blocks: 35.0 against
+  // 33.1).
+  a.rotate_here = hpw > 1 && hpw <= swan::kRotateHeads && !prefix && blocks <= 512;
   pl.prefix.slots = 0;
   if (prefix) {
     Window w;
@@ -444,6 +452,7 @@ swan_status swan_decode_step_window(const swan_prefix* prefix, const swan_cache*
     ca.Hq = c->n_q_heads;
     ca.qmult = pl.a.qmult;
     pl.a.qhat_ready = 1;
+    pl.a.rotate_here = 0;
   }
   const hipError_t e = swan::launch_compress(ca);
   if (e != hipSuccess) return hip_status(e, "compress launch");

@@ -26,9 +26,10 @@ __device__ __forceinline__ int ring_token(int L, int bb, int s) {
 // rows at a time, and the lanes' sums of the same dims meet at the end.  What bounds it is the
 // latency of its loads, so 16 of them are in flight at a time, the first values' before the
 // scores.  One query head a wave, the rows of a group's others coming from L2: two need more
-// registers than the page waves, whose kernel it is.  q: kD floats of scratch, p: 64.
+// registers than the page waves, whose kernel it is.  q: its rotated query in LDS; p: 64 floats
+// of scratch.
 template <typename E>
-__device__ void ring_wave(const WindowLaunch& a, int b, int h, int hq, int piece, float* q,
+__device__ void ring_wave(const WindowLaunch& a, int b, int h, int hq, int piece, const float* q,
                           float* p, int lane) {
   constexpr int N = 16 / (int)sizeof(E);  // elements of 16 bytes
   constexpr int kLanes = kD / N, kAtOnce = 64 / kLanes, kLoads = 16;
@@ -53,10 +54,6 @@ __device__ void ring_wave(const WindowLaunch& a, int b, int h, int hq, int piece
   };
   load_k(0);
   load_v(0);
-  const float* qh = a.qhat + ((int64_t)b * a.Hq + hq) * kD;
-  q[lane] = qh[lane];
-  q[lane + 64] = qh[lane + 64];
-  wave_lds_fence();
   const int token = ring_token(L, a.bb, 64 * piece + mine);
   const bool seen = lane < count && (token >= a.lo[b] || token < a.sink[b]);
   float s0 = 0.f, s1 = 0.f;

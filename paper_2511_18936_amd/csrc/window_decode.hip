@@ -44,7 +44,12 @@ __global__ __launch_bounds__(64) void window_kernel(WindowLaunch a, SeqGroup g) 
   w /= U;
   if (w >= g.n_splits) {
     w -= g.n_splits;
-    if (64 * w < min(a.len[b], a.bb)) ring_wave<E>(a, b, h, hq, w, qrep, acc, lane);
+    if (64 * w >= min(a.len[b], a.bb)) return;
+    const float* qh = a.qhat + ((int64_t)b * a.Hq + hq) * kD;
+    qrep[lane] = qh[lane];
+    qrep[lane + 64] = qh[lane + 64];
+    wave_lds_fence();
+    ring_wave<E>(a, b, h, hq, w, qrep, acc, lane);
     return;
   }
   const int split = w, ns = a.nsplit[b];
@@ -124,7 +129,7 @@ template <typename T>
 static hipError_t launch_window_t(const WindowLaunch& a) {
   using E = typename Fmt<T>::Elem;
   hipError_t e = hipSuccess;
-  if (!a.qhat_ready) {
+  if (!a.qhat_ready && !a.rotate_here) {
     hipLaunchKernelGGL(window_rotate_kernel<E>, dim3(a.B * a.Hq), dim3(512), 0, a.stream, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }

@@ -5,10 +5,49 @@
 
 namespace swan {
 
+// The rotated queries of N heads from hq0 on of kv head h, in `out`[head][kD] of LDS by the 128
+// threads of a block; the sums as window_rotate_kernel takes them, which this replaces.  q:
+// [N][kD] of scratch.
+template <int N>
+__device__ __forceinline__ void rotate_here(const WindowLaunch& a, int b, int h, int hq0, float* q,
+                                            float* out) {
+  const int d = threadIdx.x;
+  const float* P = a.P_qk + (int64_t)h * kD * kD + d;
+  float m[32], sum[N][4];
+  auto load = [&](int s) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) m[i] = P[(32 * s + i) * kD];
+  };
+  load(0);
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+    q[j * kD + d] = (float)((const _Float16*)a.q)[((int64_t)b * a.Hq + hq0 + j) * kD + d];
+  __syncthreads();
+#pragma unroll
+  for (int s = 0; s < 4; ++s) {
+    if (s > 0) load(s);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      float a0 = 0.f, a1 = 0.f;
+#pragma unroll
+      for (int i = 0; i < 32; i += 2) {
+        a0 = fmaf(q[j * kD + 32 * s + i], m[i], a0);
+        a1 = fmaf(q[j * kD + 32 * s + i + 1], m[i + 1], a1);
+      }
+      sum[j][s] = a0 + a1;
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+    out[j * kD + d] = ((sum[j][0] + sum[j][1]) + (sum[j][2] + sum[j][3])) * a.qmult;
+}
+
 // Grid: units * g.n_splits blocks over pages, then units * ring pieces * GH / 2, of a ring wave
 // per query head; a unit is GH query heads of one kv head of a sequence.  Two waves a SIMD, as
 // LDS allows four blocks a CU (the largest pages: one).
-template <typename T, int KP8, int GH>
+//
+// kRotate: the blocks rotate their queries themselves (swan_long_api.hip has the rule).
+template <typename T, int KP8, int GH, bool kRotate>
 __global__ __launch_bounds__(128, KP8 <= 10 ? 2 : 1) void window_gqa_kernel(WindowLaunch a, SeqGroup g) {
   constexpr int R = qrep_replicas<GH>();
   __shared__ __attribute__((aligned(16))) GqaLds<GH, kD + 1> sh;
@@ -20,9 +59,18 @@ __global__ __launch_bounds__(128, KP8 <= 10 ? 2 : 1) void window_gqa_kernel(Wind
   const int hq0 = (h * HC + ui % HC) * GH;
   if (x >= g.n_splits) {
     const int piece = (x - g.n_splits) / (GH / 2), j = (x - g.n_splits) % (GH / 2) * 2 + wave;
-    if (64 * piece < min(a.len[b], a.bb))
-      ring_wave<_Float16>(a, b, h, hq0 + j, piece, sh.qrep + wave * kD, (float*)sh.vt + wave * 64,
-                          lane);
+    if (64 * piece >= min(a.len[b], a.bb)) return;
+    float* q = sh.qrep + wave * kD;
+    if constexpr (kRotate) {
+      rotate_here<2>(a, b, h, hq0 + j - wave, (float*)sh.vt, sh.qrep);
+      __syncthreads();
+    } else {
+      const float* qh = a.qhat + ((int64_t)b * a.Hq + hq0 + j) * kD;
+      q[lane] = qh[lane];
+      q[lane + 64] = qh[lane + 64];
+      wave_lds_fence();
+    }
+    ring_wave<_Float16>(a, b, h, hq0 + j, piece, q, (float*)sh.vt + wave * 64, lane);
     return;
   }
   const int split = x, ns = a.nsplit[b];
@@ -45,10 +93,18 @@ __global__ __launch_bounds__(128, KP8 <= 10 ? 2 : 1) void window_gqa_kernel(Wind
   if constexpr (kEarly) load(ra, x0);
   {  // q_rep[dim][r][head]: thread t writes dim t, all replicas
     const int d = threadIdx.x;
-    const float* qh = a.qhat + ((int64_t)b * a.Hq + hq0) * kD;
     float q[GH];
+    if constexpr (kRotate) {
+      static_assert(sizeof(sh.vt) >= 2 * GH * kD * sizeof(float), "scratch");
+      float* qs = (float*)sh.vt;
+      rotate_here<GH>(a, b, h, hq0, qs, qs + GH * kD);  // (each thread reads its own back)
 #pragma unroll
-    for (int j = 0; j < GH; ++j) q[j] = qh[j * kD + d];
+      for (int j = 0; j < GH; ++j) q[j] = qs[(GH + j) * kD + d];
+    } else {
+      const float* qh = a.qhat + ((int64_t)b * a.Hq + hq0) * kD;
+#pragma unroll
+      for (int j = 0; j < GH; ++j) q[j] = qh[j * kD + d];
+    }
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
@@ -114,7 +170,13 @@ template <typename T, int KP8, int GH>
 static hipError_t launch_gqa_k(const WindowLaunch& a, const SeqGroup& g) {
   const int units = g.n * a.Hkv * (a.Hq / a.Hkv / GH);
   const dim3 grid(units * (g.n_splits + pages_for(a.bb) * (GH / 2)));
-  hipLaunchKernelGGL((window_gqa_kernel<T, KP8, GH>), grid, dim3(128), 0, a.stream, a, g);
+  if constexpr (GH <= kRotateHeads) {
+    if (a.rotate_here) {
+      hipLaunchKernelGGL((window_gqa_kernel<T, KP8, GH, true>), grid, dim3(128), 0, a.stream, a, g);
+      return hipGetLastError();
+    }
+  }
+  hipLaunchKernelGGL((window_gqa_kernel<T, KP8, GH, false>), grid, dim3(128), 0, a.stream, a, g);
   return hipGetLastError();
 }
 
