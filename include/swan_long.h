@@ -87,9 +87,9 @@ swan_status swan_attend_window(const swan_prefix* sources, int32_t n_sources, in
 /*
  * swan_decode_attention_window, swan_decode_step_window: as swan_decode_attention and
  * swan_decode_step, or with a prefix (not NULL) as swan_decode_attention_prefix and
- * swan_decode_step_prefix.  The query is at the position of its sequence's last token.  A step
- * gives the same results as an append and swan_decode_attention_window.  For the workspace of a
- * step ask with the lengths after it.
+ * swan_decode_step_prefix; a scale given is at least 2^-64.  The query is at the position of its
+ * sequence's last token.  A step gives the same results as an append and
+ * swan_decode_attention_window.  For the workspace of a step ask with the lengths after it.
  */
 swan_status swan_decode_window_workspace_bytes(const swan_prefix* prefix, const swan_cache* c,
                                                const int32_t* seq_len_host,

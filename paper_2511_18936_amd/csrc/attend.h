@@ -145,6 +145,48 @@ __device__ __forceinline__ void dma_tile(char* lds, const T* p, int rows, const 
                  "{m0}"(to + 1024 * x)
                  : "memory");
 }
+// The same for a tile of two pieces: rows below `bound` from p, the others as rows from `rest`.
+template <typename T>
+__device__ __forceinline__ void dma_pieces(char* lds, const T* p, int bound, const T* rest,
+                                           int rows, const DmaFrom<T>& from, int wave) {
+  typedef int i4v __attribute__((ext_vector_type(4)));
+  using R = Rows<T>;
+  rows = rows > kTileKeys ? kTileKeys : rows < 0 ? 0 : rows;
+  const uint32_t cut = (uint32_t)(bound * R::kBytes), end = (uint32_t)(rows * R::kBytes);
+  if constexpr (sizeof(T) == 4) {
+    u32x4 r[DmaFrom<T>::N];
+#pragma unroll
+    for (int x = 0; x < DmaFrom<T>::N; ++x) {
+      const char* q = (const char*)(from.at[x] < cut ? p : rest);
+      r[x] = from.at[x] < cut || from.at[x] < end ? *(const u32x4*)(q + from.at[x])
+                                                  : u32x4{0u, 0u, 0u, 0u};
+    }
+#pragma unroll
+    for (int x = 0; x < DmaFrom<T>::N; ++x)
+      *(u32x4*)(lds + wave * (R::kTile / 4) + 1024 * x + 16 * __lane_id()) = r[x];
+    return;
+  }
+  auto rsrc = [](const T* q, uint32_t bytes) {
+    return i4v{__builtin_amdgcn_readfirstlane((int)(uint32_t)(uint64_t)q),
+               __builtin_amdgcn_readfirstlane((int)(uint32_t)((uint64_t)q >> 32)),
+               __builtin_amdgcn_readfirstlane((int)bytes), 0x00020000};
+  };
+  const i4v one = rsrc(p, cut), two = rsrc(rest, end);
+  const uint32_t to = __builtin_amdgcn_readfirstlane(
+      (uint32_t)(uintptr_t)(SWAN_LDS char*)lds + wave * (R::kTile / 4));
+  // (a lane that is switched off loads and writes nothing)
+#pragma unroll
+  for (int x = 0; x < DmaFrom<T>::N; ++x) {
+    if (from.at[x] < cut)
+      asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(from.at[x]),
+                   "s"(one), "{m0}"(to + 1024 * x)
+                   : "memory");
+    else
+      asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(from.at[x]),
+                   "s"(two), "{m0}"(to + 1024 * x)
+                   : "memory");
+  }
+}
 __device__ __forceinline__ void dma_wait() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 // The products, by element type.

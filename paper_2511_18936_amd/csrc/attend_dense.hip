@@ -4,6 +4,20 @@
 
 namespace swan {
 
+// The keys of a row tile: the first `sinks`, then those from `first` to `seen`, one list.
+struct KeyList {
+  int sinks, gap, count;  // keys x of it from `sinks` on are key x + gap
+  __device__ __forceinline__ KeyList(int first, int sink, int seen)
+      : sinks(min(sink, first)), gap(first - sinks), count(seen - gap) {
+    if (gap == 0) sinks = 0;  // one piece
+  }
+  __device__ __forceinline__ int key(int x) const { return x < sinks ? x : x + gap; }
+  // whether tile t holds keys of both pieces
+  __device__ __forceinline__ bool both(int t) const {
+    return t * kTileKeys < sinks && sinks < (t + 1) * kTileKeys;
+  }
+};
+
 // Grid: a.units workgroups of 4 waves (unit_at), a group's last row tiles, of a causal prompt
 // the longest, first.
 //
@@ -23,9 +37,11 @@ namespace swan {
 // The last tile stands behind the loop, without scores to take ahead: as a condition inside
 // the loop it made registers spill.
 //
-// kWin: with a sliding window.  A row tile takes the tiles that hold the first keys, then
-// those from its first row's window on; the tiles' numbers go over the gap (key_tile), and
-// only tiles that some row of a wave does not see whole are masked.
+// kWin: with a sliding window.  A row tile takes the first keys, then those from its first
+// row's window on, one list cut into tiles, of which one may hold keys of both (KeyList); only
+// tiles that some row of a wave does not see whole are masked.  Tiles of the keys' own 64s would
+// be one or two more: 8 x 1501 rows of 32 heads on 8 over windows of 480 163 us, so 156; float32,
+// 2 x 700 rows of 8 on 2 over 288 60, so 43.
 template <typename T, bool kWin>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kernel(AttendLaunch a) {
   using Tl = Tile<T>;
@@ -59,34 +75,35 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kern
   const int all_see = sees((int)a.by_g.of(row0 + 32 * wave));
   const int block_all = sees((int)a.by_g.of(row0));
   const int seen = sees(min(toks - 1, (int)a.by_g.of(row0 + kTileRows - 1)));
-  // The window: this lane's row sees no key between `sink` and limit - window.  first, full:
-  // the workgroup's first row's first key, the wave's last row's.
+  // The window: this lane's row sees no key between `sink` and limit - window.  full: the
+  // first key that the wave's last row sees in its window.
   const int sink = kWin ? a.sink[un.j] : 0;
-  const int first = kWin ? max(0, block_all - a.window) : 0;
   const int full = kWin ? sees(min(toks - 1, (int)a.by_g.of(row0 + 32 * wave + 31))) - a.window : 0;
-  const int all_tiles = (seen + kTileKeys - 1) / kTileKeys;
-  const int skip = min(first / kTileKeys, all_tiles);  // (tiles before the window)
-  const int sink_tiles = kWin ? min((sink + kTileKeys - 1) / kTileKeys, skip) : 0;
-  const int nt = all_tiles - skip + sink_tiles;
+  const KeyList list(kWin ? max(0, block_all - a.window) : 0, sink, seen);
+  const int nt = (list.count + kTileKeys - 1) / kTileKeys;
   const int t0 = split_first(nt, un.split, un.nsplit);
   const int t1 = split_first(nt, un.split + 1, un.nsplit);
-  // the first key of tile t of these nt
-  auto key_tile = [&](int t) {
-    return kWin && t >= sink_tiles ? (t - sink_tiles + skip) * kTileKeys : t * kTileKeys;
-  };
 
   const int64_t kv0 = ((int64_t)b * a.Hkv + h) * a.m * kD;
   const T* kp = (const T*)a.k + kv0;
   const T* vp = (const T*)a.v + kv0;
   const DmaFrom<T> from = dma_from<T>(wave, lane);
   // tile t is tile t - t0 of its buffers' turns; past the last, nothing
+  auto load = [&](char* to, const T* p, int t) {
+    const int key0 = kWin ? list.key(t * kTileKeys) : t * kTileKeys;
+    if (kWin && list.both(t)) {
+      const int rest = t * kTileKeys + list.gap;
+      dma_pieces(to, p + (int64_t)key0 * kD, list.sinks - t * kTileKeys, p + (int64_t)rest * kD,
+                 keys - rest, from, wave);
+    } else {
+      dma_tile(to, p + (int64_t)key0 * kD, keys - key0, from, wave);
+    }
+  };
   auto load_k = [&](int t) {
-    if (t < t1)
-      dma_tile(kbuf[(t - t0) & 1], kp + (int64_t)key_tile(t) * kD, keys - key_tile(t), from, wave);
+    if (t < t1) load(kbuf[(t - t0) & 1], kp, t);
   };
   auto load_v = [&](int t) {
-    if (t < t1)
-      dma_tile(vbuf[(t - t0) & 1], vp + (int64_t)key_tile(t) * kD, keys - key_tile(t), from, wave);
+    if (t < t1) load(vbuf[(t - t0) & 1], vp, t);
   };
   load_k(t0);
   load_v(t0);
@@ -125,25 +142,34 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kern
         for (int e = 0; e < 4; ++e) rs.O[d][4 * i + e] = x[e] * w;
       }
   };
-  auto mask = [&](f16v (&S)[2], int key0) {
-    if (key0 + kTileKeys > all_see) {
+  auto mask = [&](f16v (&S)[2], int t) {
+    if constexpr (kWin) {
+      // In places of the list: a row sees those below limit - gap, but not from `sx` (its first
+      // keys' end) to `window` before that.
+      const int x0 = t * kTileKeys, end = limit - list.gap - x0 - 4 * (lane >> 5);
+      if (x0 + kTileKeys > all_see - list.gap) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            S[x][i] = key_of(x, i, 0) >= end ? -INFINITY : S[x][i];
+      }
+      const int sx = list.gap ? list.sinks : sink;
+      if (x0 < full - list.gap && x0 + kTileKeys > sx) {
+        const int from_x = sx - x0 - 4 * (lane >> 5);
+        const uint32_t hidden = (uint32_t)max(0, end - a.window - from_x);
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            S[x][i] = (uint32_t)(key_of(x, i, 0) - from_x) < hidden ? -INFINITY : S[x][i];
+      }
+    } else if ((t + 1) * kTileKeys > all_see) {
 #pragma unroll
       for (int x = 0; x < 2; ++x)
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-          if (key0 + key_of(x, i, lane) >= limit) S[x][i] = -INFINITY;
-    }
-    if constexpr (kWin) {
-      if (key0 < full && key0 + kTileKeys > sink) {
-        const int lo = limit - a.window;
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int key = key0 + key_of(x, i, lane);
-            if (key < lo && key >= sink) S[x][i] = -INFINITY;
-          }
-      }
+          if (t * kTileKeys + key_of(x, i, lane) >= limit) S[x][i] = -INFINITY;
     }
   };
   begin();
@@ -157,7 +183,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kern
     load_k(t + 2);
     load_v(t + 1);
     if (busy) {
-      mask(S, key_tile(t));
+      mask(S, t);
       float c = a.qmult;
       const float ref = take_scores(rs, S, c);
       rs.l += Tl::template values<true, false>(vbuf[par], S, c, ref, lane, rs.O, kbuf[par ^ 1], q,
@@ -169,7 +195,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kern
     __syncthreads();
   }
   if (busy && t0 < t1) {
-    mask(S, key_tile(t1 - 1));
+    mask(S, t1 - 1);
     float c = a.qmult;
     const float ref = take_scores(rs, S, c);
     rs.l += Tl::template values<false, false>(vbuf[(t1 - 1 - t0) & 1], S, c, ref, lane, rs.O,
@@ -185,17 +211,16 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kern
       begin();
 #pragma unroll 1
       for (int t = t0; t < t1; ++t) {
-        const int key0 = key_tile(t);
         if (tid == 0) odd_keys = 0;
-        dma_tile(kbuf[0], kp + (int64_t)key0 * kD, keys - key0, from, wave);
-        dma_tile(vbuf[0], vp + (int64_t)key0 * kD, keys - key0, from, wave);
+        load(kbuf[0], kp, t);
+        load(vbuf[0], vp, t);
         dma_wait();
         __syncthreads();
         const uint64_t mine = take_nonfinite<T, 256>(vbuf[0], tid);
         if (mine) atomicOr((unsigned long long*)&odd_keys, (unsigned long long)mine);
         __syncthreads();
         Tl::template scores<false>(kbuf[0], q, lane, S);
-        mask(S, key0);
+        mask(S, t);
         float c = a.qmult;
         const float ref = take_scores(rs, S, c);
         rs.l += Tl::template values<false, false>(vbuf[0], S, c, ref, lane, rs.O, kbuf[0], q, next);
@@ -206,10 +231,13 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kern
             for (int i = 0; i < 16; ++i)
               S[x][i] = __builtin_amdgcn_exp2f(fmaf(S[x][i], c, -ref));
           const int lo = limit - a.window;
+          auto key_at = [&](int i) {
+            return kWin ? list.key(t * kTileKeys + i) : t * kTileKeys + i;
+          };
           add_nonfinite(
-              odd, [&](int key, int d) { return (float)vp[(int64_t)(key0 + key) * kD + d]; },
-              [&](int key) {
-                key += key0;
+              odd, [&](int i, int d) { return (float)vp[(int64_t)key_at(i) * kD + d]; },
+              [&](int i) {
+                const int key = key_at(i);
                 return key < limit && (!kWin || key >= lo || key < sink);
               },
               S, lane, rs.O);

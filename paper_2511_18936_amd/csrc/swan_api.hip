@@ -787,8 +787,8 @@ swan_status prompt_prep(int32_t dtype, int32_t batch, int32_t n_q_heads, int32_t
     all += tiles[j];
     if (window > 0) {  // the tiles that a row tile's windows and the first keys take at most
       a.sink[j] = (uint16_t)(sinks_host ? sinks_host[b] : 0);
-      const int64_t most = ((int64_t)window + swan::kTileRows / G) / swan::kTileKeys + 2 +
-                           (a.sink[j] + swan::kTileKeys - 1) / swan::kTileKeys;
+      const int64_t most = ((int64_t)window + swan::kTileRows / G + 1 + a.sink[j] +
+                            swan::kTileKeys - 1) / swan::kTileKeys;
       if (most < tiles[j]) tiles[j] = (int)most;
     }
     seen += tiles[j];
@@ -798,9 +798,12 @@ swan_status prompt_prep(int32_t dtype, int32_t batch, int32_t n_q_heads, int32_t
   a.first[count] = count;
   a.groups = count;
   double cost;
-  // (windows that leave out half of a prompt's tiles make its row tiles alike)
-  const int per = plan_tiles(attend_cost(dtype, false), count, base, tiles, rows,
-                             causal != 0 && 2 * seen > all, false, cost);
+  // (windows that leave out half of a prompt's tiles make its row tiles alike, and mask more of
+  // their tiles: float32 12 us each with the mask)
+  AttendCost costs = attend_cost(dtype, false);
+  if (window > 0 && dtype == SWAN_F32) costs.tile = 12.0;
+  const int per = plan_tiles(costs, count, base, tiles, rows, causal != 0 && 2 * seen > all, false,
+                             cost);
   int64_t units = 0;
   int most = 1;
   for (int j = 0; j < count; ++j) {

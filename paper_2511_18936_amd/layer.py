@@ -133,7 +133,7 @@ class SwanAttentionLayer:
         to itself and the first `sinks` (None: all)."""
         import torch
 
-        swan._window(window, sinks)
+        swan._window(window, sinks, True)
         if window is not None and (window < 1 or sinks < 0):
             raise ValueError(f"window {window} < 1 or sinks {sinks} < 0")
         self.window, self.sinks = window, sinks

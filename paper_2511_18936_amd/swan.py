@@ -720,7 +720,10 @@ def prompt_attention(q, k, v, causal: bool = True, n: Optional[Sequence[int]] = 
     return out
 
 
-def _window(window, sinks) -> None:
+def _window(window, sinks, one: bool = False) -> None:
+    """Checks of a window and its first keys (one: a number of them, for all sequences)."""
+    if one and not isinstance(sinks, int):
+        raise SwanError(SWAN_ERR_INVALID_ARG, f"sinks must be one number here, not {sinks}")
     if window is None and (not isinstance(sinks, int) or sinks != 0):
         raise SwanError(SWAN_ERR_INVALID_ARG, "sinks without a window")
     for x in (window, sinks):
@@ -770,7 +773,7 @@ def attend(sources, q, P_qk, P_vo, n: Optional[Sequence[int]] = None, scale: flo
     is None).  P_vo None leaves o rotated.  window: row i, standing i positions behind the
     cached tokens, sees those of the last `window` positions up to itself, and the first
     `sinks`."""
-    _window(window, sinks)
+    _window(window, sinks, True)
     sources = list(sources)
     if not sources:
         raise SwanError(SWAN_ERR_INVALID_ARG, "no sources")
@@ -860,9 +863,9 @@ def prefix_workspace_bytes(prefix: Prefix, desc: CacheDesc, seq_len: Sequence[in
 
 def _window_head(desc: CacheDesc, seq_len, k_active, k_value, prefix, window, sinks):
     """The arguments that a windowed decode call and its workspace query share."""
-    _window(window, sinks)
-    if window is None or not isinstance(sinks, int):
-        raise SwanError(SWAN_ERR_INVALID_ARG, f"window {window}, sinks {sinks}")
+    _window(window, sinks, True)
+    if window is None:
+        raise SwanError(SWAN_ERR_INVALID_ARG, "window is None")
     B = desc.batch
     return (None if prefix is None else ctypes.byref(prefix._desc(B)), ctypes.byref(desc),
             _per_sequence(seq_len, B, "seq_len"), _per_sequence(k_active, B, "k_active"),

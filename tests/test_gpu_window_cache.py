@@ -324,3 +324,54 @@ def test_many_sequences_of_all_k(gpu_device, swan_mod, torch_mod):
         out = cache.decode(q, P_qk, P_vo, window=150, sinks=2)
         torch.cuda.synchronize()
         _check_decode(torch, cache, q, P_qk, P_vo, out, 150, 2, "f16")
+
+
+def test_pages_beyond_32_bit_offsets(gpu_device, swan_mod, torch_mod):
+    """The last head's pages lie past 2^32 bytes: decode, a step and rows see them."""
+    torch = torch_mod
+    hkv, tokens, capacity = 64, 300, 200000
+    cache = swan_mod.SwanCache(1, hkv, hkv, 16, capacity, [128], torch.float32, gpu_device)
+    assert cache.k_pages.numel() > 2**32
+    P = R.rotations(hkv, 3, gpu_device)
+    g = torch.Generator().manual_seed(1)
+    rows = torch.randn(1, hkv, tokens, D, generator=g).to(gpu_device)
+    cache.append(rows, rows, P, P)
+    small = swan_mod.SwanCache(1, hkv, hkv, 16, 400, [128], torch.float32, gpu_device)
+    small.append(rows, rows, P, P)
+    q = _queries(torch, gpu_device, "f32", 1, hkv, D, seed=3, sharp=1)
+    many = _queries(torch, gpu_device, "f32", 1, hkv, 40, D, seed=4, sharp=1)
+    for window, sinks in ((100, 4), (250, 0)):
+        assert torch.equal(cache.decode(q, P, P, window=window, sinks=sinks),
+                           small.decode(q, P, P, window=window, sinks=sinks))
+        a = cache.attend(many, P, P, window=window, sinks=sinks)
+        b = small.attend(many, P, P, window=window, sinks=sinks)
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    k = torch.randn(1, hkv, 1, D, generator=g).to(gpu_device)
+    assert torch.equal(cache.step(k, k, q, P, P, window=100, sinks=4),
+                       small.step(k, k, q, P, P, window=100, sinks=4))
+
+
+def test_calls_that_are_refused(gpu_device, swan_mod, torch_mod):
+    torch = torch_mod
+    cache, P_qk, P_vo = R.filled_cache(swan_mod, gpu_device, [90], 4, 2, 16, [64], "f16", 7)
+    q = _queries(torch, gpu_device, "f16", 1, 4, D)
+    rows = _queries(torch, gpu_device, "f16", 1, 4, 3, D)
+    lengths, ring = list(cache.seq_len), cache.k_ring.clone()
+    kv = _queries(torch, gpu_device, "f16", 1, 2, 1, D)
+    for kw in (dict(window=0), dict(window=-1), dict(window=4, sinks=-1), dict(sinks=3),
+               dict(window=4, sinks=70000), dict(window=2.5), dict(window=4, sinks=[1])):
+        for call in (lambda: cache.decode(q, P_qk, P_vo, **kw),
+                     lambda: cache.step(kv, kv, q, P_qk, P_vo, **kw),
+                     lambda: cache.attend(rows, P_qk, P_vo, **kw)):
+            with pytest.raises(swan_mod.SwanError):
+                call()
+    with pytest.raises(swan_mod.SwanError):
+        swan_mod.prompt_attention(rows, rows, rows, causal=False, window=3)
+    with pytest.raises(swan_mod.SwanError):
+        cache.copy_from(cache, [0])
+    with pytest.raises(swan_mod.SwanError):
+        cache.select([0], 0, [75])  # 74 tokens are pruned
+    with pytest.raises(ValueError):
+        cache.select([1])
+    torch.cuda.synchronize()
+    assert cache.seq_len == lengths and torch.equal(cache.k_ring, ring)

@@ -152,6 +152,31 @@ def test_nothing_comes_from_what_a_row_does_not_see(gpu_device, swan_mod, torch_
         assert not torch.isfinite(got[0, :, hit, 3]).any()
 
 
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("sinks", [3, 64, 70])
+def test_infinite_first_keys_reach_every_row(gpu_device, swan_mod, torch_mod, dtype, sinks):
+    """A first key and one of the windows, in a tile that holds keys of both: infinite in their
+    dim for the rows that see them, the other dims as they were."""
+    torch = torch_mod
+    n, window = 400, 30
+    q, k, v = _inputs(torch, gpu_device, 1, 3, 1, n, n, dtype, 14, sharp=0.5)
+    good = swan_mod.prompt_attention(q, k, v, window=window, sinks=sinks)
+    v[0, 0, sinks - 1, 5] = math.inf
+    v[0, 0, 200, 7] = -math.inf
+    v[0, 0, 100, 9] = math.nan
+    got = swan_mod.prompt_attention(q, k, v, window=window, sinks=sinks)
+    torch.cuda.synchronize()
+    keep = [d for d in range(D) if d not in (5, 7, 9)]
+    assert torch.equal(got[..., keep], good[..., keep])
+    assert torch.all(got[:, :, sinks - 1:, 5] == math.inf)
+    assert torch.equal(got[:, :, :sinks - 1, 5], good[:, :, :sinks - 1, 5])
+    for dim, j in ((7, 200), (9, 100)):
+        sees = torch.zeros(n, dtype=torch.bool, device=q.device)
+        sees[j:j + window] = True
+        assert torch.equal(got[:, :, ~sees, dim], good[:, :, ~sees, dim])
+        assert not torch.isfinite(got[0, :, sees, dim]).any()
+
+
 def test_the_results_repeat_and_do_not_depend_on_neighbours(gpu_device, swan_mod, torch_mod):
     torch = torch_mod
     q, k, v = _inputs(torch, gpu_device, 3, 8, 2, 500, 500, "f16", 9)
