@@ -3,6 +3,7 @@
 // (optional), then rotated to the token's position as swan_rope does it; v as it is.
 //   r = 1 / sqrt(mean_j x_j^2 + eps),  y_j = x_j r w_j,
 //   (y_j, y_{j+64}) turned by pos base^(-2j/128)
+// (or in another form, rotary.h: then also heads alone, swan_rope_rotary)
 // in float64 and rounded once, so that without weights the bits are swan_rope's.
 //
 // Bound by memory for long prompts: 8 x 8190 positions of 32 + 2 x 32 heads without norms
@@ -162,7 +163,12 @@ __device__ __forceinline__ void turn_row(Four<T>& lo, Four<T>& hi, bool norm,
 // chunks of heads): its 256 threads compute the 4 x 64 sines and cosines once for all of
 // them, then a quarter wave (16 lanes of 4 pairs, 8-byte accesses for binary16) has a head's
 // row of one position, wave w every fourth head, two at a time.
-template <typename T, int kForm>
+//
+// kStream: rows that no later call finds in the 256 MB of the last cache go past the caches (4 x
+// 32 heads x 8190 positions 113 us, 4.75 TB/s, so 91; 2 x 8191 of 32 + 2 x 8 heads with norms 94, so
+// 74).  Of fewer rows what is won so (1 us of 22 for 4095 positions) is lost by the append
+// and the attention that read them.
+template <typename T, int kForm, bool kStream = false>
 __global__ __launch_bounds__(256) void qkv_rows_kernel(QkvRowsLaunch a, int heads,
                                                        FormArg<kForm> f) {
   __shared__ f64x2 cs[kTilePos][kD / 2];
@@ -228,8 +234,14 @@ __global__ __launch_bounds__(256) void qkv_rows_kernel(QkvRowsLaunch a, int head
               turn_row<T, kForm>(lo[x], hi[x], norm, w, a.eps, c, s, turn);
             }
             T* to = out + (int64_t)(h + 4 * x) * a.n * kD;
-            *(Vec*)(to + at0) = lo[x];
-            *(Vec*)(to + at1) = hi[x];
+            if constexpr (kStream) {
+              using W = typename std::conditional<sizeof(T) == 2, u32x2, u32x4>::type;
+              __builtin_nontemporal_store(__builtin_bit_cast(W, lo[x]), (W*)(to + at0));
+              __builtin_nontemporal_store(__builtin_bit_cast(W, hi[x]), (W*)(to + at1));
+            } else {
+              *(Vec*)(to + at0) = lo[x];
+              *(Vec*)(to + at1) = hi[x];
+            }
           }
         }
         first += count;
@@ -298,6 +310,13 @@ static hipError_t launch_qkv_rows_t(const QkvRowsLaunch& a, const FormArg<kForm>
   chunks = chunks < 1 ? 1 : chunks > (H + 3) / 4 ? (H + 3) / 4 : chunks;
   const int heads = (int)(((H + chunks - 1) / chunks + 3) / 4 * 4);
   const dim3 grid((unsigned)(tiles < 2048 ? tiles : 2048), (unsigned)((H + heads - 1) / heads));
+  if constexpr (kForm != 0) {
+    if (positions * H * kD * (int64_t)sizeof(T) * 2 > ((int64_t)256 << 20)) {
+      hipLaunchKernelGGL((qkv_rows_kernel<T, kForm, true>), grid, dim3(256), 0, a.stream, a, heads,
+                         f);
+      return hipGetLastError();
+    }
+  }
   hipLaunchKernelGGL((qkv_rows_kernel<T, kForm>), grid, dim3(256), 0, a.stream, a, heads, f);
   return hipGetLastError();
 }

@@ -137,3 +137,22 @@ def test_on_another_stream_and_captured(gpu_device, swan_mod, torch_mod):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(y, want)
+
+
+@pytest.mark.parametrize("name,H", [("float16", 130), ("float32", 66)])
+def test_outputs_larger_than_the_caches(gpu_device, swan_mod, torch_mod, name, H):
+    """More than 128 MiB of outputs, in one call and in parts of it: bit for bit the same."""
+    torch = torch_mod
+    n = 4099
+    dtype = getattr(torch, name)
+    g = torch.Generator().manual_seed(H)
+    part = torch.randn(1, 7, n, D, generator=g).to(dtype).to(gpu_device)
+    x = part.repeat(1, (H + 6) // 7, 1, 1)[:, :H].contiguous()
+    r = swan_mod.Rotary(500000.0, dims=96, interleaved=True)
+    y = swan_mod.rope(x, [11], r)
+    few = swan_mod.rope(part, [11], r)
+    for h in range(0, H, 7):
+        assert torch.equal(y[:, h:h + 7], few[:, :min(7, H - h)])
+    in_place = x.clone()
+    swan_mod.rope(in_place, [11], r, out=in_place)
+    assert torch.equal(in_place, y)
