@@ -134,8 +134,6 @@ class SwanAttentionLayer:
         import torch
 
         swan._window(window, sinks, True)
-        if window is not None and (window < 1 or sinks < 0):
-            raise ValueError(f"window {window} < 1 or sinks {sinks} < 0")
         self.window, self.sinks = window, sinks
 
         d = HEAD_DIM

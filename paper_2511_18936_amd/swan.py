@@ -729,9 +729,10 @@ def _window(window, sinks, one: bool = False) -> None:
     for x in (window, sinks):
         if isinstance(x, (bool, float)):
             raise SwanError(SWAN_ERR_INVALID_ARG, f"window and sinks are whole numbers, not {x}")
-    # (ctypes would take such a number's low 32 bits)
-    if window is not None and window > 2**31 - 1 or isinstance(sinks, int) and sinks > 2**31 - 1:
-        raise SwanError(SWAN_ERR_INVALID_ARG, f"window {window} or sinks {sinks} too large")
+    # (ctypes would take the low 32 bits of numbers outside)
+    first = [sinks] if isinstance(sinks, int) else sinks
+    if window is not None and not 1 <= window < 2**31 or any(not 0 <= x < 2**31 for x in first):
+        raise SwanError(SWAN_ERR_INVALID_ARG, f"window {window} or sinks {sinks} out of range")
 
 
 def _state(state, B: int, heads: int, n: int):
@@ -1038,10 +1039,14 @@ class SwanCache:
         """Per sequence, how many pruned tokens after the first `sinks` (a number, or one per
         sequence) no later row with this window sees: the `drop` that copy_from and select can
         leave out from first=sinks on."""
-        if window < 1:
-            raise SwanError(SWAN_ERR_INVALID_ARG, f"window {window} < 1")
+        if window is None:
+            raise SwanError(SWAN_ERR_INVALID_ARG, "window is None")
+        _window(window, sinks)
         b = self.desc.buffer_tokens
         first = [sinks] * self.batch if isinstance(sinks, int) else list(sinks)
+        if len(first) != self.batch:
+            raise SwanError(SWAN_ERR_INVALID_ARG,
+                            f"sinks has {len(first)} entries for {self.batch} sequences")
         return [max(0, min(L - window + 1, L - b) - f) for L, f in zip(self.seq_len, first)]
 
     def copy_from(self, src: "SwanCache", of: Sequence[int], first=0,
@@ -1050,13 +1055,22 @@ class SwanCache:
         may be taken several times), without its tokens first .. first + drop[b] - 1 (pruned
         ones; first: a number, or one per sequence).  The tokens behind move up: keys keep the
         positions they were turned to, so a caller that counts positions adds drop[b]."""
+        import torch
+
         of = [int(p) for p in of]
         first = [first] * self.batch if isinstance(first, int) else list(first)
+        for x in (of, first, [] if drop is None else drop):  # (ctypes would take their low 32 bits)
+            if any(not -1 <= v < 2**31 for v in x):
+                raise SwanError(SWAN_ERR_INVALID_ARG, f"of, first or drop out of range: {x}")
         device = _same_gpu(src=src.k_pages, dst=self.k_pages)
         with _CallsOn(device, stream):
             copy_sequences(src.desc, src.seq_len, src.k_active, src.k_value, self.desc,
                            self.k_active, self.k_value, of, first, drop,
                            stream)
+            # src may be dropped before the copy has read it
+            at = stream or torch.cuda.current_stream(device)
+            for t in (src.k_pages, src.v_pages, src.k_ring, src.v_ring):
+                t.record_stream(at)
         for b, p in enumerate(of):
             if p >= 0:
                 self.seq_len[b] = src.seq_len[p] - (0 if drop is None else int(drop[b]))

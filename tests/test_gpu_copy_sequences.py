@@ -153,3 +153,23 @@ def test_offsets_beyond_32_bits(gpu_device, swan_mod, torch_mod):
         for r in (0, 1):
             a, b = R.cached_rows(dst, 0, h, r), R.cached_rows(src, 0, h, r)
             assert torch.equal(a, _without(torch, b, 3, 133))
+
+
+def test_a_source_dropped_at_once(gpu_device, swan_mod, torch_mod):
+    """A copy on another stream than the source's memory, which is dropped while the copy
+    waits: new tensors do not take its place before the copy has read it."""
+    torch = torch_mod
+    side = torch.cuda.Stream()
+    src, _, _ = R.filled_cache(swan_mod, gpu_device, [3000, 2500], 8, 8, 64, [48, 48], "f16", 5)
+    want = src.select([1, 0], 4, [0, 77])
+    torch.cuda.synchronize()
+    sizes = [t.numel() * t.element_size() for t in (src.k_pages, src.v_pages, src.k_ring, src.v_ring)]
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)
+        got = src.select([1, 0], 4, [0, 77])
+    del src
+    others = [torch.full((n,), 0x3C, dtype=torch.uint8, device=gpu_device) for n in sizes * 2]
+    torch.cuda.synchronize()
+    for name in ("k_pages", "v_pages", "k_ring", "v_ring"):
+        assert torch.equal(getattr(got, name), getattr(want, name)), name
+    del others

@@ -297,3 +297,36 @@ def test_sinks_and_windows_of_python():
         with pytest.raises(swan.SwanError):
             swan._window(window, sinks)
     swan._window(5, [1, 2])
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (-1, 0), (-2**31 - 1, 0), (-2**32 + 5, 0), (5, -1),
+                                          (5, -2**32 + 1), (5, [1, -2**32]), (5, [2**32, 0])])
+def test_numbers_that_32_bits_would_wrap(window, sinks):
+    """ctypes takes a number's low 32 bits: -2^31 - 1 would be a window of 2^31 - 1."""
+    with pytest.raises(swan.SwanError):
+        swan._window(window, sinks)
+    cache = swan.SwanCache(2, 2, 2, 16, 1000, [64] * 2, __import__("torch").float16, "cpu")
+    cache.seq_len = [500, 100]
+    with pytest.raises(swan.SwanError):
+        cache.outside(window, sinks)
+
+
+def test_what_a_window_leaves_takes_whole_lists():
+    cache = swan.SwanCache(3, 2, 2, 16, 1000, [64] * 3, __import__("torch").float16, "cpu")
+    cache.seq_len = [500, 100, 7]
+    for sinks in ([0], [0] * 4, -1, 1.0):
+        with pytest.raises(swan.SwanError):
+            cache.outside(50, sinks)
+    with pytest.raises(swan.SwanError):
+        cache.outside(None)
+
+
+@pytest.mark.parametrize("of,first,drop", [([2**32, 1], 0, None), ([0, 1], 2**32, [3, 3]),
+                                           ([0, 1], [0, -2**32], [3, 3]), ([0, 1], 0, [2**32 + 1, 0])])
+def test_copies_that_32_bits_would_wrap(of, first, drop):
+    torch = __import__("torch")
+    src, dst = (swan.SwanCache(2, 2, 2, 16, 1000, [64] * 2, torch.float16, "cpu") for _ in range(2))
+    src.seq_len = [500, 100]
+    with pytest.raises(swan.SwanError, match="out of range"):
+        dst.copy_from(src, of, first, drop)
+    assert dst.seq_len == [0, 0]
