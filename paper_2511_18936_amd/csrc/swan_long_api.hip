@@ -183,10 +183,10 @@ swan_status window_prep(const swan_prefix* prefix, const swan_cache* c,
   double blocks = rings;
   for (int b = 0; b < c->batch; ++b) blocks += (double)a.nsplit[b] * (c->n_q_heads / hpw);
   // Few blocks rotate the queries of their heads themselves, each reading its P_qk from L2: a
-  // launch less (4 us of the host's time: 17 against 20.5 us a call for one sequence of 8 kv
-  // heads) at the same time on the GPU for 4 heads (15.1 us), for 2 at less (12.9 against 14.6).
-  // Not 8 heads (21.5 against 18.3), nor many blocks (16 sequences, 1024 blocks: 35.0 against
-  // 33.1).
+  // launch less (4 us of the host's time), and less on the GPU too: one sequence of 8 kv heads
+  // of 4 query heads over 1024 tokens 13.9 us against 14.9, two 14.2 against 15.8, one of 16 kv
+  // heads of 2 12.7 against 14.5.  Not many blocks (8 sequences: 20.6 against 20.4), nor 8 heads,
+  // whose sums LDS has no room for.
   a.rotate_here = hpw > 1 && hpw <= swan::kRotateHeads && !prefix && blocks <= 512;
   pl.prefix.slots = 0;
   if (prefix) {

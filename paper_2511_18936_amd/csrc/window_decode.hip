@@ -31,7 +31,13 @@ __global__ __launch_bounds__(512) void window_rotate_kernel(WindowLaunch a) {
         ((part[0][j] + part[1][j]) + (part[2][j] + part[3][j])) * a.qmult;
 }
 
-// Grid: n * Hq * g.n_splits waves over pages, then n * Hq * ring pieces.
+// Grid: n * Hq * g.n_splits waves over pages, then n * Hq * ring pieces, a wave for 64 rows, last:
+// they start beside the last page waves.
+//
+// The online softmax over pages of decode_mha.h, whose slots outside the window are no tokens,
+// two pages' loads in flight.  Bound by memory: 16 sequences of 32 heads over windows of 4096 of
+// up to 6000 tokens (k = 48, 444 MB of pages and rings) 73 us, 6.1 TB/s (a streaming read reaches
+// 6.8), with the queries' rotation and the join 84.
 template <typename T, int KP8>
 __global__ __launch_bounds__(64) void window_kernel(WindowLaunch a, SeqGroup g) {
   constexpr int kRows = kD + 1;  // and the spare row

@@ -5,46 +5,60 @@
 
 namespace swan {
 
-// The rotated queries of N heads from hq0 on of kv head h, in `out`[head][kD] of LDS by the 128
-// threads of a block; the sums as window_rotate_kernel takes them, which this replaces.  q:
-// [N][kD] of scratch.
+// The rotated queries of N heads from hq0 on of kv head h, dim threadIdx.x of them in `out`, by
+// the 128 threads of a block; the sums as window_rotate_kernel takes them, which this replaces:
+// 32 lanes have a quarter of P_qk's rows, 16 bytes of each (one sequence of 8 kv heads 13.9 us a
+// call; with a dim of all rows a thread, for four times the loads and reads of LDS, 15.1).  q: [5 N][kD] of scratch.
 template <int N>
 __device__ __forceinline__ void rotate_here(const WindowLaunch& a, int b, int h, int hq0, float* q,
-                                            float* out) {
-  const int d = threadIdx.x;
-  const float* P = a.P_qk + (int64_t)h * kD * kD + d;
-  float m[32], sum[N][4];
-  auto load = [&](int s) {
+                                            float (&out)[N]) {
+  constexpr int kLoads = 16;
+  const int t = threadIdx.x, sq = t >> 5, d = 4 * (t & 31);
+  float* part = q + N * kD;
+  const float* P = a.P_qk + (int64_t)h * kD * kD + 32 * sq * kD + d;
+  f4 m[kLoads], a0[N], a1[N];
+  auto load = [&](int i0) {
 #pragma unroll
-    for (int i = 0; i < 32; ++i) m[i] = P[(32 * s + i) * kD];
+    for (int i = 0; i < kLoads; ++i) m[i] = *(const f4*)(P + (i0 + i) * kD);
   };
   load(0);
 #pragma unroll
-  for (int j = 0; j < N; ++j)
-    q[j * kD + d] = (float)((const _Float16*)a.q)[((int64_t)b * a.Hq + hq0 + j) * kD + d];
+  for (int j = 0; j < N; ++j) {
+    q[j * kD + t] = (float)((const _Float16*)a.q)[((int64_t)b * a.Hq + hq0 + j) * kD + t];
+    a0[j] = a1[j] = f4{0.f, 0.f, 0.f, 0.f};
+  }
   __syncthreads();
 #pragma unroll
-  for (int s = 0; s < 4; ++s) {
-    if (s > 0) load(s);
+  for (int i0 = 0; i0 < 32; i0 += kLoads) {
+    if (i0 > 0) load(i0);
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      float a0 = 0.f, a1 = 0.f;
+    for (int i = 0; i < kLoads; i += 2)
 #pragma unroll
-      for (int i = 0; i < 32; i += 2) {
-        a0 = fmaf(q[j * kD + 32 * s + i], m[i], a0);
-        a1 = fmaf(q[j * kD + 32 * s + i + 1], m[i + 1], a1);
-      }
-      sum[j][s] = a0 + a1;
-    }
+      for (int j = 0; j < N; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          a0[j][e] = fmaf(q[j * kD + 32 * sq + i0 + i], m[i][e], a0[j][e]);
+          a1[j][e] = fmaf(q[j * kD + 32 * sq + i0 + i + 1], m[i + 1][e], a1[j][e]);
+        }
   }
 #pragma unroll
-  for (int j = 0; j < N; ++j)
-    out[j * kD + d] = ((sum[j][0] + sum[j][1]) + (sum[j][2] + sum[j][3])) * a.qmult;
+  for (int j = 0; j < N; ++j) *(f4*)(part + (4 * j + sq) * kD + d) = a0[j] + a1[j];
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const float* p = part + 4 * j * kD + t;
+    out[j] = ((p[0] + p[kD]) + (p[2 * kD] + p[3 * kD])) * a.qmult;
+  }
 }
 
 // Grid: units * g.n_splits blocks over pages, then units * ring pieces * GH / 2, of a ring wave
 // per query head; a unit is GH query heads of one kv head of a sequence.  Two waves a SIMD, as
 // LDS allows four blocks a CU (the largest pages: one).
+//
+// Few sequences are bound by latency: one of 8 kv heads over 1024 tokens (k = 64) 10 us, the
+// chain of P_qk, a page or two, and their barriers, and 4 to join.  Many by memory and what a
+// page costs in LDS: 32 sequences of up to 8000 tokens over 4096 (331 MB of pages and rings) 76-83
+// us with the queries' rotation and the join.
 //
 // kRotate: the blocks rotate their queries themselves (swan_long_api.hip has the rule).
 template <typename T, int KP8, int GH, bool kRotate>
@@ -62,7 +76,11 @@ __global__ __launch_bounds__(128, KP8 <= 10 ? 2 : 1) void window_gqa_kernel(Wind
     if (64 * piece >= min(a.len[b], a.bb)) return;
     float* q = sh.qrep + wave * kD;
     if constexpr (kRotate) {
-      rotate_here<2>(a, b, h, hq0 + j - wave, (float*)sh.vt, sh.qrep);
+      static_assert(sizeof(sh.vt) >= 10 * kD * sizeof(float), "scratch");
+      float both[2];
+      rotate_here<2>(a, b, h, hq0 + j - wave, (float*)sh.vt, both);
+      sh.qrep[threadIdx.x] = both[0];
+      sh.qrep[kD + threadIdx.x] = both[1];
       __syncthreads();
     } else {
       const float* qh = a.qhat + ((int64_t)b * a.Hq + hq0 + j) * kD;
@@ -95,11 +113,8 @@ __global__ __launch_bounds__(128, KP8 <= 10 ? 2 : 1) void window_gqa_kernel(Wind
     const int d = threadIdx.x;
     float q[GH];
     if constexpr (kRotate) {
-      static_assert(sizeof(sh.vt) >= 2 * GH * kD * sizeof(float), "scratch");
-      float* qs = (float*)sh.vt;
-      rotate_here<GH>(a, b, h, hq0, qs, qs + GH * kD);  // (each thread reads its own back)
-#pragma unroll
-      for (int j = 0; j < GH; ++j) q[j] = qs[(GH + j) * kD + d];
+      static_assert(sizeof(sh.vt) >= 5 * GH * kD * sizeof(float), "scratch");
+      rotate_here<GH>(a, b, h, hq0, (float*)sh.vt, q);
     } else {
       const float* qh = a.qhat + ((int64_t)b * a.Hq + hq0) * kD;
 #pragma unroll
