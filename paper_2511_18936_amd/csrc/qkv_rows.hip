@@ -164,10 +164,11 @@ __device__ __forceinline__ void turn_row(Four<T>& lo, Four<T>& hi, bool norm,
 // them, then a quarter wave (16 lanes of 4 pairs, 8-byte accesses for binary16) has a head's
 // row of one position, wave w every fourth head, two at a time.
 //
-// kStream: rows that no later call finds in the 256 MB of the last cache go past the caches (4 x
-// 32 heads x 8190 positions 113 us, 4.75 TB/s, so 91; 2 x 8191 of 32 + 2 x 8 heads with norms 94, so
-// 74).  Of fewer rows what is won so (1 us of 22 for 4095 positions) is lost by the append
-// and the attention that read them.
+// kStream: rows that no later call finds in the 256 MB of the last cache go past the caches,
+// which keep more of what is read: 4 x 32 heads x 8190 positions 110 us, so 107 (5.0 TB/s) where
+// every call has other rows, and 113, so 91, with the same ones again; 2 x 8191 of 32 + 2 x 8 heads
+// with norms (the same ones) 94, so 74.  Of fewer rows what is won so (1 us of 22 for 4095
+// positions) is lost by the append and the attention that read them.
 template <typename T, int kForm, bool kStream = false>
 __global__ __launch_bounds__(256) void qkv_rows_kernel(QkvRowsLaunch a, int heads,
                                                        FormArg<kForm> f) {
