@@ -145,6 +145,33 @@ __device__ __forceinline__ void dma_tile(char* lds, const T* p, int rows, const 
                  "{m0}"(to + 1024 * x)
                  : "memory");
 }
+// A tile on its way to LDS through registers, loaded before the products that it passes (2 x 2000
+// float32 rows over windows of 700 252 us, not 255; 300 rows 23.9, not 24.5): rows
+// below `bound` from p, the others as rows from `rest`.
+template <typename T>
+struct Staged {
+  using R = Rows<T>;
+  u32x4 r[DmaFrom<T>::N];
+  uint32_t end = 0;  // bytes of the tile's rows; 0: no tile
+  __device__ __forceinline__ void load(const T* p, int bound, const T* rest, int rows,
+                                       const DmaFrom<T>& from) {
+    bound = min(bound, kTileKeys);
+    const uint32_t cut = (uint32_t)(bound * R::kBytes);
+    end = (uint32_t)(max(bound, min(rows, kTileKeys)) * R::kBytes);
+#pragma unroll
+    for (int x = 0; x < DmaFrom<T>::N; ++x) {
+      const uint32_t at = min(from.at[x], end - 16);  // (a row behind the last: zero in store)
+      r[x] = *(const u32x4*)((const char*)(at < cut ? p : rest) + at);
+    }
+  }
+  __device__ __forceinline__ void store(char* lds, const DmaFrom<T>& from, int wave) const {
+    if (end == 0) return;
+#pragma unroll
+    for (int x = 0; x < DmaFrom<T>::N; ++x)
+      *(u32x4*)(lds + wave * (R::kTile / 4) + 1024 * x + 16 * __lane_id()) =
+          from.at[x] < end ? r[x] : u32x4{0u, 0u, 0u, 0u};
+  }
+};
 // The same for a tile of two pieces: rows below `bound` from p, the others as rows from `rest`.
 template <typename T>
 __device__ __forceinline__ void dma_pieces(char* lds, const T* p, int bound, const T* rest,
@@ -154,16 +181,9 @@ __device__ __forceinline__ void dma_pieces(char* lds, const T* p, int bound, con
   rows = rows > kTileKeys ? kTileKeys : rows < 0 ? 0 : rows;
   const uint32_t cut = (uint32_t)(bound * R::kBytes), end = (uint32_t)(rows * R::kBytes);
   if constexpr (sizeof(T) == 4) {
-    u32x4 r[DmaFrom<T>::N];
-#pragma unroll
-    for (int x = 0; x < DmaFrom<T>::N; ++x) {
-      const char* q = (const char*)(from.at[x] < cut ? p : rest);
-      r[x] = from.at[x] < cut || from.at[x] < end ? *(const u32x4*)(q + from.at[x])
-                                                  : u32x4{0u, 0u, 0u, 0u};
-    }
-#pragma unroll
-    for (int x = 0; x < DmaFrom<T>::N; ++x)
-      *(u32x4*)(lds + wave * (R::kTile / 4) + 1024 * x + 16 * __lane_id()) = r[x];
+    Staged<T> tile;
+    tile.load(p, bound, rest, rows, from);
+    tile.store(lds, from, wave);
     return;
   }
   auto rsrc = [](const T* q, uint32_t bytes) {
@@ -288,19 +308,32 @@ struct Tile<float> {
     f4v hi[16];  // dims 8 s + 4 (lane / 32) .. + 3
   };
   static constexpr int kSteps = 32;
+  // A step's reads of LDS are issued before the products of the step before (sched_barrier: the
+  // scheduler would put each beside its use, where the one wave of a SIMD waits for it).  2 x
+  // 2000 rows of 16 heads on 4 over windows of 700: 255 us, not 306.
+  __device__ static __forceinline__ f4v key_piece(const char* kb, int x, int lane) {
+    return *(const SWAN_LDS f4v*)((SWAN_LDS const char*)kb + 32 * (x & 1) * R::kBytes +
+                                  R::at(lane & 31, 8 * (x >> 1) + 4 * (lane >> 5)));
+  }
+  template <bool kLow>
+  __device__ static __forceinline__ void score_step(const f4v& k, int x, const Q<kLow>& q,
+                                                    f16v (&S)[2]) {
+    if (x < 2) S[x] = f16v{};
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      S[x & 1] = __builtin_amdgcn_mfma_f32_32x32x2f32(k[e], q.hi[x >> 1][e], S[x & 1], 0, 0, 0);
+  }
   template <bool kLow>
   __device__ static __forceinline__ void scores(const char* kb, const Q<kLow>& q, int lane,
-                                                f16v (&S)[2], int s0 = 0, int s1 = kSteps) {
-    const int key = lane & 31;
+                                                f16v (&S)[2]) {
+    f4v k = key_piece(kb, 0, lane);
 #pragma unroll
-    for (int x = s0; x < s1; ++x) {
-      const int t = x & 1, s = x >> 1;
-      const f4v k = *(const SWAN_LDS f4v*)((SWAN_LDS const char*)kb + 32 * t * R::kBytes +
-                                           R::at(key, 8 * s + 4 * (lane >> 5)));
-      if (s == 0) S[t] = f16v{};
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        S[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(k[e], q.hi[s][e], S[t], 0, 0, 0);
+    for (int x = 0; x < kSteps; ++x) {
+      const f4v next = key_piece(kb, min(x + 1, kSteps - 1), lane);
+      __builtin_amdgcn_sched_barrier(0);
+      score_step<kLow>(k, x, q, S);
+      __builtin_amdgcn_sched_barrier(0);
+      k = next;
     }
   }
   template <bool kNext, bool kOdd, bool kLow>
@@ -308,21 +341,38 @@ struct Tile<float> {
                                                  float ref, int lane, f16v (&O)[4],
                                                  const char* next_k, const Q<kLow>& q,
                                                  f16v (&next)[2]) {
-    float l = 0.f;
+    struct Step {
+      f4v k;
+      float v[4];
+    };
+    // step i: keys 8 (i / 4) + i % 4 and 4 further, and step i of the next tile's scores
+    auto load = [&](int i) {
+      Step st;
+      if constexpr (kNext) st.k = key_piece(next_k, i, lane);
+      const int key = 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3);
 #pragma unroll
-    for (int s = 0; s < 8; ++s) {
-      if constexpr (kNext) scores<kLow>(next_k, q, lane, next, 4 * s, 4 * s + 4);
+      for (int d = 0; d < 4; ++d)
+        st.v[d] = *(const SWAN_LDS float*)((SWAN_LDS const char*)vb + R::at(key, 32 * d + (lane & 31)));
+      return st;
+    };
+    auto weight = [&](int i) {
+      return __builtin_amdgcn_exp2f(fmaf(S[i >> 4][i & 15], c, -ref));
+    };
+    float l = 0.f, p = weight(0);
+    Step st = load(0);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(S[s >> 2][4 * (s & 3) + e], c, -ref));
-        l += p;
-        const int key = 8 * s + 4 * (lane >> 5) + e;
+    for (int i = 0; i < kSteps; ++i) {
+      const Step after = load(min(i + 1, kSteps - 1));
+      __builtin_amdgcn_sched_barrier(0);
+      const float p1 = weight(min(i + 1, kSteps - 1));
+      l += p;
+      if constexpr (kNext) score_step<kLow>(st.k, i, q, next);
 #pragma unroll
-        for (int d = 0; d < 4; ++d)
-          O[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(
-              *(const SWAN_LDS float*)((SWAN_LDS const char*)vb + R::at(key, 32 * d + (lane & 31))),
-              p, O[d], 0, 0, 0);
-      }
+      for (int d = 0; d < 4; ++d)
+        O[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(st.v[d], p, O[d], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      st = after;
+      p = p1;
     }
     return l;
   }

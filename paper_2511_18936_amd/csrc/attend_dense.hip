@@ -41,9 +41,9 @@ struct KeyList {
 // row's window on, one list cut into tiles, of which one may hold keys of both (KeyList); only
 // tiles that some row of a wave does not see whole are masked.  Tiles of the keys' own 64s would
 // be one or two more: 8 x 1501 rows of 32 heads on 8 over windows of 480 163 us, so 156; float32,
-// 2 x 700 rows of 8 on 2 over 288 60, so 43.  16383 rows of 32 heads on 8 over windows of 4096
+// 2 x 700 rows of 8 on 2 over 288 60, so 43 (39 since tiles read LDS a step ahead, attend.h).  16383 rows of 32 heads on 8 over windows of 4096
 // 1370-1410 us by machine, 1030-1050 TFLOP/s of products done; 8 x up to 1501 rows over windows of
-// 500 95 us, of which 70 are starts, queries and outputs.
+// 500 95-99 us, of 250 79, of 64 59, of 1 47: the starts, queries and outputs of 3.3 rounds.
 template <typename T, bool kWin>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kernel(AttendLaunch a) {
   using Tl = Tile<T>;
@@ -107,9 +107,28 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kern
   auto load_v = [&](int t) {
     if (t < t1) load(vbuf[(t - t0) & 1], vp, t);
   };
-  load_k(t0);
-  load_v(t0);
-  load_k(t0 + 1);
+  // float32: the same in two halves, a tile's loads and its way to LDS
+  auto stage = [&](const T* p, int t) {
+    Staged<T> tile;
+    if (t >= t1) return tile;
+    const int key0 = kWin ? list.key(t * kTileKeys) : t * kTileKeys;
+    const bool both = kWin && list.both(t);
+    const int rest = both ? t * kTileKeys + list.gap : key0;
+    tile.load(p + (int64_t)key0 * kD, both ? list.sinks - t * kTileKeys : keys - key0,
+              p + (int64_t)rest * kD, keys - rest, from);
+    return tile;
+  };
+  constexpr bool kStage = sizeof(T) == 4;
+  Staged<T> first[3];
+  if constexpr (kStage) {
+    first[0] = stage(kp, t0);
+    first[1] = stage(vp, t0);
+    first[2] = stage(kp, t0 + 1);
+  } else {
+    load_k(t0);
+    load_v(t0);
+    load_k(t0 + 1);
+  }
 
   typename Tl::template Q<false> q;
   {
@@ -176,14 +195,25 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kern
   };
   begin();
   f16v S[2], next[2];
+  if constexpr (kStage) {
+    first[0].store(kbuf[0], from, wave);
+    first[1].store(vbuf[0], from, wave);
+    first[2].store(kbuf[1], from, wave);
+  }
   dma_wait();
   __syncthreads();
   if (busy && t0 < t1) Tl::template scores<false>(kbuf[0], q, lane, S);
   __syncthreads();
   for (int t = t0; t < t1 - 1; ++t) {
     const int par = (t - t0) & 1;
-    load_k(t + 2);
-    load_v(t + 1);
+    Staged<T> k2, v1;
+    if constexpr (kStage) {
+      k2 = stage(kp, t + 2);
+      v1 = stage(vp, t + 1);
+    } else {
+      load_k(t + 2);
+      load_v(t + 1);
+    }
     if (busy) {
       mask(S, t);
       float c = a.qmult;
@@ -192,6 +222,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kern
                                                next);
       S[0] = next[0];
       S[1] = next[1];
+    }
+    if constexpr (kStage) {
+      k2.store(kbuf[par], from, wave);
+      v1.store(vbuf[par ^ 1], from, wave);
     }
     dma_wait();
     __syncthreads();

@@ -799,9 +799,9 @@ swan_status prompt_prep(int32_t dtype, int32_t batch, int32_t n_q_heads, int32_t
   a.groups = count;
   double cost;
   // (windows that leave out half of a prompt's tiles make its row tiles alike, and mask more of
-  // their tiles: float32 12 us each with the mask)
+  // their tiles: float32 10 us each with the mask)
   AttendCost costs = attend_cost(dtype, false);
-  if (window > 0 && dtype == SWAN_F32) costs.tile = 12.0;
+  if (window > 0 && dtype == SWAN_F32) costs.tile = 10.0;
   const int per = plan_tiles(costs, count, base, tiles, rows, causal != 0 && 2 * seen > all, false,
                              cost);
   int64_t units = 0;
