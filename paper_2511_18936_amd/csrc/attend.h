@@ -146,8 +146,8 @@ __device__ __forceinline__ void dma_tile(char* lds, const T* p, int rows, const 
                  : "memory");
 }
 // A tile on its way to LDS through registers, loaded before the products that it passes (2 x 2000
-// float32 rows over windows of 700 252 us, not 255; 300 rows 23.9, not 24.5): rows
-// below `bound` from p, the others as rows from `rest`.
+// float32 rows over windows of 700 252 us, not 255; 300 rows 23.9, not 24.5): rows below `bound`
+// from p, the others as rows from `rest`.
 template <typename T>
 struct Staged {
   using R = Rows<T>;
@@ -352,7 +352,8 @@ struct Tile<float> {
       const int key = 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3);
 #pragma unroll
       for (int d = 0; d < 4; ++d)
-        st.v[d] = *(const SWAN_LDS float*)((SWAN_LDS const char*)vb + R::at(key, 32 * d + (lane & 31)));
+        st.v[d] = *(const SWAN_LDS float*)((SWAN_LDS const char*)vb +
+                                           R::at(key, 32 * d + (lane & 31)));
       return st;
     };
     auto weight = [&](int i) {
