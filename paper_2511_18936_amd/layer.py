@@ -221,7 +221,8 @@ class SwanAttentionLayer:
         """Leaves out of the cache the pruned tokens that no later row sees through the window,
         with room for `capacity` pruned tokens from now on (None: as before).  The tokens kept
         are copied as they are, so later results stay the same.  Returns how many were left out
-        of each sequence."""
+        of each sequence.  The layer has new cache arrays then: a graph captured before would go on
+        with the old ones, which are dropped here."""
         if self.window is None:
             raise ValueError("a layer without a window sees every token")
         first = self._own_sinks(0)

@@ -452,6 +452,8 @@ class Rotary:
         self._check_factor(factor)
         if not 0 < low < high:
             raise SwanError(SWAN_ERR_INVALID_ARG, f"low {low} and high {high}: 0 < low < high")
+        if not original > 0 or math.isinf(original):
+            raise SwanError(SWAN_ERR_INVALID_ARG, f"original {original} must be finite, > 0")
         if magnitude is None:
             magnitude = 0.1 * math.log(factor) + 1.0 if factor > 1 else 1.0
         freqs = []
@@ -1079,7 +1081,8 @@ class SwanCache:
                sparse_capacity: Optional[int] = None, stream=None) -> "SwanCache":
         """A new cache of len(of) sequences, sequence b a copy of sequence of[b] (-1: empty):
         forks, a new order, without finished sequences, with another capacity, or (first, drop
-        as in copy_from) without tokens that are not needed any more."""
+        as in copy_from) without tokens that are not needed any more.  (Graphs captured with this
+        cache go on with this one.)"""
         of = [int(p) for p in of]
         if any(not -1 <= p < self.batch for p in of):
             raise ValueError(f"of must be sequences of this cache, -1..{self.batch - 1}")

@@ -330,3 +330,9 @@ def test_copies_that_32_bits_would_wrap(of, first, drop):
     with pytest.raises(swan.SwanError, match="out of range"):
         dst.copy_from(src, of, first, drop)
     assert dst.seq_len == [0, 0]
+
+
+@pytest.mark.parametrize("original", [0, -4096, float("nan"), float("inf")])
+def test_the_original_context_is_one(original):
+    with pytest.raises(swan.SwanError):
+        swan.Rotary(10000.0).by_parts(4.0, original)
