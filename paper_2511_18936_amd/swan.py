@@ -980,6 +980,8 @@ class SwanCache:
         if self.k_value is not None and len(self.k_value) != batch:
             raise ValueError("k_value needs one entry per sequence")
         self.seq_len = [0] * batch
+        # sequences copied with tokens left out: their length then, and the first token behind the gap
+        self._cuts = {}
         self.desc = CacheDesc(batch, n_q_heads, n_kv_heads, head_dim, buffer_tokens,
                               sparse_capacity, dtype_code(dtype, sparse_values), 0, None, None,
                               None, None)
@@ -1013,7 +1015,14 @@ class SwanCache:
                         n_new_per_seq, stream, self.k_value)
         n = int(k_new.shape[2])
         per = [n] * self.batch if n_new_per_seq is None else [int(x) for x in n_new_per_seq]
-        self.seq_len = [L + m for L, m in zip(self.seq_len, per)]
+        self._grow([L + m for L, m in zip(self.seq_len, per)])
+
+    def _grow(self, seq_len) -> None:
+        """The lengths after an append.  A sequence that grows forgets how it was cut."""
+        if self._cuts:
+            self._cuts = {b: cut for b, cut in self._cuts.items()
+                          if cut[0] == self.seq_len[b] == seq_len[b]}
+        self.seq_len = seq_len
 
     def change_k(self, k_active: Sequence[int], k_value: Optional[Sequence[int]] = None,
                  stream=None) -> None:
@@ -1037,10 +1046,13 @@ class SwanCache:
         self.desc, self.k_pages, self.v_pages = dst, k_pages, v_pages
         self.k_active, self.k_value = k_active, k_value
 
-    def outside(self, window: int, sinks=0):
+    def outside(self, window: int, sinks=0, decode: bool = False):
         """Per sequence, how many pruned tokens after the first `sinks` (a number, or one per
         sequence) no later row with this window sees: the `drop` that copy_from and select can
-        leave out from first=sinks on."""
+        leave out from first=sinks on.  Later rows are those of step() and attend(), and of
+        decode() after an append; decode() before it stands at the last cached token, one row
+        earlier: decode=True keeps what that sees too (without, decode() with this window
+        refuses the copy until a token is appended)."""
         if window is None:
             raise SwanError(SWAN_ERR_INVALID_ARG, "window is None")
         _window(window, sinks)
@@ -1049,7 +1061,26 @@ class SwanCache:
         if len(first) != self.batch:
             raise SwanError(SWAN_ERR_INVALID_ARG,
                             f"sinks has {len(first)} entries for {self.batch} sequences")
-        return [max(0, min(L - window + 1, L - b) - f) for L, f in zip(self.seq_len, first)]
+        hidden = [L - window + (0 if decode else 1) for L in self.seq_len]
+        return [max(0, min(x, L - b) - f) for x, L, f in zip(hidden, self.seq_len, first)]
+
+    def _check_last_row(self, window: int, sinks: int, prefix: Optional[Prefix]) -> None:
+        """Refuses a decode call whose window shows one more token than the copies that cut its
+        sequences kept: its row stands one before the rows that outside() speaks of."""
+        _window(window, sinks, True)
+        of = None if prefix is None else prefix.of or [0] * self.batch
+        for b in range(self.batch):
+            held = [(self, b)]
+            if not self.seq_len[b] and of is not None and len(of) == self.batch and \
+                    0 <= of[b] < prefix.cache.batch:
+                held.append((prefix.cache, of[b]))
+            for cache, p in held:
+                length, first = cache._cuts.get(p, (-1, 0))
+                if length == cache.seq_len[p] and length - window == first - 1:
+                    raise SwanError(SWAN_ERR_INVALID_ARG,
+                                    f"decode: the token before the last {window - 1} of sequence "
+                                    f"{b} was left out of a copy (outside(..., decode=True) keeps "
+                                    "it)")
 
     def copy_from(self, src: "SwanCache", of: Sequence[int], first=0,
                   drop: Optional[Sequence[int]] = None, stream=None) -> None:
@@ -1074,8 +1105,15 @@ class SwanCache:
             for t in (src.k_pages, src.v_pages, src.k_ring, src.v_ring):
                 t.record_stream(at)
         for b, p in enumerate(of):
-            if p >= 0:
-                self.seq_len[b] = src.seq_len[p] - (0 if drop is None else int(drop[b]))
+            if p < 0:
+                continue
+            left_out = 0 if drop is None else int(drop[b])
+            self.seq_len[b] = src.seq_len[p] - left_out
+            self._cuts.pop(b, None)
+            if left_out:
+                self._cuts[b] = (self.seq_len[b], first[b])
+            elif p in src._cuts:
+                self._cuts[b] = src._cuts[p]
 
     def select(self, of: Sequence[int], first=0, drop: Optional[Sequence[int]] = None,
                sparse_capacity: Optional[int] = None, stream=None) -> "SwanCache":
@@ -1089,7 +1127,7 @@ class SwanCache:
         new = copy.copy(self)
         new.k_active = [self.k_active[max(p, 0)] for p in of]
         new.k_value = None if self.k_value is None else [self.k_value[max(p, 0)] for p in of]
-        new.seq_len = [0] * len(of)
+        new.seq_len, new._cuts = [0] * len(of), {}
         d = self.desc
         new.desc = CacheDesc(len(of), d.n_q_heads, d.n_kv_heads, d.head_dim, d.buffer_tokens,
                              d.sparse_capacity if sparse_capacity is None else sparse_capacity,
@@ -1132,6 +1170,8 @@ class SwanCache:
         if out is None:
             out = _result_like(q, q.shape, stream)
         if window is not None or sinks:
+            if self._cuts or prefix is not None and prefix.cache._cuts:
+                self._check_last_row(window, sinks, prefix)
             decode_window(self.desc, self.seq_len, self.k_active, q, P_qk, P_vo, out, None, window,
                           sinks, scale, stream, self.k_value, prefix)
         elif prefix is None:
@@ -1154,7 +1194,7 @@ class SwanCache:
         if window is not None or sinks:
             decode_window(self.desc, self.seq_len, self.k_active, q, P_qk, P_vo, out, None, window,
                           sinks, scale, stream, self.k_value, prefix, (k_new, v_new))
-            self.seq_len = after
+            self._grow(after)
             return out
         ws = self.workspace(after, prefix, stream)
         if prefix is None:
@@ -1163,5 +1203,5 @@ class SwanCache:
         else:
             decode_step_prefix(prefix, self.desc, self.seq_len, self.k_active, k_new, v_new, q,
                                P_qk, P_vo, out, ws, scale, stream, self.k_value)
-        self.seq_len = after
+        self._grow(after)
         return out
