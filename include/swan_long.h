@@ -90,6 +90,8 @@ swan_status swan_attend_window(const swan_prefix* sources, int32_t n_sources, in
  * swan_decode_step_prefix; a scale given is at least 2^-64.  The query is at the position of its
  * sequence's last token.  A step gives the same results as an append and
  * swan_decode_attention_window.  For the workspace of a step ask with the lengths after it.
+ * Their plan is their own: swan_set_decode_tuning does not change it, and
+ * swan_set_profile_events records nothing around them.
  */
 swan_status swan_decode_window_workspace_bytes(const swan_prefix* prefix, const swan_cache* c,
                                                const int32_t* seq_len_host,
@@ -115,7 +117,9 @@ swan_status swan_decode_step_window(const swan_prefix* prefix, const swan_cache*
  * sequence b becomes sequence of_host[b] of src, whose tokens first_host[b] .. first_host[b] +
  * drop_host[b] - 1 are left out (drop_host NULL: none; first_host NULL: 0).  The copy has
  * src_len_host[of] - drop tokens, numbered anew from 0: a caller that turns keys to absolute
- * positions keeps count of the tokens left out.  Only pruned tokens can be left out, so first +
+ * positions keeps count of the tokens left out.  A window of W shows a query at the copy's last
+ * token (swan_decode_attention_window) the source's tokens from src_len_host[of] - W on, the next row
+ * those from one further.  Only pruned tokens can be left out, so first +
  * drop is src_len_host[of] - buffer_tokens at most.  A sequence of dst with of_host[b] = -1 stays
  * as it is, so do the slots behind a copy's last token.  The same source may be taken several
  * times.

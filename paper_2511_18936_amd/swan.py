@@ -939,7 +939,7 @@ def copy_sequences(src: CacheDesc, src_len: Sequence[int], k_active_src: Sequenc
 
 def set_decode_tuning(target_waves: int = 0, short_split_pages: int = 0, merge_pct: int = 0,
                       side_streams: int = 0) -> None:
-    """Split plan and launch grouping of the decode calls on this thread
+    """Split plan and launch grouping of the decode calls without a window on this thread
     (swan_set_decode_tuning; 0 = the default, -1 = off where the header allows it).
     With every argument 0 the defaults are restored."""
     t = DecodeTuning(target_waves, short_split_pages, merge_pct, side_streams)
@@ -948,8 +948,8 @@ def set_decode_tuning(target_waves: int = 0, short_split_pages: int = 0, merge_p
 
 def set_profile_events(start=None, stop=None) -> None:
     """Record start/stop (events with a .cuda_event HIP handle: torch.cuda.Event, or one
-    made for timing only) around the attention kernels of the next decode calls on
-    this thread (None, None disables)."""
+    made for timing only) around the attention kernels of the next decode calls without a
+    window on this thread (None, None disables)."""
     _check(_lib.swan_set_profile_events(None if start is None else start.cuda_event,
                                         None if stop is None else stop.cuda_event))
 
