@@ -37,7 +37,9 @@ __global__ __launch_bounds__(512) void window_rotate_kernel(WindowLaunch a) {
 // The online softmax over pages of decode_mha.h, whose slots outside the window are no tokens,
 // two pages' loads in flight.  Bound by memory: 16 sequences of 32 heads over windows of 4096 of
 // up to 6000 tokens (k = 48, 444 MB of pages and rings) 73 us, 6.1 TB/s (a streaming read reaches
-// 6.8), with the queries' rotation and the join 84.
+// 6.8), with the queries' rotation and the join 83.  Groups of odd size, and float32 ones, take it
+// too, a wave for each of their heads: 16 sequences of 24 heads on 8 over windows of 4096 (k = 64,
+// 204 MB) 113 us, where a page is loaded three times.
 template <typename T, int KP8>
 __global__ __launch_bounds__(64) void window_kernel(WindowLaunch a, SeqGroup g) {
   constexpr int kRows = kD + 1;  // and the spare row

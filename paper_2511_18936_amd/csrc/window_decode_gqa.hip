@@ -56,9 +56,12 @@ __device__ __forceinline__ void rotate_here(const WindowLaunch& a, int b, int h,
 // LDS allows four blocks a CU (the largest pages: one).
 //
 // Few sequences are bound by latency: one of 8 kv heads over 1024 tokens (k = 64) 10 us, the
-// chain of P_qk, a page or two, and their barriers, and 4 to join.  Many by memory and what a
-// page costs in LDS: 32 sequences of up to 8000 tokens over 4096 (331 MB of pages and rings) 76-83
-// us with the queries' rotation and the join.
+// chain of P_qk, a page or two, and their barriers, and 4 to join.  Many: 32 sequences of up to
+// 8000 tokens over 4096 (331 MB of pages and rings) 76-83 us with the queries' rotation and the
+// join, 32 of 8000 (407 MB) 84, of 8-bit values (277 MB) 70: 4.0-4.9 TB/s, where the call without a
+// window moves 5.9-6.1 with the same work a page.  What differs are short splits, each filling its
+// query replicas, the ring's workgroups, which hold LDS for pages, and two more launches; their
+// shares are not measured.
 //
 // kRotate: the blocks rotate their queries themselves (swan_long_api.hip has the rule).
 template <typename T, int KP8, int GH, bool kRotate>

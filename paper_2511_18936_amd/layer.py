@@ -19,8 +19,8 @@ dense, causal kind over the rows themselves (swan_prompt_attention), continued f
 swan_attend over what is cached before them (pruned tokens as they are stored).  Sequences
 can stand behind a prefix that another layer's cache holds once for all of them (fork).
 With a sliding window all of these see the last `window` tokens and the first `sinks` alone
-(swan_long.h), and compact() gives back the memory of those that no row sees any more; the
-positions count on.  select() makes a layer of copies of some sequences.
+(swan_long.h), and compact() leaves out those that no row sees any more, so that a capacity of
+the window's size is enough; the positions count on.  select() makes a layer of copies of some sequences.
 The SWAN steps run in libswan's kernels.
 Weights are [in][out] row-major, x . W.
 """
@@ -219,9 +219,10 @@ class SwanAttentionLayer:
 
     def compact(self, capacity: Optional[int] = None):
         """Leaves out of the cache the pruned tokens that no later row sees through the window,
-        with room for `capacity` pruned tokens from now on (None: as before).  The tokens kept
-        are copied as they are, so later results stay the same.  Returns how many were left out
-        of each sequence.  The layer has new cache arrays then: a graph captured before would go on
+        with room for `capacity` pruned tokens from now on.  None: as before, so the cache takes as
+        much memory as it did; a smaller number gives the rest back.  (Both caches are held until
+        the copy is enqueued.)  The tokens kept are copied as they are, so the results of later
+        rows stay the same.  Returns how many were left out of each sequence.  The layer has new cache arrays then: a graph captured before would go on
         with the old ones, which are dropped here."""
         if self.window is None:
             raise ValueError("a layer without a window sees every token")
