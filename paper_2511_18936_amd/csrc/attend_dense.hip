@@ -42,9 +42,9 @@ struct KeyList {
 // tiles that some row of a wave does not see whole are masked.  Tiles of the keys' own 64s would
 // be one or two more: 8 x 1501 rows of 32 heads on 8 over windows of 480 163 us, so 156; float32,
 // 2 x 700 rows of 8 on 2 over 288 60, so 43.  16383 rows of 32 heads on 8 over windows of 4096
-// 1368-1416 us by machine (1411-1423 under a kernel trace), 1015-1055 TFLOP/s of products done; 8 x up
-// to 1501 rows over windows of 500 93-99 us (100-112), of 250 79, of 64 59, of 1 47: the starts,
-// queries and outputs of 3.3 rounds.
+// 1364-1416 us by machine (1411-1423 under a kernel trace), 1015-1060 TFLOP/s of products done;
+// 8 x up to 1501 rows over windows of 500 93-99 us (100-112), of 250 79, of 64 59, of 1 47: the
+// starts, queries and outputs of 3.3 rounds.
 // Float32: 10 us a tile of 128 rows, 7 of them products.
 template <typename T, bool kWin>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attend_dense_kernel(AttendLaunch a) {

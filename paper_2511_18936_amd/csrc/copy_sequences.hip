@@ -16,12 +16,12 @@ constexpr int kCopyRing = 64;  // ring rows of a workgroup
 // 6.4 TB/s, where each call has other caches; 76 us with the same ones again, which the 256 MB of
 // the last cache hold in part.  32 of up to 8000 tokens, 8 heads, k = 64, cut to windows of 4096
 // that begin anywhere in a page: 83 us, 6.4 TB/s, and 80.
-// Non-temporal stores: copies of 300 MB 102 us, with ordinary stores 112, of 96 MB 37 and 40, of 26
-// MB 13.2 and 14.4, each call with other caches; below 10 MB no difference.  They leave the copy to
-// be read from HBM: with the first decode over it 167 and 169 us, 73 and 69, 38 and 37, so up to some
-// 200 MB a copy that is read at once would gain 1-5 % by ordinary ones.  With the same caches again:
-// non-temporal loads 78 us for 77, but 88 for tokens moved within their pages, and both 83 and 94;
-// loads four chunks ahead gain nothing.
+// Non-temporal stores: copies of 300 MB 102 us, with ordinary stores 112, of 96 MB 37 and 40, of
+// 26 MB 13.2 and 14.4, each call with other caches; below 10 MB no difference.  They leave the
+// copy to be read from HBM: with the first decode over it 167 and 169 us, 73 and 69, 38 and 37, so
+// up to some 200 MB a copy that is read at once would gain 1-5 % by ordinary ones.  With the same
+// caches again: non-temporal loads 78 us for 77, but 88 for tokens moved within their pages, and
+// both 83 and 94; loads four chunks ahead gain nothing.
 template <int VB>
 __global__ __launch_bounds__(256) void copy_kernel(CopyLaunch a) {
   constexpr int CB = VB == 1 ? 8 : 16, VCH = 8 * VB / CB;

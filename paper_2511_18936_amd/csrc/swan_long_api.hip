@@ -37,10 +37,11 @@ swan_status rotary_form(const swan_rotary* r, int32_t head_dim, swan::RotaryForm
 // role have one wave a SIMD, half as many; and one launch is taken for the whole batch, though
 // sequences of several k go out in one for each of their tiers, one after another (16 sequences
 // of 32 heads on 8 over windows of 4096 with k of 32, 48, 64 and 96 in turn 127 us, with k = 60
-// 50; of 32 heads without groups 196 and 136).  A plan's time is taken as that of its longest split, or of all pages
-// spread evenly, in one such round, or as rounds, or as spread evenly with half a workgroup's time
-// more; then `rings` workgroups of the ring, of 5, which find room beside a first round that
-// leaves some (32 sequences x 8 kv heads: 75 us with 848 workgroups, 92 with 1000 and with 1048).
+// 50; of 32 heads without groups 196 and 136).  A plan's time is taken as that of its longest
+// split, or of all pages spread evenly, in one such round, or as rounds, or as spread evenly with
+// half a workgroup's time more; then `rings` workgroups of the ring, of 5, which find room beside
+// a first round that leaves some (32 sequences x 8 kv heads: 75 us with 848 workgroups, 92 with
+// 1000 and with 1048).
 // 2 us to start, and for a page (of `entries` in both roles) 1024 of them at 10 TB/s (8-bit
 // values no less: their LDS work is that of 16-bit ones).  Of eleven plans measured for each of
 // nine shapes (1 to 32 sequences, 8 to 64 heads, one k a batch) it takes the best or one within

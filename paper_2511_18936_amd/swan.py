@@ -1166,7 +1166,8 @@ class SwanCache:
     def decode(self, q, P_qk, P_vo, out=None, scale: float = 0.0, stream=None,
                prefix: Optional[Prefix] = None, window: Optional[int] = None, sinks: int = 0):
         """Attention of q ([B][H_q][d]) over the cache, behind a prefix where one is given.
-        window: over the last `window` tokens and the first `sinks` alone."""
+        window: over the last `window` tokens and the first `sinks` alone (an error where a copy
+        cut for later rows, see outside(), left out the first of these `window`)."""
         if out is None:
             out = _result_like(q, q.shape, stream)
         if window is not None or sinks:
